@@ -57,7 +57,7 @@
 extern "C" {
 #endif
 
-#define FASQ_ABI_VERSION 6
+#define FASQ_ABI_VERSION 7
 
 typedef enum {
   FASQ_OK = 0,
@@ -356,6 +356,207 @@ void fasq_launch_list_destroy(fasq_launch_list* list);
 fasq_status fasq_pq_reconstruct(const void* idx, int64_t N, int64_t K, int idx_bits, int d,
                                 const void* codebook, int64_t C, void* w,
                                 hipStream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Between the projections of a decoder layer: rotary positions and the write
+ * of a paged cache, attention over that cache, the residual stream's norms,
+ * and low-rank adapters beside the projections.  As everywhere in the
+ * library the values are fp16, sums and softmax statistics are fp32, every
+ * call is asynchronous on `stream`, allocates nothing and can be captured in
+ * a hipGraph or recorded into a launch list.  What changes from step to step
+ * (positions, slots, lengths, page tables, adapter ids) is read from device
+ * memory when the kernels run, so one recorded step serves every step of the
+ * same shape.  Zero tokens (T or M = 0) is a valid call that launches
+ * nothing.  Strides are in elements; the last dimension of every tensor is
+ * contiguous.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * A paged cache of keys and values: element i of head h in slot t of page p
+ * is k[p * page_stride + t * slot_stride + h * head_stride + i], and the same
+ * for v.  So [pages x page_size x heads x D] and [pages x heads x page_size x
+ * D] are both caches.  Offsets are formed in 64 bits.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  int64_t num_pages;
+  int64_t page_size;
+  int64_t page_stride, slot_stride, head_stride;
+} fasq_kv_cache;
+
+/*
+ * Rotary table: table[p][i] = (cos(p w_i), sin(p w_i)) * scale for positions
+ * 0 <= p < positions and the `half` frequencies w_i of inv_freq, a HOST array
+ * (copied during the call).  Angles are formed in 64 bits and each value is
+ * rounded to fp32 once, so that the table is as good at position 131072 as
+ * at 0.  Scaled variants for long contexts differ in w and scale only.
+ *
+ *   table  out: fp32 [positions x half x 2], 8-byte aligned
+ *
+ * Returns FASQ_ERR_INVALID_ARG (half outside [1, 128]; positions < 1 or above
+ * 2^31; a NULL or misaligned pointer) or FASQ_ERR_HIP.
+ */
+fasq_status fasq_rope_table(const double* inv_freq, int half, int64_t positions, double scale,
+                            float* table, hipStream_t stream);
+
+/*
+ * Rotary positions of T new tokens, and the write of their keys and values
+ * to the cache.  For each token t and head of q and k:
+ *
+ *   x = head, or, with a norm weight w,  x = head / sqrt(mean(head^2) + eps) * w
+ *   (x_a, x_b) -> (x_a c - x_b s, x_b c + x_a s),  (c, s) = table[positions[t]][i]
+ *
+ * for the rot / 2 pairs i: (a, b) = (i, i + rot / 2), or (2i, 2i + 1) with
+ * `interleaved`.  Dimensions from rot on are not turned.  q goes to q_out; k
+ * and the unchanged v go to cache slot slots[t] = page * page_size + offset.
+ * Arithmetic is fp32, rounded to fp16 once.
+ *
+ *   q, q_out    fp16 [T x Hq x D] with token and head strides; q_out may be q
+ *               (with the same strides).  Both NULL: keys and values only
+ *   k, v        fp16 [T x Hkv x D] with strides; both NULL (cache and slots
+ *               are then not used): queries only
+ *   D           1 <= D <= 256
+ *   table, table_positions, rot
+ *               the table of fasq_rope_table with rot / 2 frequencies; rot
+ *               even, 0 <= rot <= D.  rot = 0: no rotation (table and
+ *               positions are not used)
+ *   positions   int32 [T]; a position outside [0, table_positions) turns its
+ *               token into NaN (in q_out and in the cache's k)
+ *   slots       int32 [T], distinct; a slot outside [0, num_pages *
+ *               page_size) is not written (padding tokens: -1)
+ *   q_norm, k_norm  fp16 [D] or NULL
+ *
+ * Returns FASQ_ERR_INVALID_ARG or FASQ_ERR_HIP.
+ */
+fasq_status fasq_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_stride, int Hq,
+                             void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                             const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                             const void* v, int64_t v_token_stride, int64_t v_head_stride, int Hkv,
+                             int64_t T, int D, const float* table, int64_t table_positions, int rot,
+                             int interleaved, const int32_t* positions, const int32_t* slots,
+                             const void* q_norm, const void* k_norm, float eps,
+                             const fasq_kv_cache* cache, hipStream_t stream);
+
+/*
+ * Attention of the new tokens of B requests over a paged cache that already
+ * holds their keys and values.  Request b has the tokens q_start[b] <= t <
+ * q_start[b + 1] of q (n of them, in the order of their positions) and the
+ * first kv_len[b] slots of its pages: key j is slot j % page_size of page
+ * pages[b][j / page_size].  Token i of the request stands at position
+ * p = kv_len[b] - n + i and sees the keys
+ *
+ *   j <= p (causal) or j < kv_len[b];  with window > 0 also j > p - window
+ *
+ *   s_j = scale * q . k_j;   out = sum_j exp(s_j - lse) v_j,  lse = log sum_j exp(s_j)
+ *
+ * with query head h on cache head h / (Hq / Hkv).  A token that sees no key
+ * gets out = 0 and lse = -inf.  Keys and values that a token does not see do
+ * not reach its output, whatever they hold (NaN and infinities included), and
+ * what is stored past kv_len is never used.
+ *
+ *   q, out      fp16 [T x Hq x D] with token and head strides; tokens outside
+ *               every request are neither read nor written
+ *   cache       16-byte aligned, strides multiples of 8
+ *   D           a multiple of 8, 8 <= D <= 256
+ *   pages       int32 [B x max_pages], row stride page_row_stride; entries
+ *               past a request's last page are not used, others lie in
+ *               [0, num_pages) (an entry outside is read as the nearest page)
+ *   q_start     int32 [B + 1], not decreasing, within [0, T]
+ *   kv_len      int32 [B], at most max_pages * page_size (more is cut there)
+ *   lse         fp32 [T x Hq], contiguous, or NULL
+ *   workspace   device scratch of fasq_paged_attention_workspace_bytes()
+ *               bytes (16-byte aligned) for the fp32 partial results where
+ *               the keys of a tile are split over workgroups; joined in a
+ *               fixed order by a second kernel.  NULL or a smaller one: no
+ *               split (slower where there are few tokens and long caches)
+ *
+ * The keys are split by what q_start and kv_len hold when the kernels run, so
+ * the bits of a request's result may depend on the others in the batch; the
+ * same batch gives the same bits.
+ *
+ * Returns FASQ_ERR_INVALID_ARG, FASQ_ERR_UNSUPPORTED (D not a multiple of 8
+ * or above 256) or FASQ_ERR_HIP.
+ */
+fasq_status fasq_paged_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, int64_t T, int Hq,
+                                 const fasq_kv_cache* cache, int Hkv, int D,
+                                 const int32_t* pages, int64_t page_row_stride, int64_t max_pages,
+                                 const int32_t* q_start, const int32_t* kv_len, int64_t B,
+                                 float scale, int causal, int64_t window,
+                                 void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                                 void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes fasq_paged_attention splits keys with on the current device
+ * for T tokens of B requests (0 when it would not split), -1 for invalid
+ * sizes. */
+int64_t fasq_paged_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D);
+
+/*
+ * The residual stream between two blocks: the block's output y is normed (if
+ * post_weight), gated (if gate), scaled and added to the stream, and the norm
+ * that the next block reads is taken of the sum (if weight):
+ *
+ *   u     = y / sqrt(mean(y^2) + eps) * post_weight   or   y
+ *   x_new = x + scale * gate * u
+ *   h     = x_new / sqrt(mean(x_new^2) + eps) * weight
+ *
+ * over each of M rows of N values.  Arithmetic is fp32 throughout (h is taken
+ * of the unrounded x_new); x_out and h are rounded to fp16 once.
+ *
+ *   x, y         fp16 [M x N], contiguous; y NULL: x_new = x (post_weight and
+ *                gate must be NULL, x_out may be)
+ *   post_weight, weight  fp16 [N] or NULL
+ *   gate         fp16: [N] with gate_stride 0, or [M x N] with gate_stride N;
+ *                NULL: 1
+ *   x_out        fp16 [M x N] or NULL; may be x or y
+ *   h            fp16 [M x N]; NULL exactly when weight is; may be x or y,
+ *                not x_out
+ *
+ * Returns FASQ_ERR_INVALID_ARG (sizes; eps not positive and finite; nothing to
+ * write) or FASQ_ERR_HIP.
+ */
+fasq_status fasq_residual_norm(const void* x, const void* y, int64_t M, int64_t N, const void* post_weight,
+                               const void* gate, int64_t gate_stride, float scale, const void* weight, float eps,
+                               void* x_out, void* h, hipStream_t stream);
+
+/*
+ * Low-rank adapters of many requests beside `count` projections that read the
+ * same activations (q + k + v, gate + up, or one): for i < count and each of
+ * M tokens with adapter a = adapters[m],
+ *
+ *   y[i][m] = base[i][m] + scales[a] * B[i][a] . (A[i][a] . x[m])
+ *
+ * and y[i][m] = base[i][m] where a lies outside [0, L) (a request without an
+ * adapter).  base is what the shared projection gave (fasq_pq_gemv, _gemm and
+ * their kin).  The low-rank values A x are fp32 and enter the second product
+ * with 22 bits or more, sums are fp32, and y is rounded to fp16 once.
+ * Adapters of a smaller rank than r are padded with zero rows in A.
+ *
+ *   x         fp16 [M x K]
+ *   adapters  int32 [M], device memory: any order, any mix
+ *   L, r      adapters in the pool, their rank (1 <= r <= 256)
+ *   scales    fp32 [L]
+ *   N, A, B, base, y   HOST arrays of `count` entries: sizes, and device
+ *             buffers fp16 [L x r x K], [L x N[i] x r], [M x N[i]], [M x N[i]];
+ *             y[i] may be base[i]; base[i] NULL: zero
+ *   workspace device scratch of fasq_lora_workspace_bytes() bytes, 16-byte
+ *             aligned; contents are overwritten
+ *
+ * count is 1 to 8.  The K sum of a token does not depend on the other tokens'
+ * values.  Returns FASQ_ERR_INVALID_ARG (sizes, count, a NULL or misaligned
+ * pointer, a workspace that is too small), FASQ_ERR_UNSUPPORTED (r > 256) or
+ * FASQ_ERR_HIP.
+ */
+fasq_status fasq_lora_batched(const void* x, int64_t M, int64_t K, const int32_t* adapters, int64_t L, int r,
+                              const float* scales, int count, const int64_t* N, const void* const* A,
+                              const void* const* B, const void* const* base, void* const* y,
+                              void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes fasq_lora_batched needs for these sizes on the current
+ * device; -1 if they are invalid. */
+int64_t fasq_lora_workspace_bytes(int64_t M, int64_t K, int r, int count);
 
 /*
  * Bytes of one packed index row: ceil((K / d) * idx_bits / 8).  Each of the

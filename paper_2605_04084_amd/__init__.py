@@ -15,6 +15,7 @@ weights by k-means.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import threading
 from typing import Optional
@@ -55,13 +56,21 @@ __all__ = [
     "FASQ_ERR_HIP",
     "FASQ_ERR_HOST_MEMORY",
     "LaunchList",
+    "rope_frequencies",
+    "rope_table",
+    "rope_append",
+    "paged_attention",
+    "paged_attention_workspace_bytes",
+    "residual_norm",
+    "lora_batched",
+    "lora_workspace_bytes",
     "EXPORTED_SYMBOLS",
     "ABI_VERSION",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfasq.so")
 
-ABI_VERSION = 6  # FASQ_ABI_VERSION of include/fasq.h
+ABI_VERSION = 7  # FASQ_ABI_VERSION of include/fasq.h
 
 FASQ_OK = 0
 FASQ_ERR_INVALID_ARG = 1
@@ -94,6 +103,13 @@ EXPORTED_SYMBOLS = (
     "fasq_launch_list_run",
     "fasq_launch_list_size",
     "fasq_launch_list_destroy",
+    "fasq_rope_table",
+    "fasq_rope_append",
+    "fasq_paged_attention",
+    "fasq_paged_attention_workspace_bytes",
+    "fasq_residual_norm",
+    "fasq_lora_batched",
+    "fasq_lora_workspace_bytes",
 )
 
 
@@ -113,6 +129,13 @@ _lib: Optional[ctypes.CDLL] = None
 _c_i64 = ctypes.c_int64
 _c_int = ctypes.c_int
 _c_vp = ctypes.c_void_p
+
+
+class KvCache(ctypes.Structure):
+    """``fasq_kv_cache``: the pages of keys and values and their strides (in elements)."""
+
+    _fields_ = [("k", _c_vp), ("v", _c_vp), ("num_pages", _c_i64), ("page_size", _c_i64), ("page_stride", _c_i64),
+                ("slot_stride", _c_i64), ("head_stride", _c_i64)]
 
 
 def lib() -> ctypes.CDLL:
@@ -179,6 +202,24 @@ def lib() -> ctypes.CDLL:
         L.fasq_launch_list_size.restype = _c_i64
         L.fasq_launch_list_destroy.argtypes = [_c_vp]
         L.fasq_launch_list_destroy.restype = None
+        L.fasq_rope_table.argtypes = [ctypes.POINTER(ctypes.c_double), _c_int, _c_i64, ctypes.c_double, _c_vp, _c_vp]
+        L.fasq_rope_append.argtypes = [_c_vp, _c_i64, _c_i64, _c_int, _c_vp, _c_i64, _c_i64, _c_vp, _c_i64, _c_i64,
+                                       _c_vp, _c_i64, _c_i64, _c_int, _c_i64, _c_int, _c_vp, _c_i64, _c_int, _c_int,
+                                       _c_vp, _c_vp, _c_vp, _c_vp, ctypes.c_float, ctypes.POINTER(KvCache), _c_vp]
+        L.fasq_paged_attention.argtypes = [_c_vp, _c_i64, _c_i64, _c_i64, _c_int, ctypes.POINTER(KvCache), _c_int,
+                                           _c_int, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, ctypes.c_float, _c_int,
+                                           _c_i64, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, _c_vp]
+        L.fasq_paged_attention_workspace_bytes.argtypes = [_c_i64, _c_i64, _c_int, _c_int, _c_int]
+        L.fasq_residual_norm.argtypes = [_c_vp, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, ctypes.c_float, _c_vp,
+                                         ctypes.c_float, _c_vp, _c_vp, _c_vp]
+        L.fasq_lora_batched.argtypes = [_c_vp, _c_i64, _c_i64, _c_vp, _c_i64, _c_int, _c_vp, _c_int, _pi64, _pp, _pp,
+                                        _pp, _pp, _c_vp, _c_i64, _c_vp]
+        L.fasq_lora_workspace_bytes.argtypes = [_c_i64, _c_i64, _c_int, _c_int]
+        for name in ("fasq_rope_table", "fasq_rope_append", "fasq_paged_attention", "fasq_residual_norm",
+                     "fasq_lora_batched"):
+            getattr(L, name).restype = _c_int
+        for name in ("fasq_paged_attention_workspace_bytes", "fasq_lora_workspace_bytes"):
+            getattr(L, name).restype = _c_i64
         _lib = L
         return L
 
@@ -543,6 +584,337 @@ def pq_gemm_ex(x, idx, idx_bits: int, d: int, codebook, out=None, workspace=None
         return lib().fasq_pq_gemm_ex(xp, M_, K_, N_, ip, bits, dd, cp, C_, yp, ws_ptr, ws_bytes, stream)
 
     return _matmul(call, x, idx, idx_bits, d, codebook, out)
+
+
+# ---------------------------------------------------------------------------
+# Between the projections: rotary positions, attention, norms, adapters
+# ---------------------------------------------------------------------------
+
+def _require_rows(t, name, dtype, ndim):
+    """As ``_require``, but only the last dimension has to be contiguous."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != ndim:
+        raise ValueError(f"{name} must be {ndim}-D")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("all tensors must be on one device")
+
+
+def _ptr(t):
+    return 0 if t is None else t.data_ptr()
+
+
+def _kv_cache(k_cache, v_cache):
+    """The structure of two caches [pages x page_size x heads x D] (any strides but the last)."""
+    torch = _torch()
+    _require_rows(k_cache, "k_cache", torch.float16, 4)
+    _require_rows(v_cache, "v_cache", torch.float16, 4)
+    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+        raise ValueError("k_cache and v_cache must have the same shape and strides")
+    pages, page_size, _, _ = k_cache.shape
+    sp, ss, sh, _ = k_cache.stride()
+    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size, sp, ss, sh)
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                     original: int = 0, low: float = 1.0, high: float = 4.0):
+    """The rotary frequencies ``w_i`` (``rot / 2`` Python floats) and the scale of
+    the table, for :func:`rope_table`.
+
+    ``w_i = base ** (-2 i / rot)``, and for contexts ``factor`` times the
+    ``original`` one:
+
+    * ``"linear"``: ``w / factor`` (positions interpolated);
+    * ``"ntk"``: the base raised to ``base * factor ** (rot / (rot - 2))``, which
+      leaves the fastest pair alone and slows the slowest by ``factor``;
+    * ``"wavelength"``: pairs that turn more than ``high`` times over the original
+      context are left, those that turn less than ``low`` times are slowed by
+      ``factor``, between them both are mixed by the number of turns (the
+      scaling of Llama-3's long-context models: low 1, high 4);
+    * ``"yarn"`` (arXiv 2309.00071): the mix is linear in the pair's index between
+      the pairs that turn ``high`` (32 in the paper) and ``low`` times, and the
+      table's scale is ``0.1 ln(factor) + 1``.
+    """
+    if rot < 2 or rot % 2 or rot > 256:
+        raise ValueError("rot must be even and lie in [2, 256]")
+    if not base > 0 or not factor > 0:
+        raise ValueError("base and factor must be positive")
+    half, scale = rot // 2, 1.0
+    if scaling == "ntk":
+        if rot < 4:
+            raise ValueError("ntk needs rot >= 4")
+        base = base * factor ** (rot / (rot - 2))
+    w = [base ** (-2.0 * i / rot) for i in range(half)]
+    if scaling is None or scaling == "ntk":
+        return w, scale
+    if scaling == "linear":
+        return [v / factor for v in w], scale
+    if scaling not in ("wavelength", "yarn"):
+        raise ValueError("scaling must be None, 'linear', 'ntk', 'wavelength' or 'yarn'")
+    if original < 1 or not 0 < low < high:
+        raise ValueError(f"{scaling} needs original >= 1 and 0 < low < high")
+    turns = [original * v / (2 * math.pi) for v in w]
+    if scaling == "wavelength":
+        keep = [min(max((t - low) / (high - low), 0.0), 1.0) for t in turns]
+    else:
+        def pair_of(n):  # the (fractional) pair that turns n times over the original context
+            return rot * math.log(original / (2 * math.pi * n)) / (2 * math.log(base))
+
+        first = max(math.floor(pair_of(high)), 0)
+        last = min(math.ceil(pair_of(low)), rot - 1)
+        span = max(last - first, 1e-3)
+        keep = [1.0 - min(max((i - first) / span, 0.0), 1.0) for i in range(half)]
+        scale = 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+    return [v * k + v / factor * (1 - k) for v, k in zip(w, keep)], scale
+
+
+def rope_table(inv_freq, positions: int, scale: float = 1.0, device="cuda"):
+    """fp32 ``[positions x rot / 2 x 2]``: cosine and sine of every position and
+    pair, times ``scale``; made once and kept.  See ``fasq_rope_table``."""
+    torch = _torch()
+    half = len(inv_freq)
+    if positions < 1:
+        raise ValueError("positions must be >= 1")
+    table = torch.empty((positions, half, 2), dtype=torch.float32, device=device)
+    if not table.is_cuda:
+        raise ValueError("the table must be on a device")
+    w = (ctypes.c_double * max(half, 1))(*[float(v) for v in inv_freq])
+    _check(_on_device(table.get_device(), lib().fasq_rope_table, w, half, positions, float(scale), table.data_ptr()))
+    return table
+
+
+def rope_append(q, k, v, table, positions, slots, k_cache, v_cache, interleaved: bool = False, q_norm=None,
+                k_norm=None, eps: float = 1e-6, out=None):
+    """Rotary positions (and, with ``q_norm`` / ``k_norm``, the norm of each head
+    before them) of new tokens ``q`` [T x Hq x D], ``k`` and ``v`` [T x Hkv x D];
+    ``k`` and ``v`` go to the slots ``slots`` of the paged caches
+    [pages x page_size x Hkv x D], the turned queries are returned (``out`` may
+    be ``q``).  ``q`` may be None (returns None), or ``k`` and ``v`` (with
+    ``slots`` and the caches).  ``table`` None: no rotation.  See
+    ``fasq_rope_append``."""
+    torch = _torch()
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("q or k must be given")
+    if (k is None) != (v is None):
+        raise ValueError("k and v are given together or not at all")
+    _require_rows(some, "q" if q is not None else "k", torch.float16, 3)
+    T, _, D = some.shape
+    device = some.get_device()
+    Hq = Hkv = rot = rows = 0
+    qs = qos = ks = vs = (0, 0)
+    cache = None
+    if q is not None:
+        Hq = q.shape[1]
+        if out is None:
+            out = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device)
+        else:
+            _require_rows(out, "out", torch.float16, 3)
+            if out.shape != q.shape:
+                raise ValueError("out must have the shape of q")
+        qs, qos = q.stride(), out.stride()
+    elif out is not None:
+        raise ValueError("out needs q")
+    if k is not None:
+        _require_rows(k, "k", torch.float16, 3)
+        _require_rows(v, "v", torch.float16, 3)
+        Hkv = k.shape[1]
+        if k.shape != v.shape or k.shape[0] != T or k.shape[2] != D:
+            raise ValueError("k and v must be [T x Hkv x D]")
+        cache = _kv_cache(k_cache, v_cache)
+        if k_cache.shape[2] != Hkv or k_cache.shape[3] != D:
+            raise ValueError("the caches must be [pages x page_size x Hkv x D]")
+        _require(slots, "slots", torch.int32, 1)
+        if slots.shape[0] != T:
+            raise ValueError("slots must be [T]")
+        ks, vs = k.stride(), v.stride()
+        _same_device(device, k, v, k_cache, v_cache, slots)
+    if table is not None:
+        _require(table, "table", torch.float32, 3)
+        _require(positions, "positions", torch.int32, 1)
+        rows, half, two = table.shape
+        rot = 2 * half
+        if two != 2 or rot > D:
+            raise ValueError("table must be [positions x rot / 2 x 2] with rot <= D")
+        if positions.shape[0] != T:
+            raise ValueError("positions must be [T]")
+        _same_device(device, table, positions)
+    for w, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if w is not None:
+            _require(w, name, torch.float16, 1)
+            if w.shape[0] != D:
+                raise ValueError(f"{name} must be [D]")
+    _same_device(device, out, q_norm, k_norm)
+    _check(_on_device(device, lib().fasq_rope_append, _ptr(q), qs[0], qs[1], Hq, _ptr(out), qos[0], qos[1], _ptr(k),
+                      ks[0], ks[1], _ptr(v), vs[0], vs[1], Hkv, T, D, _ptr(table), rows, rot, int(interleaved),
+                      _ptr(positions) if table is not None else 0, _ptr(slots) if k is not None else 0, _ptr(q_norm),
+                      _ptr(k_norm), eps, cache))
+    return out
+
+
+def paged_attention_workspace_bytes(T: int, B: int, Hq: int, Hkv: int, D: int) -> int:
+    return lib().fasq_paged_attention_workspace_bytes(T, B, Hq, Hkv, D)
+
+
+def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional[float] = None, causal: bool = True,
+                    window: int = 0, out=None, return_lse: bool = False, workspace=None):
+    """Attention of the new tokens ``q`` [T x Hq x D] of B requests over the paged
+    caches [pages x page_size x Hkv x D]: request b has the tokens
+    ``q_start[b] : q_start[b + 1]`` and the first ``kv_len[b]`` slots of the
+    pages ``pages[b]`` (all int32).  Returns the output [T x Hq x D] (tokens of
+    no request are not written), and with ``return_lse`` also the fp32 logarithms
+    of the softmax sums [T x Hq].  ``scale`` is ``D ** -0.5`` unless given;
+    ``window`` 0 sees everything.  See ``fasq_paged_attention``."""
+    torch = _torch()
+    _require_rows(q, "q", torch.float16, 3)
+    T, Hq, D = q.shape
+    cache = _kv_cache(k_cache, v_cache)
+    Hkv = k_cache.shape[2]
+    if k_cache.shape[3] != D or Hkv < 1 or Hq % Hkv:
+        raise ValueError("the caches must be [pages x page_size x Hkv x D], Hq a multiple of Hkv")
+    _require_rows(pages, "pages", torch.int32, 2)
+    _require(q_start, "q_start", torch.int32, 1)
+    _require(kv_len, "kv_len", torch.int32, 1)
+    B = kv_len.shape[0]
+    if pages.shape[0] != B or q_start.shape[0] != B + 1:
+        raise ValueError("pages must be [B x max_pages], q_start [B + 1] and kv_len [B]")
+    device = q.get_device()
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device)
+    else:
+        _require_rows(out, "out", torch.float16, 3)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if return_lse else None
+    _same_device(device, k_cache, v_cache, pages, q_start, kv_len, out, workspace)
+    if workspace is None:
+        need = _on_device(device, lambda stream: paged_attention_workspace_bytes(T, B, Hq, Hkv, D))
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    qs, os_ = q.stride(), out.stride()
+    _check(_on_device(device, lib().fasq_paged_attention, q.data_ptr(), qs[0], qs[1], T, Hq, cache, Hkv, D,
+                      pages.data_ptr(), pages.stride(0), pages.shape[1], q_start.data_ptr(), kv_len.data_ptr(), B,
+                      D ** -0.5 if scale is None else scale, int(causal), window, out.data_ptr(), os_[0], os_[1],
+                      _ptr(lse), _ptr(workspace), ws_bytes))
+    return (out, lse) if return_lse else out
+
+
+def residual_norm(x, y=None, weight=None, eps: float = 1e-5, post_weight=None, gate=None, scale: float = 1.0,
+                  x_out=None, out=None):
+    """The residual stream between two blocks, over rows of ``x`` [M x N]:
+    ``x_new = x + scale * gate * u`` with ``u = y`` or, with ``post_weight``, its
+    norm, and ``h`` = the norm of ``x_new`` with ``weight``.  ``gate`` is [N] or
+    [M x N].  Returns ``(x_new, h)``; ``x_new`` is None without ``y`` (unless
+    ``x_out`` is given), ``h`` is None without ``weight``.  See
+    ``fasq_residual_norm``."""
+    torch = _torch()
+    _require(x, "x", torch.float16, 2)
+    M, N = x.shape
+    device = x.get_device()
+    stride = 0
+    if y is not None:
+        _require(y, "y", torch.float16, 2)
+        if y.shape != x.shape:
+            raise ValueError("y must have the shape of x")
+        if x_out is None:
+            x_out = torch.empty_like(x)
+    for w, name in ((weight, "weight"), (post_weight, "post_weight")):
+        if w is not None:
+            _require(w, name, torch.float16, 1)
+            if w.shape[0] != N:
+                raise ValueError(f"{name} must be [N]")
+    if gate is not None:
+        if not isinstance(gate, torch.Tensor) or gate.dim() not in (1, 2):
+            raise ValueError("gate must be [N] or [M x N]")
+        _require(gate, "gate", torch.float16, gate.dim())
+        if gate.shape[-1] != N or (gate.dim() == 2 and gate.shape[0] != M):
+            raise ValueError("gate must be [N] or [M x N]")
+        stride = N if gate.dim() == 2 else 0
+    if weight is not None and out is None:
+        out = torch.empty_like(x)
+    for t, name in ((x_out, "x_out"), (out, "out")):
+        if t is not None:
+            _require(t, name, torch.float16, 2)
+            if t.shape != x.shape:
+                raise ValueError(f"{name} must have the shape of x")
+    _same_device(device, y, weight, post_weight, gate, x_out, out)
+    _check(_on_device(device, lib().fasq_residual_norm, x.data_ptr(), _ptr(y), M, N, _ptr(post_weight), _ptr(gate),
+                      stride, scale, _ptr(weight), eps, _ptr(x_out), _ptr(out)))
+    return x_out, out
+
+
+def lora_workspace_bytes(M: int, K: int, r: int, count: int) -> int:
+    return lib().fasq_lora_workspace_bytes(M, K, r, count)
+
+
+def lora_batched(x, adapters, As, Bs, scales, bases, outs=None, workspace=None):
+    """Low-rank adapters beside projections that read the same ``x`` [M x K]:
+    ``y_i = base_i + scales[a] * B_i[a] (A_i[a] x)`` with ``a = adapters[m]`` for
+    each token m (int32; outside the pool: no adapter).  ``As[i]`` is
+    [L x r x K], ``Bs[i]`` [L x N_i x r], ``bases[i]`` [M x N_i] or None,
+    ``scales`` fp32 [L].  ``outs[i]`` may be ``bases[i]``.  Returns the list of
+    outputs; see ``fasq_lora_batched``."""
+    torch = _torch()
+    _require(x, "x", torch.float16, 2)
+    _require(adapters, "adapters", torch.int32, 1)
+    _require(scales, "scales", torch.float32, 1)
+    M, K = x.shape
+    L, n = scales.shape[0], len(As)
+    if not (len(Bs) == len(bases) == n and (outs is None or len(outs) == n)) or n < 1:
+        raise ValueError("As, Bs, bases and outs must have equal lengths, at least 1")
+    if adapters.shape[0] != M:
+        raise ValueError("adapters must be [M]")
+    device = x.get_device()
+    _same_device(device, adapters, scales, workspace)
+    r, ys = 0, []
+    for i, (A, B, base) in enumerate(zip(As, Bs, bases)):
+        _require(A, f"A[{i}]", torch.float16, 3)
+        _require(B, f"B[{i}]", torch.float16, 3)
+        N = B.shape[1]
+        if i == 0:
+            r = A.shape[1]
+        if tuple(A.shape) != (L, r, K) or tuple(B.shape) != (L, N, r):
+            raise ValueError(f"A[{i}] must be [L x r x K] and B[{i}] [L x N x r], with the L of scales and one r")
+        if base is not None:
+            _require(base, f"base[{i}]", torch.float16, 2)
+            if tuple(base.shape) != (M, N):
+                raise ValueError(f"base[{i}] must be [M x N]")
+        if outs is None:
+            y = x.new_empty((M, N))
+        else:
+            y = outs[i]
+            _require(y, f"out[{i}]", torch.float16, 2)
+            if tuple(y.shape) != (M, N):
+                raise ValueError(f"out[{i}] must be [M x N]")
+        _same_device(device, A, B, base, y)
+        ys.append(y)
+    if workspace is None:
+        need = _on_device(device, lambda stream: lora_workspace_bytes(M, K, r, n))
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    elif not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    arr_p, arr_i = _c_vp * n, _c_i64 * n
+    _check(_on_device(device, lib().fasq_lora_batched, x.data_ptr(), M, K, adapters.data_ptr(), L, r,
+                      scales.data_ptr(), n, arr_i(*[B.shape[1] for B in Bs]), arr_p(*[A.data_ptr() for A in As]),
+                      arr_p(*[B.data_ptr() for B in Bs]), arr_p(*[_ptr(b) for b in bases]),
+                      arr_p(*[y.data_ptr() for y in ys]), _ptr(workspace), ws_bytes))
+    return ys
 
 
 # ---------------------------------------------------------------------------
