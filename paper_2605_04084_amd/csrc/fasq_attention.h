@@ -1,0 +1,509 @@
+// Attention over a paged cache: the work of one wave, and where a workgroup's
+// work lies in the batch.
+//
+// A wave holds 32 query rows.  A row is a (token, query head) pair of one
+// cache head: with G = Hq / Hkv query heads per cache head, row r of a request
+// is its token r / G and head r % G, so the heads of a group share the keys
+// and values that a tile brings on chip, from one token (G rows) to a chunk.
+//
+// Scores are computed transposed, S^T = K Q^T (v_mfma_f32_32x32x16_f16, keys
+// down, queries across): lane l then holds 16 of every 32 keys of query l % 32,
+// and its softmax statistics are its own but for one exchange with lane l ^ 32.
+// The weights leave the score registers already in the layout of the second
+// product's operand, O^T = V^T P^T, if V's rows are taken in the order the
+// score registers have them, which is free: V^T comes from LDS through the
+// transposing read (ds_read_b64_tr_b16), four rows at a time from anywhere.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fasq_device.h"
+#include "fasq_layer.h"
+
+namespace fasq {
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+struct AttentionArgs {
+  HeadsView q, out;
+  int64_t T, B;
+  int Hq, Hkv, G, D;
+  const uint16_t* ck;
+  const uint16_t* cv;
+  int num_pages;
+  uint32_t page_size;
+  int page_shift;  // log2(page_size), -1 where it is no power of two
+  int64_t page_stride, slot_stride, head_stride;
+  const int32_t* pages;
+  int64_t page_row_stride;
+  int capacity;  // max_pages * page_size
+  const int32_t* q_start;
+  const int32_t* kv_len;
+  float c;  // |scale| * log2(e)
+  bool negate;  // scale < 0: the queries change sign instead
+  bool causal;
+  bool q_vec, out_vec;  // 16-byte loads of q, 8-byte stores of out
+  int window;  // 0: none
+  float* lse;
+  // Split over workgroups (part_o != nullptr): workgroup w of `parts` takes
+  // the w-th equal share of the batch's keys; see Place.
+  int parts;
+  float* part_o;  // [2 * parts][rows][DP], not divided by the sum
+  float* part_ml;  // [2 * parts][rows][2]: maximum (in powers of two), sum
+};
+
+// ---------------------------------------------------------------------------
+// Where work lies
+// ---------------------------------------------------------------------------
+
+// A request as the kernels read it: lengths cut to what exists.
+struct Request {
+  int q0, n, kv;
+};
+
+__device__ __forceinline__ Request read_request(const AttentionArgs& a, int64_t b) {
+  const int T = (int)a.T;
+  int q0 = a.q_start[b], q1 = a.q_start[b + 1], kv = a.kv_len[b];
+  q0 = q0 < 0 ? 0 : q0 > T ? T : q0;
+  q1 = q1 < q0 ? q0 : q1 > T ? T : q1;
+  kv = kv < 0 ? 0 : kv > a.capacity ? a.capacity : kv;
+  return {q0, q1 - q0, kv};
+}
+
+// Keys [begin, end) that token i of a request sees.
+struct Span {
+  int begin, end;
+};
+
+__device__ __forceinline__ Span token_span(const AttentionArgs& a, const Request& r, int i) {
+  const int pos = r.kv - r.n + i;  // may be negative: more new tokens than keys
+  int end = a.causal && pos + 1 < r.kv ? pos + 1 : r.kv;
+  int begin = a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
+  end = end < 0 ? 0 : end;
+  return {begin < end ? begin : end, end};
+}
+
+// Keys that some token of tile t (ROWS rows) sees.
+template <int ROWS>
+__device__ __forceinline__ Span tile_span(const AttentionArgs& a, const Request& r, int t) {
+  const int rows = r.n * a.G;
+  const int last = (t + 1) * ROWS < rows ? (t + 1) * ROWS : rows;
+  const Span s0 = token_span(a, r, t * ROWS / a.G), s1 = token_span(a, r, (last - 1) / a.G);
+  return {s0.begin < s1.begin ? s0.begin : s1.begin, s1.end > s0.end ? s1.end : s0.end};
+}
+
+// The batch as a line of positions.  With `parts` shares, every cache head
+// has the same stretch, in it the requests in order, in them their tiles, and
+// a tile is as long as the keys its request can need (a multiple of STEP, at
+// least one).  Share w holds the positions [w * share, (w + 1) * share): each
+// workgroup has the same number of keys to read, whatever the lengths, and a
+// tile is cut only where two shares meet.  Without shares a tile is one
+// position long.
+struct Place {
+  int b, tile, head;
+  Request r;
+  int64_t start, end;  // the tile's positions
+};
+
+template <int ROWS, int STEP>
+__device__ __forceinline__ int64_t tile_length(const AttentionArgs& a, const Request& r, bool shared) {
+  if (!shared) return 1;
+  int keys = r.kv;
+  if (a.window > 0) {
+    const int most = a.window + ROWS / a.G + 32;  // of the tile's tokens, from a multiple of 32 on
+    keys = keys < most ? keys : most;
+  }
+  return keys <= STEP ? STEP : ((int64_t)keys + STEP - 1) / STEP * STEP;
+}
+
+// A value that every lane of the wave holds, as a scalar.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const uint32_t lo = (uint32_t)uniform((int)(uint32_t)v), hi = (uint32_t)uniform((int)(uint32_t)(v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// Lane l's value (l uniform), as a scalar.
+__device__ __forceinline__ int lane_value(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ __forceinline__ int64_t lane_value(int64_t v, int l) {
+  const uint32_t lo = (uint32_t)lane_value((int)(uint32_t)v, l), hi = (uint32_t)lane_value((int)(uint32_t)(v >> 32), l);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+__device__ __forceinline__ int64_t wave_total(int64_t v) {
+#pragma unroll
+  for (int x = 1; x < kWave; x *= 2) v += __shfl_xor(v, x, kWave);
+  return v;
+}
+
+template <int ROWS>
+__device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r) {
+  return (r.n * a.G + ROWS - 1) / ROWS;
+}
+
+// Positions of one cache head.
+template <int ROWS, int STEP>
+__device__ __forceinline__ int64_t head_length(const AttentionArgs& a, bool shared) {
+  int64_t sum = 0;
+  for (int64_t b = threadIdx.x % kWave; b < a.B; b += kWave) {
+    const Request r = read_request(a, b);
+    sum += tiles_of<ROWS>(a, r) * tile_length<ROWS, STEP>(a, r, shared);
+  }
+  return a.B == 1 ? lane_value(sum, 0) : uniform(wave_total(sum));
+}
+
+// The tile at a position within a head's stretch, in every lane of the wave.
+// pos < head_length.
+template <int ROWS, int STEP>
+__device__ __forceinline__ Place locate(const AttentionArgs& a, int64_t pos, bool shared) {
+  Place p = {};
+  int64_t base = 0;
+  for (int64_t b0 = 0; b0 < a.B; b0 += kWave) {
+    const int64_t b = b0 + threadIdx.x % kWave;
+    Request r = {};
+    int64_t one = 0, own = 0;
+    if (b < a.B) {
+      r = read_request(a, b);
+      one = tile_length<ROWS, STEP>(a, r, shared);
+      own = tiles_of<ROWS>(a, r) * one;
+    }
+    int64_t upto = own;  // positions up to and with this lane's request
+    if (a.B > 1) {
+#pragma unroll
+      for (int x = 1; x < kWave; x *= 2) {
+        const int64_t below = __shfl_up(upto, x, kWave);
+        if ((int)(threadIdx.x % kWave) >= x) upto += below;
+      }
+    }
+    const uint64_t hit = __ballot(base + upto > pos && b < a.B);
+    if (hit != 0) {
+      const int l = __ffsll((unsigned long long)hit) - 1;
+      p.b = (int)(b0 + l);
+      p.r.q0 = lane_value(r.q0, l);
+      p.r.n = lane_value(r.n, l);
+      p.r.kv = lane_value(r.kv, l);
+      one = lane_value(one, l);
+      const int64_t first = base + lane_value(upto - own, l);
+      p.tile = (int)((pos - first) / one);
+      p.start = first + p.tile * one;
+      p.end = p.start + one;
+      return p;
+    }
+    base += lane_value(upto, kWave - 1);
+  }
+  p.b = -1;
+  return p;
+}
+
+// Element offset of key j's row in a cache head (page table row `pages`).
+__device__ __forceinline__ int64_t key_offset(const AttentionArgs& a, int page, int j) {
+  const uint32_t in_page = a.page_shift >= 0 ? (uint32_t)j & (a.page_size - 1) : (uint32_t)j % a.page_size;
+  page = page < 0 ? 0 : page >= a.num_pages ? a.num_pages - 1 : page;
+  return page * a.page_stride + in_page * a.slot_stride;
+}
+
+__device__ __forceinline__ int page_of(const AttentionArgs& a, const int32_t* pages, int j) {
+  return pages[a.page_shift >= 0 ? (uint32_t)j >> a.page_shift : (uint32_t)j / a.page_size];
+}
+
+// ---------------------------------------------------------------------------
+// Keys and values in LDS: rows of DP values, 16-byte chunks permuted within a
+// row so that both readers meet all banks: 16 lanes reading one chunk column
+// of 16 rows (scores), and 32 lanes reading four chunks of four neighbouring
+// rows (the transposing read).
+// ---------------------------------------------------------------------------
+template <int DP>
+__device__ __forceinline__ int chunk_swap(int row) {
+  if constexpr (DP == 64) return ((row & 2) << 1) | ((row >> 2) & 3);
+  else return ((row & 3) << 2) | ((row >> 2) & 3);
+}
+
+// Wait until at most N of this wave's vector-memory operations are in flight
+// (gfx9 encoding), and a barrier that neither waits for them nor lets the
+// compiler move memory accesses across.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+  asm volatile("" ::: "memory");
+}
+// Wait for this wave's reads of LDS: before copies that overwrite what they read.
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (0x7 << 4) | (0 << 8));
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void barrier_only() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// LDS by its address: rows are powers of two long, so the permuted chunk of a
+// column is one exclusive or away from the lane's first address, and rows
+// and blocks are immediate offsets.
+typedef __attribute__((address_space(3))) const half8_t* lds_half8;
+typedef __attribute__((address_space(3))) short4_t* lds_short4;
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+__device__ __forceinline__ void copy16_to_lds(const uint16_t* src, void* lds) {
+  __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+// ---------------------------------------------------------------------------
+// One wave: 32 rows against KB blocks of 32 keys at a time
+// ---------------------------------------------------------------------------
+template <int DP, int KB>
+struct WaveTile {
+  half8_t q[DP / 16];
+  float16_t o[DP / 32];
+  float m, mc, l;  // running maximum of the scores (this row), m * c, sum of this lane's weights
+  half8_t bad;     // NaN where a value of a masked tile was not finite
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    m = mc = -INFINITY;
+    l = 0.f;
+    bad = half8_t{};
+  }
+
+  // Row `row` of the request (lane l and l ^ 32 hold one row; rows past the
+  // end, and values past D, are zero).
+  __device__ __forceinline__ void load_q(const AttentionArgs& a, const Request& r, int head, int row, bool live) {
+    const int h = (threadIdx.x % kWave) / 32;
+    const uint16_t* src = nullptr;
+    if (live) src = a.q.p + (r.q0 + row / a.G) * a.q.ts + (head * a.G + row % a.G) * a.q.hs;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      const int d = s * 16 + h * 8;
+      half8_t v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = static_cast<half_t>(0.f);
+      if (live && d < a.D) {
+        if (a.q_vec) {
+          v = *reinterpret_cast<const half8_t*>(src + d);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(half_t, src[d + e]);
+        }
+        if (a.negate) v = -v;
+      }
+      q[s] = v;
+    }
+  }
+
+  // keys, values: the tile's rows in LDS (KB * 32 of them); key0: its first
+  // key.  A row sees keys [begin, end).  MASKED: not every live row sees all
+  // of them; the values are then cut to finite ones, since a weight of zero
+  // leaves those out but not NaN and infinities, and `bad` remembers the cut.
+  template <bool MASKED>
+  __device__ __forceinline__ void step(const uint16_t* keys, const uint16_t* values, int key0, int begin, int end,
+                                       float c) {
+    const int lane = threadIdx.x % kWave, l32 = lane % 32, h = lane / 32;
+    float16_t s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+    const uint32_t k_at = lds_address(keys) + l32 * (DP * 2) + (h ^ chunk_swap<DP>(l32)) * 16;
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) {
+      if constexpr (MASKED) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const half8_t k = *(lds_half8)(uintptr_t)((k_at ^ (t % 8 * 32)) + t / 8 * 256 + kb * 32 * DP * 2);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[t], s[kb], 0, 0, 0);
+      }
+    }
+    if constexpr (MASKED) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = key0 + kb * 32 + (e / 4) * 8 + h * 4 + e % 4;
+          if (key < begin || key >= end) s[kb][e] = -INFINITY;
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+    {
+      const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+    }
+    // The maximum need not be the newest one: weights up to 2^8 are as exact
+    // in fp16 as weights up to 1, so a row is rescaled only where its maximum
+    // has grown by more than that (each row by its own scores alone).
+    const bool grown = (top - m) * c > 8.f || (m == -INFINITY && top > -INFINITY);
+    if (__any(grown)) {
+      // the weights are 2^(s c - mc) with the rounded product mc, here too
+      const float next_c = top * c;
+      const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= keep;
+      m = grown ? top : m;
+      mc = grown ? next_c : mc;
+    }
+    half8_t p[2 * KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float w = __builtin_amdgcn_exp2f(s[kb][e] * c - mc);
+        if (MASKED && s[kb][e] == -INFINITY) w = 0.f;
+        l += w;
+        p[2 * kb + e / 8][e % 8] = static_cast<half_t>(w);
+      }
+    // rows of V in the order of the score registers: weight j of slab u is
+    // key 16 u + (j / 4) * 8 + h * 4 + j % 4
+    const int r = (lane % 16) / 4, x = (lane / 16 & 1) * 2 + (lane & 3) / 2;
+    uint32_t v_at[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = j * 8 + h * 4 + r;
+      v_at[j] = lds_address(values) + row * (DP * 2) + (x ^ chunk_swap<DP>(row)) * 16 + (lane & 1) * 8;
+    }
+#pragma unroll
+    for (int u = 0; u < 2 * KB; ++u)
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) {
+        if constexpr (MASKED) __builtin_amdgcn_sched_barrier(0);  // few registers, seldom run
+        short4_t part[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_short4)(uintptr_t)((v_at[j] ^ (i % 4 * 64)) + i / 4 * 256 + u * 16 * DP * 2));
+        }
+        half8_t v = __builtin_bit_cast(half8_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        if constexpr (MASKED) {
+          const half_t most = static_cast<half_t>(65504.f);
+          bad += v * half8_t{};
+          v = __builtin_elementwise_min(__builtin_elementwise_max(v, half8_t(-most)), half8_t(most));
+        }
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[u], o[i], 0, 0, 0);
+      }
+  }
+
+  // Sum of the row's weights, in both its lanes.
+  __device__ __forceinline__ float total() const {
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  }
+
+  // Whether a masked tile held values that are not finite (uniform).
+  __device__ __forceinline__ bool suspect() const {
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) nan = nan || !(bad[e] == static_cast<half_t>(0.f));
+    return __any(nan);
+  }
+
+  // Whether this lane's part of the row holds a value that is not finite.
+  __device__ __forceinline__ bool broken() const {
+    float z = (l - l) + (mc == -INFINITY ? 0.f : mc - mc);
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z += o[i][e] - o[i][e];
+    return !(z == 0.f);
+  }
+};
+
+// fp16 bits to fp32.
+__device__ __forceinline__ float half_value(uint16_t b) { return (float)__builtin_bit_cast(half_t, b); }
+
+// What a finished row holds: its sum of weighted values still has to be
+// divided by l.  A row that sees keys but whose scores are all -inf is 0 / 0.
+__device__ __forceinline__ float row_factor(float l, bool sees) {
+  return l == 0.f ? (sees ? __builtin_nanf("") : 0.f) : 1.f / l;
+}
+__device__ __forceinline__ float row_lse(float mc, float l, bool sees) {
+  if (l == 0.f) return sees ? __builtin_nanf("") : -INFINITY;
+  return (mc + __log2f(l)) * 0.69314718055994530942f;
+}
+
+// One row over the keys [begin, end), key by key, by a whole wave: for rows
+// whose result is not finite, or whose masked tiles held values that are not.
+// Only keys that the row sees are touched.  Lane l holds dimensions l, l + 64, ...
+template <int DP>
+struct SlowRow {
+  float m = -INFINITY, l = 0.f, o[(DP + kWave - 1) / kWave] = {};
+
+  __device__ __forceinline__ void run(const AttentionArgs& a, const uint16_t* q, int64_t head_off,
+                                      const int32_t* pages, int begin, int end) {
+    const int lane = threadIdx.x % kWave;
+    for (int j0 = begin; j0 < end; j0 += kWave) {
+      const int j = j0 + lane;
+      float s = -INFINITY;
+      int64_t off = 0;
+      if (j < end) {
+        off = key_offset(a, page_of(a, pages, j), j) + head_off;
+        s = 0.f;
+        for (int i = 0; i < a.D; ++i) s += half_value(q[i]) * half_value(a.ck[off + i]);
+        s *= a.negate ? -a.c : a.c;
+      }
+      float top = s;
+#pragma unroll
+      for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kWave));
+      const float next = fmaxf(m, top);
+      const float p = j < end ? exp2f(s - (next == -INFINITY ? 0.f : next)) : 0.f;
+      const float keep = l == 0.f ? 0.f : exp2f(m - next);
+      l = l * keep + wave_sum(p);
+      m = next;
+#pragma unroll
+      for (float& v : o) v = keep == 0.f ? 0.f : v * keep;
+      const int count = end - j0 < kWave ? end - j0 : kWave;
+      for (int e = 0; e < count; ++e) {
+        const float w = __shfl(p, e, kWave);
+        const int64_t vo = __shfl(off, e, kWave);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(o) / sizeof(float)); ++i)
+          if (lane + i * kWave < a.D) o[i] += w * half_value(a.cv[vo + lane + i * kWave]);
+      }
+    }
+  }
+
+  // Writes the row, to the output (slot < 0) or as row `at` of a slot, if it
+  // holds a value that is not finite or the one there does (`broken`): the
+  // tiles' result stands for rows that see finite values alone.
+  template <int ROWS>
+  __device__ __forceinline__ void store(const AttentionArgs& a, const Request& r, int head, int row, int at,
+                                        int64_t slot, bool sees, bool broken) const {
+    const int lane = threadIdx.x % kWave;
+    constexpr int N = (DP + kWave - 1) / kWave;
+    float z = l - l;
+#pragma unroll
+    for (int i = 0; i < N; ++i) z += o[i] - o[i];
+    if (!broken && !__any(!(z == 0.f))) return;
+    if (slot >= 0) {
+      const int64_t to = slot * ROWS + at;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (lane + i * kWave < DP) a.part_o[to * DP + lane + i * kWave] = o[i];
+      if (lane == 0) {
+        a.part_ml[to * 2] = m;
+        a.part_ml[to * 2 + 1] = l;
+      }
+      return;
+    }
+    const float f = row_factor(l, sees);
+    uint16_t* dst = a.out.p + (r.q0 + row / a.G) * a.out.ts + (head * a.G + row % a.G) * a.out.hs;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (lane + i * kWave < a.D) dst[lane + i * kWave] = f32_to_f16_bits(o[i] * f);
+    if (lane == 0 && a.lse != nullptr)
+      a.lse[(int64_t)(r.q0 + row / a.G) * a.Hq + head * a.G + row % a.G] = row_lse(m, l, sees);
+  }
+};
+
+}  // namespace fasq

@@ -1,113 +1,515 @@
-// Attention of new tokens over a paged cache.
+// Attention of new tokens over a paged cache: kernels and launch.
 //
-// One wave per token and query head, 64 keys at a time with the running
-// maximum and sum of a softmax: lanes hold keys for the scores and dimensions
-// for the weighted sum of values.
+//   k_attention_few   up to 32 rows of a cache head (decode, a few tokens): the
+//                     waves of a workgroup share the rows and split the keys
+//   k_attention_tile  128 rows: the waves share the keys and split the rows
+//   k_attention_join  joins what shares of a tile's keys gave
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 
-#include "fasq_device.h"
-#include "fasq_layer.h"
+#include "fasq_attention.h"
 
 namespace fasq {
 
 namespace {
 
-struct AttentionArgs {
-  HeadsView q, out;
-  int64_t T, B;
-  int Hq, Hkv, D;
-  const uint16_t* ck;
-  const uint16_t* cv;
-  int64_t num_pages;
-  uint32_t page_size;
-  int64_t page_stride, slot_stride, head_stride;
-  const int32_t* pages;
-  int64_t page_row_stride;
-  int64_t capacity;  // max_pages * page_size
-  const int32_t* q_start;
-  const int32_t* kv_len;
-  float scale;
-  bool causal;
-  int64_t window;
-  float* lse;
-};
-
-__device__ __forceinline__ float h2f(uint16_t b) { return (float)__builtin_bit_cast(half_t, b); }
-
-__global__ __launch_bounds__(256) void k_attention_rows(AttentionArgs a) {
-  const int64_t row = blockIdx.x * (int64_t)4 + threadIdx.x / kWave;
-  if (row >= a.T * a.Hq) return;
-  const int lane = threadIdx.x % kWave;
-  const int64_t t = row / a.Hq;
-  const int h = (int)(row % a.Hq);
-  // the request of token t: the last one that starts at or before it
-  int64_t lo = 0, hi = a.B;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (a.q_start[mid + 1] <= t) lo = mid + 1;
-    else hi = mid;
+// Stores four consecutive values of an output row.
+__device__ __forceinline__ void store4(const AttentionArgs& a, uint16_t* dst, int d, const float (&v)[4]) {
+  if (d >= a.D) return;  // D is a multiple of 8
+  if (a.out_vec) {
+    half4_t h;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = static_cast<half_t>(v[i]);
+    *reinterpret_cast<half4_t*>(dst + d) = h;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[d + i] = f32_to_f16_bits(v[i]);
   }
-  if (lo >= a.B || t < a.q_start[lo]) return;
-  const int64_t n = a.q_start[lo + 1] - a.q_start[lo];
-  int64_t kv = a.kv_len[lo];
-  kv = kv < 0 ? 0 : kv > a.capacity ? a.capacity : kv;
-  const int64_t pos = kv - n + (t - a.q_start[lo]);
-  const int64_t end = a.causal ? (pos + 1 < kv ? pos + 1 : kv) : kv;
-  int64_t begin = a.window > 0 ? pos - a.window + 1 : 0;
-  if (begin < 0) begin = 0;
-  const int32_t* pages = a.pages + lo * a.page_row_stride;
-  const int64_t head = (h / (a.Hq / a.Hkv)) * a.head_stride;
-  const uint16_t* q = a.q.p + t * a.q.ts + h * a.q.hs;
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t j0 = begin; j0 < end; j0 += kWave) {
-    const int64_t j = j0 + lane;
-    float s = -INFINITY;
-    int64_t off = 0;
-    if (j < end) {
-      int64_t page = pages[j / a.page_size];
-      page = page < 0 ? 0 : page >= a.num_pages ? a.num_pages - 1 : page;
-      off = page * a.page_stride + (j % a.page_size) * a.slot_stride + head;
-      s = 0.f;
-      for (int i = 0; i < a.D; ++i) s += h2f(q[i]) * h2f(a.ck[off + i]);
-      s *= a.scale;
+}
+
+__device__ __forceinline__ uint16_t* out_row(const AttentionArgs& a, const Request& r, int head, int row) {
+  return a.out.p + (r.q0 + row / a.G) * a.out.ts + (head * a.G + row % a.G) * a.out.hs;
+}
+
+__device__ __forceinline__ int64_t lse_at(const AttentionArgs& a, const Request& r, int head, int row) {
+  return (int64_t)(r.q0 + row / a.G) * a.Hq + head * a.G + row % a.G;
+}
+
+// Copies rows (keys k0 + row, cut to [first, last]) of a cache head to LDS,
+// one wave's share of INSTR wave-wide copies of 64 16-byte chunks, from row
+// `row0` on.  `page`: the page of key k0 + row0 + lane (lanes below the rows
+// copied).
+template <int DP, int INSTR>
+__device__ __forceinline__ void copy_rows(const AttentionArgs& a, int64_t head_off, int page, int k0, int first, int last,
+                                          int row0, uint16_t* keys, uint16_t* values) {
+  constexpr int CH = DP / 8, RPI = kWave / CH;  // chunks of a row, rows of a copy
+  const int lane = threadIdx.x % kWave;
+  const int j = k0 + row0 + lane;
+  const int64_t own = key_offset(a, page, j < first ? first : j < last ? j : last) + head_off;
+#pragma unroll
+  for (int i = 0; i < INSTR; ++i) {
+    const int row = row0 + i * RPI + lane / CH;
+    const int chunk = (lane % CH) ^ chunk_swap<DP>(row);
+    const int64_t off = __shfl(own, i * RPI + lane / CH, kWave) + chunk * 8;
+    if (chunk * 8 < a.D) {
+      copy16_to_lds(a.ck + off, keys + (row0 + i * RPI) * DP);
+      copy16_to_lds(a.cv + off, values + (row0 + i * RPI) * DP);
     }
-    float top = s;
+  }
+}
+
+// Chunks past D are zero and stay so.
+template <int DP>
+__device__ __forceinline__ void clear_lds(const AttentionArgs& a, uint16_t* at, int rows) {
+  if (a.D == DP) return;
+  const u32x4 zero = {0, 0, 0, 0};
+  for (int i = threadIdx.x % kWave; i < rows * DP / 8; i += kWave) reinterpret_cast<u32x4*>(at)[i] = zero;
+  wait_lds();  // before copies that land beside them
+}
+
+// The rows a share of a tile's keys gives: a slot of the partial results.
+// Share w has at most two cut tiles: one that it starts with (slot 2 w) and
+// one that starts within it (slot 2 w + 1).
+__device__ __forceinline__ int64_t slot_of(int64_t w, int64_t share, int64_t tile_start) {
+  return 2 * w + (tile_start > w * share ? 1 : 0);
+}
+
+template <int STEP>
+__device__ __forceinline__ int64_t share_of(int64_t total, int parts, int least) {
+  const int64_t s = (total + parts - 1) / parts;
+  return s <= least ? least : (s + STEP - 1) / STEP * STEP;
+}
+
+constexpr int kFewShare = 128;   // keys a share has at least
+constexpr int kTileShare = 256;
+
+// ---------------------------------------------------------------------------
+// Up to 32 rows: NW waves, each 32 keys at a time with its own two stages of
+// LDS, so that no wave waits for another until the end, where their results
+// are joined in wave order.
+// ---------------------------------------------------------------------------
+template <int DP, int NW>
+__global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a) {
+  constexpr int ROWS = 32, STEP = NW * 32, INSTR = DP / 16, OS = DP + 4;
+  extern __shared__ uint8_t smem[];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int l32 = lane % 32, h = lane / 32;
+  uint16_t* ring = reinterpret_cast<uint16_t*>(smem) + wave * (2 * 2 * 32 * DP);
+  float* jo = reinterpret_cast<float*>(smem);           // [NW][32][OS]
+  float* jm = jo + NW * 32 * OS;                        // [NW][32]
+  float* jl = jm + NW * 32;                             // [NW][32]
+  int* flag = reinterpret_cast<int*>(jl + NW * 32);     // [32], then [NW] of the waves
+
+  const bool shared = a.part_o != nullptr;
+  const int64_t head_len = head_length<ROWS, STEP>(a, shared);
+  int64_t pos, pos_end, share = 0, w = blockIdx.x;
+  if (shared) {
+    share = share_of<STEP>(head_len * a.Hkv, a.parts, kFewShare);
+    pos = w * share;
+    pos_end = pos + share < head_len * a.Hkv ? pos + share : head_len * a.Hkv;
+  } else {
+    pos = (w % a.Hkv) * head_len + w / a.Hkv;
+    pos_end = w / a.Hkv < head_len ? pos + 1 : pos;
+  }
+  while (pos < pos_end) {
+    const int head = (int)(pos / head_len);
+    const Place p = locate<ROWS, STEP>(a, pos - head * head_len, shared);
+    if (p.b < 0) return;
+    const int64_t t0 = head * head_len + p.start, t1 = head * head_len + p.end;
+    const int64_t seg_end = t1 < pos_end ? t1 : pos_end;
+    const Span span = tile_span<ROWS>(a, p.r, p.tile);
+    const int base = span.begin / 32 * 32;
+    int lo = base, hi = span.end;
+    if (shared) {
+      lo = base + (int)(pos - t0);
+      const int64_t most = base + (seg_end - t0);
+      hi = most < hi ? (int)most : hi;
+    }
+    const int rows = p.r.n * a.G, row0 = p.tile * ROWS, live = rows - row0 < ROWS ? rows - row0 : ROWS;
+    const bool alive = l32 < live;
+    Span mine = token_span(a, p.r, (row0 + (alive ? l32 : live - 1)) / a.G);
+    // keys that every live row sees
+    const Span s0 = token_span(a, p.r, row0 / a.G), s1 = token_span(a, p.r, (row0 + live - 1) / a.G);
+    const int all_begin = s0.begin > s1.begin ? s0.begin : s1.begin;
+    int all_end = s0.end < s1.end ? s0.end : s1.end;
+    if (mine.end > hi) mine.end = hi;
+    if (all_end > hi) all_end = hi;
+    const int32_t* pages = a.pages + p.b * a.page_row_stride;
+    const int64_t head_off = head * a.head_stride;
+
+    clear_lds<DP>(a, ring, 2 * 2 * 32);
+    WaveTile<DP, 1> t;
+    t.clear();
+    t.load_q(a, p.r, head, row0 + l32, alive);
+    int k0 = lo + wave * 32;
+    auto page_at = [&](int k) {
+      const int j = k + l32;
+      return k < hi ? page_of(a, pages, j < span.begin ? span.begin : j < hi ? j : hi - 1) : 0;
+    };
+    auto issue = [&](int k, int page, int stage) {
+      copy_rows<DP, INSTR>(a, head_off, page, k, span.begin, hi - 1, 0, ring + stage * (2 * 32 * DP),
+                           ring + stage * (2 * 32 * DP) + 32 * DP);
+    };
+    int page = page_at(k0), stage = 0;
+    if (k0 < hi) issue(k0, page, 0);
+    page = page_at(k0 + STEP);
+    for (; k0 < hi; k0 += STEP, stage ^= 1) {
+      const int next = k0 + STEP;
+      if (next < hi) {
+        const int now = page;
+        page = page_at(next + STEP);
+        wait_lds();  // the other stage's readers are done
+        issue(next, now, stage ^ 1);
+        wait_loads<2 * INSTR>();  // the copies of this stage
+      } else {
+        wait_loads<0>();
+      }
+      const uint16_t* keys = ring + stage * (2 * 32 * DP);
+      if (k0 < all_begin || k0 + 32 > all_end)
+        t.template step<true>(keys, keys + 32 * DP, k0, alive ? mine.begin : 0, alive ? mine.end : 0, a.c);
+      else
+        t.template step<false>(keys, keys + 32 * DP, k0, 0, 0, a.c);
+    }
+    // ---- join the waves
+    __syncthreads();
+    const float l = t.total();
+    if (alive) {
+      float* o = jo + (wave * 32 + l32) * OS;
 #pragma unroll
-    for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kWave));
-    const float m_new = fmaxf(m, top);
-    const float p = j < end ? expf(s - m_new) : 0.f;
-    const float keep = m == -INFINITY ? 0.f : expf(m - m_new);
-    l = l * keep + wave_sum(p);
-    m = m_new;
+      for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] *= keep;
-    const int count = (int)(end - j0 < kWave ? end - j0 : kWave);
-    for (int c = 0; c < count; ++c) {
-      const float pc = __shfl(p, c, kWave);
-      const int64_t vo = __shfl(off, c, kWave);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int d = lane + e * kWave;
-        if (d < a.D) o[e] += pc * h2f(a.cv[vo + d]);
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<float4_t*>(o + i * 32 + e * 8 + h * 4) =
+              float4_t{t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
+      if (h == 0) {
+        jm[wave * 32 + l32] = t.mc;
+        jl[wave * 32 + l32] = l;
       }
     }
-  }
-  uint16_t* out = a.out.p + t * a.out.ts + h * a.out.hs;
+    const bool suspect = t.suspect();
+    if (lane == 0) flag[32 + wave] = suspect;
+    if (threadIdx.x < 32) flag[threadIdx.x] = 0;
+    __syncthreads();
+    const bool cut = shared && (t0 < pos || seg_end < t1);
+    const int64_t slot = cut ? slot_of(w, share, t0) : 0;
+    for (int u = threadIdx.x; u < live * (DP / 4); u += NW * kWave) {
+      const int row = u / (DP / 4), d = u % (DP / 4) * 4;
+      float top = jm[row];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int d = lane + e * kWave;
-    if (d < a.D) out[d] = begin < end ? f32_to_f16_bits(o[e] / l) : 0;
+      for (int i = 1; i < NW; ++i) top = fmaxf(top, jm[i * 32 + row]);
+      float v[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        const float m = jm[i * 32 + row], f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        const float4_t o = *reinterpret_cast<const float4_t*>(jo + (i * 32 + row) * OS + d);
+        sum += f * jl[i * 32 + row];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += f * o[e];
+      }
+      const float z = (v[0] - v[0]) + (v[1] - v[1]) + (v[2] - v[2]) + (v[3] - v[3]) + (sum - sum);
+      if (!(z == 0.f)) flag[row] = 1;
+      if (cut) {
+        *reinterpret_cast<float4_t*>(a.part_o + (slot * ROWS + row) * DP + d) = float4_t{v[0], v[1], v[2], v[3]};
+        if (d == 0) {
+          a.part_ml[(slot * ROWS + row) * 2] = top;
+          a.part_ml[(slot * ROWS + row) * 2 + 1] = sum;
+        }
+      } else {
+        const Span s = token_span(a, p.r, (row0 + row) / a.G);
+        const float f = row_factor(sum, s.begin < s.end);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= f;
+        store4(a, out_row(a, p.r, head, row0 + row), d, v);
+        if (d == 0 && a.lse != nullptr) a.lse[lse_at(a, p.r, head, row0 + row)] = row_lse(top, sum, s.begin < s.end);
+      }
+    }
+    __syncthreads();
+    int any_suspect = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) any_suspect |= flag[32 + i];
+    for (int row = wave; row < live; row += NW) {
+      if ((flag[row] | any_suspect) == 0) continue;
+      const Span s = token_span(a, p.r, (row0 + row) / a.G);
+      SlowRow<DP> slow;
+      slow.run(a, a.q.p + (p.r.q0 + (row0 + row) / a.G) * a.q.ts + (head * a.G + (row0 + row) % a.G) * a.q.hs, head_off,
+               pages, s.begin > lo ? s.begin : lo, s.end < hi ? s.end : hi);
+      slow.template store<ROWS>(a, p.r, head, row0 + row, row, cut ? slot : -1, s.begin < s.end, flag[row] != 0);
+    }
+    __syncthreads();
+    pos = seg_end;
   }
-  if (a.lse != nullptr && lane == 0) a.lse[t * a.Hq + h] = begin < end ? m + logf(l) : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------
+// 128 rows: four waves of 32 rows over shared tiles of 64 keys, two stages.
+// ---------------------------------------------------------------------------
+template <int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(AttentionArgs a) {
+  constexpr int ROWS = 128, STEP = 64, INSTR = DP / 32;
+  extern __shared__ uint8_t smem[];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int l32 = lane % 32, h = lane / 32;
+  uint16_t* ring = reinterpret_cast<uint16_t*>(smem);
+
+  const bool shared = a.part_o != nullptr;
+  const int64_t head_len = head_length<ROWS, STEP>(a, shared);
+  int64_t pos, pos_end, share = 0, w = blockIdx.x;
+  if (shared) {
+    share = share_of<STEP>(head_len * a.Hkv, a.parts, kTileShare);
+    pos = w * share;
+    pos_end = pos + share < head_len * a.Hkv ? pos + share : head_len * a.Hkv;
+  } else {
+    pos = (w % a.Hkv) * head_len + w / a.Hkv;
+    pos_end = w / a.Hkv < head_len ? pos + 1 : pos;
+  }
+  while (pos < pos_end) {
+    const int head = (int)(pos / head_len);
+    Place p = locate<ROWS, STEP>(a, pos - head * head_len, shared);
+    if (p.b < 0) return;
+    // the tiles with the most keys first
+    if (!shared) p.tile = tiles_of<ROWS>(a, p.r) - 1 - p.tile;
+    const int64_t t0 = head * head_len + p.start, t1 = head * head_len + p.end;
+    const int64_t seg_end = t1 < pos_end ? t1 : pos_end;
+    const Span span = tile_span<ROWS>(a, p.r, p.tile);
+    const int base = span.begin / 32 * 32;
+    int lo = base, hi = span.end;
+    if (shared) {
+      lo = base + (int)(pos - t0);
+      const int64_t most = base + (seg_end - t0);
+      hi = most < hi ? (int)most : hi;
+    }
+    const int rows = p.r.n * a.G, row0 = p.tile * ROWS + wave * 32;
+    const int live = rows - row0 < 32 ? rows - row0 : 32;  // may be <= 0
+    const bool alive = l32 < live;
+    Span mine = {0, 0}, all = {0, 0}, any = {0, 0};
+    if (live > 0) {
+      if (alive) mine = token_span(a, p.r, (row0 + l32) / a.G);
+      const Span s0 = token_span(a, p.r, row0 / a.G), s1 = token_span(a, p.r, (row0 + live - 1) / a.G);
+      all = {s0.begin > s1.begin ? s0.begin : s1.begin, s0.end < s1.end ? s0.end : s1.end};
+      any = {s0.begin < s1.begin ? s0.begin : s1.begin, s0.end > s1.end ? s0.end : s1.end};
+    }
+    const bool sees = mine.begin < mine.end;
+    if (mine.end > hi) mine.end = hi;
+    if (all.end > hi) all.end = hi;
+    const int32_t* pages = a.pages + p.b * a.page_row_stride;
+    const int64_t head_off = head * a.head_stride;
+
+    clear_lds<DP>(a, ring + wave * (64 * DP), 64);
+    if (a.D != DP) __syncthreads();
+    WaveTile<DP, 2> t;
+    t.clear();
+    t.load_q(a, p.r, head, row0 + l32, alive);
+    auto page_at = [&](int k) {
+      const int j = k + wave * 16 + lane % 16;
+      return k < hi ? page_of(a, pages, j < span.begin ? span.begin : j < hi ? j : hi - 1) : 0;
+    };
+    auto issue = [&](int k, int page, int stage) {
+      copy_rows<DP, INSTR>(a, head_off, page, k, span.begin, hi - 1, wave * 16, ring + stage * (2 * 64 * DP),
+                           ring + stage * (2 * 64 * DP) + 64 * DP);
+    };
+    int page = page_at(lo), stage = 0;
+    if (lo < hi) issue(lo, page, 0);
+    page = page_at(lo + STEP);
+    for (int k0 = lo; k0 < hi; k0 += STEP, stage ^= 1) {
+      wait_lds();
+      wait_loads<0>();  // this wave's copies of this stage
+      barrier_only();   // everyone's; nobody reads the other stage any more
+      if (k0 + STEP < hi) {
+        issue(k0 + STEP, page, stage ^ 1);
+        page = page_at(k0 + 2 * STEP);
+      }
+      if (k0 < any.end && k0 + STEP > any.begin) {
+        const uint16_t* keys = ring + stage * (2 * 64 * DP);
+        if (k0 < all.begin || k0 + STEP > all.end)
+          t.template step<true>(keys, keys + 64 * DP, k0, mine.begin, mine.end, a.c);
+        else
+          t.template step<false>(keys, keys + 64 * DP, k0, 0, 0, a.c);
+      }
+    }
+    const float l = t.total();
+    const bool cut = shared && (t0 < pos || seg_end < t1);
+    const int64_t slot = cut ? slot_of(w, share, t0) : 0;
+    if (alive) {
+      if (cut) {
+        const int64_t at = slot * ROWS + wave * 32 + l32;
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<float4_t*>(a.part_o + at * DP + i * 32 + e * 8 + h * 4) =
+                float4_t{t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
+        if (h == 0) {
+          a.part_ml[at * 2] = t.mc;
+          a.part_ml[at * 2 + 1] = l;
+        }
+      } else {
+        const float f = row_factor(l, sees);
+        uint16_t* dst = out_row(a, p.r, head, row0 + l32);
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v[4] = {t.o[i][4 * e] * f, t.o[i][4 * e + 1] * f, t.o[i][4 * e + 2] * f, t.o[i][4 * e + 3] * f};
+            store4(a, dst, i * 32 + e * 8 + h * 4, v);
+          }
+        if (h == 0 && a.lse != nullptr) a.lse[lse_at(a, p.r, head, row0 + l32)] = row_lse(t.mc, l, sees);
+      }
+    }
+    uint64_t broken = __ballot(alive && t.broken());
+    broken = (broken | broken >> 32) & 0xFFFFFFFFu;
+    uint64_t again = t.suspect() && live > 0 ? (uint64_t(1) << live) - 1 : broken;
+    if (again != 0) {
+      wait_loads<0>();  // the stores above come first
+      while (again != 0) {
+        const int i = __ffsll((unsigned long long)again) - 1, row = row0 + i;
+        again &= again - 1;
+        const Span s = token_span(a, p.r, row / a.G);
+        SlowRow<DP> slow;
+        slow.run(a, a.q.p + (p.r.q0 + row / a.G) * a.q.ts + (head * a.G + row % a.G) * a.q.hs, head_off, pages,
+                 s.begin > lo ? s.begin : lo, s.end < hi ? s.end : hi);
+        slow.template store<ROWS>(a, p.r, head, row, wave * 32 + i, cut ? slot : -1, s.begin < s.end,
+                                  (broken >> i & 1) != 0);
+      }
+    }
+    pos = seg_end;
+    if (pos < pos_end) __syncthreads();  // the stages are free
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joins the shares of one cut tile: workgroup x takes the tile that contains
+// the border between shares x and x + 1, if it is that tile's first border;
+// y cuts the tile's rows.  Shares are added in their order, by groups of
+// threads that take every PG-th share where there are few rows.
+// ---------------------------------------------------------------------------
+template <int DP, int ROWS, int STEP, int LEAST, int YS>
+__global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a) {
+  constexpr int TH = 256, CH = DP / 4;
+  __shared__ float so[TH * 4], sm[TH], sl[TH];
+  const int64_t head_len = head_length<ROWS, STEP>(a, true), total = head_len * a.Hkv;
+  const int64_t share = share_of<STEP>(total, a.parts, LEAST);
+  const int64_t pos = (blockIdx.x + 1) * share;
+  if (pos >= total) return;
+  const int head = (int)(pos / head_len);
+  const Place p = locate<ROWS, STEP>(a, pos - head * head_len, true);
+  if (p.b < 0) return;
+  const int64_t t0 = head * head_len + p.start, t1 = head * head_len + p.end;
+  if (t0 == pos || pos - share > t0) return;
+  const int64_t w0 = t0 / share, w1 = (t1 - 1) / share;
+  const int nparts = (int)(w1 - w0 + 1);
+  constexpr int YROWS = ROWS / YS;
+  const int rows = p.r.n * a.G, row0 = p.tile * ROWS, first = blockIdx.y * YROWS;
+  const int live = (rows - row0 < ROWS ? rows - row0 : ROWS) - first < YROWS ? rows - row0 - first : YROWS;
+  if (live <= 0) return;
+  int groups = TH / (live * CH);
+  groups = groups < 1 ? 1 : groups > nparts ? nparts : groups;
+  const int units = live * CH;
+  for (int u0 = 0; u0 < units; u0 += TH) {
+    // thread: unit (row, four values), and its group of shares
+    const int u = groups > 1 ? (int)threadIdx.x % units : u0 + (int)threadIdx.x;
+    const int g = groups > 1 ? (int)threadIdx.x / units : 0;
+    const bool active = u < units && g < groups;
+    const int row = first + u / CH, d = u % CH * 4;
+    float m = -INFINITY, l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (active) {
+#pragma unroll 4
+      for (int i = g; i < nparts; i += groups) {
+        const int64_t at = slot_of(w0 + i, share, t0) * ROWS + row;
+        const float pm = a.part_ml[at * 2], pl = a.part_ml[at * 2 + 1];
+        const float4_t o = *reinterpret_cast<const float4_t*>(a.part_o + at * DP + d);
+        const float top = fmaxf(m, pm);
+        const float fm = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        const float fp = pm == top ? 1.f : __builtin_amdgcn_exp2f(pm - top);
+        l = l * fm + pl * fp;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = v[e] * fm + o[e] * fp;
+        m = top;
+      }
+    }
+    if (groups > 1) {
+      sm[threadIdx.x] = m;
+      sl[threadIdx.x] = l;
+      *reinterpret_cast<float4_t*>(so + threadIdx.x * 4) = float4_t{v[0], v[1], v[2], v[3]};
+      __syncthreads();
+      if (g > 0 || !active) return;
+      for (int i = 1; i < groups; ++i) {
+        const int t = i * units + u;
+        const float pm = sm[t], top = fmaxf(m, pm);
+        const float fm = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        const float fp = pm == top ? 1.f : __builtin_amdgcn_exp2f(pm - top);
+        const float4_t o = *reinterpret_cast<const float4_t*>(so + t * 4);
+        l = l * fm + sl[t] * fp;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = v[e] * fm + o[e] * fp;
+        m = top;
+      }
+    }
+    if (!active) continue;
+    const Span s = token_span(a, p.r, (row0 + row) / a.G);
+    const float f = row_factor(l, s.begin < s.end);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= f;
+    store4(a, out_row(a, p.r, head, row0 + row), d, v);
+    if (d == 0 && a.lse != nullptr) a.lse[lse_at(a, p.r, head, row0 + row)] = row_lse(m, l, s.begin < s.end);
+  }
+}
+
+// Which kernel a call takes, and its grid.
+struct AttentionPlan {
+  bool few;       // k_attention_few
+  int DP;
+  int rows;       // of a tile
+  int64_t tiles;  // at most, of one cache head
+  int parts;      // shares of a split call
+  bool split;     // worth splitting
+  int64_t bytes;  // of the workspace
+};
+
+AttentionPlan plan_attention(int64_t T, int64_t B, int Hq, int Hkv, int D, const DeviceInfo& dev) {
+  AttentionPlan p;
+  const int64_t G = Hq / Hkv, rows = T * G;
+  p.DP = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+  // up to 32 rows of a request on average: a tile of 32
+  p.few = rows <= 32 * B;
+  p.rows = p.few ? 32 : 128;
+  p.tiles = rows / p.rows + (B < T ? B : T);
+  // workgroups that the chip holds at once (by LDS)
+  p.parts = dev.num_cus * (p.few ? (p.DP == 64 ? 2 : 1) : (p.DP == 256 ? 1 : 2));
+  // with twice as many whole tiles as the chip holds a split gains nothing
+  p.split = p.few || rows / p.rows * Hkv < 2 * p.parts;
+  p.bytes = p.split ? int64_t(2) * p.parts * p.rows * (p.DP + 2) * (int64_t)sizeof(float) : 0;
+  return p;
+}
+
+template <int DP>
+hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipStream_t stream) {
+  constexpr int NW = DP == 256 ? 2 : 4;
+  const bool shared = a.part_o != nullptr;
+  const int64_t blocks = shared ? pl.parts : pl.tiles * a.Hkv;
+  hipError_t e;
+  if (pl.few) {
+    if ((e = prepare_kernel(k_attention_few<DP, NW>)) != hipSuccess) return e;
+    e = launch_kernel(k_attention_few<DP, NW>, dim3((unsigned)blocks), dim3(NW * kWave), NW * 256 * DP, stream, a);
+    if (e != hipSuccess || !shared) return e;
+    return launch_kernel(k_attention_join<DP, 32, NW * 32, kFewShare, 1>, dim3((unsigned)blocks - 1), dim3(256), 0,
+                         stream, a);
+  }
+  if ((e = prepare_kernel(k_attention_tile<DP>)) != hipSuccess) return e;
+  e = launch_kernel(k_attention_tile<DP>, dim3((unsigned)blocks), dim3(256), 512 * DP, stream, a);
+  if (e != hipSuccess || !shared) return e;
+  return launch_kernel(k_attention_join<DP, 128, 64, kTileShare, 8>, dim3((unsigned)blocks - 1, 8), dim3(256), 0, stream,
+                       a);
 }
 
 }  // namespace
 
-int64_t attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D, const DeviceInfo& dev) { return 0; }
+int64_t attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D, const DeviceInfo& dev) {
+  return plan_attention(T, B, Hq, Hkv, D, dev).bytes;
+}
 
 hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hipStream_t stream) {
+  const AttentionPlan pl = plan_attention(p.T, p.B, p.Hq, p.Hkv, p.D, dev);
   AttentionArgs a = {};
   a.q = p.q;
   a.out = p.out;
@@ -115,24 +517,43 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
   a.B = p.B;
   a.Hq = p.Hq;
   a.Hkv = p.Hkv;
+  a.G = p.Hq / p.Hkv;
   a.D = p.D;
   a.ck = static_cast<const uint16_t*>(p.cache.k);
   a.cv = static_cast<const uint16_t*>(p.cache.v);
-  a.num_pages = p.cache.num_pages;
+  a.num_pages = (int)p.cache.num_pages;
   a.page_size = (uint32_t)p.cache.page_size;
+  a.page_shift = -1;
+  for (int s = 0; s < 31; ++s)
+    if (p.cache.page_size == int64_t(1) << s) a.page_shift = s;
   a.page_stride = p.cache.page_stride;
   a.slot_stride = p.cache.slot_stride;
   a.head_stride = p.cache.head_stride;
   a.pages = p.pages;
   a.page_row_stride = p.page_row_stride;
-  a.capacity = p.max_pages * p.cache.page_size;
+  a.capacity = (int)(p.max_pages * p.cache.page_size);
   a.q_start = p.q_start;
   a.kv_len = p.kv_len;
-  a.scale = p.scale;
+  a.c = (float)(std::fabs((double)p.scale) * 1.4426950408889634074);
+  a.negate = p.scale < 0.f;
   a.causal = p.causal;
-  a.window = p.window;
+  a.window = p.window < INT32_MAX / 2 ? (int)p.window : 0;  // wider than any cache: none
+  auto aligned = [](const HeadsView& v, int bytes) {
+    return reinterpret_cast<uintptr_t>(v.p) % bytes == 0 && v.ts % (bytes / 2) == 0 && v.hs % (bytes / 2) == 0;
+  };
+  a.q_vec = aligned(p.q, 16);
+  a.out_vec = aligned(p.out, 8);
   a.lse = p.lse;
-  return launch_kernel(k_attention_rows, dim3((unsigned)((p.T * p.Hq + 3) / 4)), dim3(256), 0, stream, a);
+  if (pl.split && p.workspace != nullptr && p.workspace_bytes >= pl.bytes) {
+    a.parts = pl.parts;
+    a.part_o = static_cast<float*>(p.workspace);
+    a.part_ml = a.part_o + int64_t(2) * pl.parts * pl.rows * pl.DP;
+  }
+  switch (pl.DP) {
+    case 64: return launch_planned<64>(pl, a, stream);
+    case 128: return launch_planned<128>(pl, a, stream);
+    default: return launch_planned<256>(pl, a, stream);
+  }
 }
 
 }  // namespace fasq
