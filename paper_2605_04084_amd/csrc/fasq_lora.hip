@@ -50,35 +50,43 @@ struct LoraArgs {
   LoraProjection p[kLoraMaxCount];
 };
 
+// A quotient that is the same in every lane: the division leaves it in a vector
+// register.
+__device__ __forceinline__ int scalar(uint32_t v) { return __builtin_amdgcn_readfirstlane((int)v); }
+
 typedef half8_t half8_any __attribute__((aligned(2)));
 
 // Eight values at p[at ...] of a row of n (zeros behind its end).  Without
 // VEC the row may start anywhere and end inside the eight: they are read at
 // once all the same, past the row's end too, but not past `last`, the end of
-// the tensor.
-template <bool VEC>
-__device__ __forceinline__ half8_t row8(const uint16_t* p, int64_t at, int64_t n, const uint16_t* last, bool live) {
-  if constexpr (VEC) {  // one load in any case, so that loads of different rows follow each other
-    const bool has = live && at < n;
-    const half8_t v = *reinterpret_cast<const half8_t*>(has ? p + at : last - 8);
-    return has ? v : half8_t{};
+// the tensor.  There is one load in any case (of the tensor's last values where
+// there is nothing to read), so that the loads of different rows follow each
+// other without a branch between them.  RAW: what lies behind the row's end,
+// or of a row that is not live, is anything, and nothing has to wait for the
+// loaded values yet.
+template <bool VEC, bool RAW = false>
+__device__ __forceinline__ half8_t row8(const uint16_t* p, int64_t at, int64_t n, const uint16_t* last, int64_t total,
+                                        bool live) {
+  const bool has = live && at < n;
+  const uint16_t* q = p + at;
+  if constexpr (VEC) {
+    const half8_t v = *reinterpret_cast<const half8_t*>(has ? q : last - 8);
+    return RAW || has ? v : half8_t{};
   }
+  const bool end = has && last - q < 8;
   half8_t v = {};
-  if (live && at < n) {
-    if (last - p - at >= 8) {
-      v = *reinterpret_cast<const half8_any*>(p + at);
-    } else {
+  if (total >= 8) v = *reinterpret_cast<const half8_any*>(has && !end ? q : last - 8);
+  u32x4 w = __builtin_bit_cast(u32x4, v);
+  if (end) {
+    w = u32x4{};
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (p + at + i < last) v[i] = __builtin_bit_cast(half_t, p[at + i]);
-    }
-    u32x4 w = __builtin_bit_cast(u32x4, v);
-    const int keep = n - at < 8 ? (int)(n - at) : 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] &= keep >= 2 * i + 2 ? ~0u : keep == 2 * i + 1 ? 0xFFFFu : 0u;
-    v = __builtin_bit_cast(half8_t, w);
+    for (int i = 0; i < 8; ++i) w[i / 2] |= (uint32_t)(q + i < last ? q[i] : 0) << (i % 2 * 16);
   }
-  return v;
+  if constexpr (RAW) return __builtin_bit_cast(half8_t, w);
+  const int keep = !has ? 0 : n - at < 8 ? (int)(n - at) : 8;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] &= keep >= 2 * i + 2 ? ~0u : keep == 2 * i + 1 ? 0xFFFFu : 0u;
+  return __builtin_bit_cast(half8_t, w);
 }
 
 // The adapters of a block of TM tokens: lane l holds the ids of tokens l, l +
@@ -132,9 +140,9 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraArgs a) {
   __shared__ float4_t sums[3][RT * TT][kWave];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l16 = lane % 16, g = lane / 16;
-  const int m0 = blockIdx.x / a.J * TM, j = blockIdx.x % a.J;
-  const int i = blockIdx.y % a.count, r0 = blockIdx.y / a.count * (16 * RT);
-  const int64_t begin = blockIdx.z * a.k_share, end = begin + a.k_share < a.K ? begin + a.k_share : a.K;
+  const int m0 = blockIdx.x * TM, j = scalar(blockIdx.z / a.splits), z = blockIdx.z - j * a.splits;
+  const int rank_part = scalar(blockIdx.y / a.count), i = blockIdx.y - rank_part * a.count, r0 = rank_part * (16 * RT);
+  const int64_t begin = z * a.k_share, end = begin + a.k_share < a.K ? begin + a.k_share : a.K;
   const BlockIds<TM> ids(a, m0);
   ids.each(j, a.J, [&](int ad, const uint64_t (&masks)[1]) {
     const uint64_t mask = masks[0];
@@ -143,17 +151,16 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraArgs a) {
     float4_t acc[RT][TT] = {};
     // UN steps' loads before their products; steps past the end are zeros
     constexpr int UN = RT * TT >= 8 ? 2 : 4;
-    const uint16_t* x_last = a.x + (int64_t)a.M * a.K;
-    const uint16_t* A_last = a.p[i].A + a.L * a.r * a.K;
+    const int64_t x_all = (int64_t)a.M * a.K, A_all = a.L * a.r * a.K;
     for (int64_t k = begin + wave * (32 * UN); k < end; k += 4 * 32 * UN) {
       half8_t b[UN][TT], w[UN][RT];
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
         const int64_t at = k + u * 32 + g * 8;
 #pragma unroll
-        for (int q = 0; q < TT; ++q) b[u][q] = row8<VEC>(x + q * 16 * a.K, at, end, x_last, mask >> (q * 16 + l16) & 1);
+        for (int q = 0; q < TT; ++q) b[u][q] = row8<VEC>(x + q * 16 * a.K, at, end, a.x + x_all, x_all, mask >> (q * 16 + l16) & 1);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) w[u][t] = row8<VEC>(A + t * 16 * a.K, at, end, A_last, r0 + t * 16 + l16 < a.r);
+        for (int t = 0; t < RT; ++t) w[u][t] = row8<VEC>(A + t * 16 * a.K, at, end, a.p[i].A + A_all, A_all, r0 + t * 16 + l16 < a.r);
       }
 #pragma unroll
       for (int u = 0; u < UN; ++u)
@@ -176,7 +183,7 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraArgs a) {
 #pragma unroll
     for (int q = 0; q < TT; ++q) {
       const bool mine = mask >> (q * 16 + l16) & 1;
-      float* out = a.t + (((int64_t)blockIdx.z * a.count + i) * a.M + m0 + q * 16 + l16) * a.r;
+      float* out = a.t + (((int64_t)z * a.count + i) * a.M + m0 + q * 16 + l16) * a.r;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
 #pragma unroll
@@ -256,12 +263,13 @@ __global__ __launch_bounds__(256, 2) void k_lora_up(LoraArgs a) {
   constexpr int TT = TM / 16;
   constexpr bool FOLDED = TM > 16;
   extern __shared__ uint8_t smem[];
-  const LoraProjection& p = a.p[blockIdx.z];
+  const int j = scalar(blockIdx.z / a.count), i = blockIdx.z - j * a.count;
+  const LoraProjection& p = a.p[i];
     const int n_block = blockIdx.y * (kSlice * a.slices);
   if (n_block >= p.N) return;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l16 = lane % 16, g = lane / 16;
-  const int m0 = blockIdx.x / a.J * TM, j = blockIdx.x % a.J;
+  const int m0 = blockIdx.x * TM;
   const int rp = (a.r + 31) / 32 * 32;
   // not folded: the block's low-rank values in LDS
   const int pitch = rp + 8;
@@ -272,21 +280,17 @@ __global__ __launch_bounds__(256, 2) void k_lora_up(LoraArgs a) {
   const BlockIds<TM> ids(a, m0);
   constexpr int W = BlockIds<TM>::W;
 
+  const int64_t B_all = a.L * p.N * a.r, y_all = (int64_t)a.M * p.N;
   // the kU features n ... of token m
   auto load = [&](int m, int n, bool live) {
     if (p.base == nullptr) return half8_t{};
-    const uint16_t* at = p.base + (int64_t)m * p.N + n;
-    if constexpr (VEC) return *reinterpret_cast<const half8_t*>(live && n < p.N ? at : p.base);
-    if (!live || n >= p.N) return half8_t{};
-    u32x4 w = {};  // the row's last value in the place of those behind it
-#pragma unroll
-    for (int e = 0; e < kU; ++e) w[e / 2] |= (uint32_t)at[n + e < p.N ? e : p.N - 1 - n] << (e % 2 * 16);
-    return __builtin_bit_cast(half8_t, w);
+    return row8<VEC, true>(p.base + (int64_t)m * p.N, n, p.N, p.base + y_all, y_all, live);
   };
   auto store = [&](int m, int n, half8_t v) {
     uint16_t* at = p.y + (int64_t)m * p.N + n;
-    if constexpr (VEC) {
-      if (n < p.N) *reinterpret_cast<half8_t*>(at) = v;
+    if (VEC || n + 8 <= p.N) {
+      if (VEC && n < p.N) *reinterpret_cast<half8_t*>(at) = v;
+      if (!VEC) *reinterpret_cast<half8_any*>(at) = v;
       return;
     }
     const u32x4 w = __builtin_bit_cast(u32x4, v);
@@ -294,14 +298,13 @@ __global__ __launch_bounds__(256, 2) void k_lora_up(LoraArgs a) {
     for (int e = 0; e < kU; ++e)
       if (n + e < p.N) at[e] = (uint16_t)(w[e / 2] >> (e % 2 * 16));
   };
-  const uint16_t* B_last = p.B + a.L * p.N * a.r;
 
   ids.each(j, a.J, [&](int ad, const uint64_t (&mask)[W]) {
     if constexpr (!FOLDED) {  // 16 lanes a token
       __syncthreads();  // the last adapter's values have been read
       const int64_t split = (int64_t)a.count * a.M * a.r;
       const int tok = threadIdx.x / 16;
-      const float* src = a.t + ((int64_t)blockIdx.z * a.M + m0 + tok) * a.r;
+      const float* src = a.t + ((int64_t)i * a.M + m0 + tok) * a.r;
       float v[NQ] = {}, top = 0.f;
       auto add = [&](int z) {
 #pragma unroll
@@ -336,11 +339,11 @@ __global__ __launch_bounds__(256, 2) void k_lora_up(LoraArgs a) {
     for (int n0 = n_block + wave * (16 * kU); n0 < n_end; n0 += kSlice) {
       const int n = n0 + l16 * kU;
       const uint16_t* B = p.B + ((int64_t)ad * p.N + n) * a.r;
-      auto rank8 = [&](int k, int u) { return row8<VEC>(B + u * a.r, k + g * 8, a.r, B_last, n + u < p.N); };
+      auto rank8 = [&](int k, int u) { return row8<VEC>(B + u * a.r, k + g * 8, a.r, p.B + B_all, B_all, n + u < p.N); };
       auto low = [&](int t, int k, half8_t& th, half8_t& tl) {
         if constexpr (FOLDED) {
           const int m = m0 + t * 16 + l16;
-          const half_t* h = a.low + ((int64_t)blockIdx.z * a.M + (m < a.M ? m : a.M - 1)) * (2 * rp) + k + g * 8;
+          const half_t* h = a.low + ((int64_t)i * a.M + (m < a.M ? m : a.M - 1)) * (2 * rp) + k + g * 8;
           th = *reinterpret_cast<const half8_t*>(h);
           tl = *reinterpret_cast<const half8_t*>(h + rp);
         } else {
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(256, 2) void k_lora_up(LoraArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int m = m0 + t * 16 + g * 4 + e;
-            r.f[e] = a.factors[(int64_t)blockIdx.z * a.M + (m < a.M ? m : a.M - 1)];
+            r.f[e] = a.factors[(int64_t)i * a.M + (m < a.M ? m : a.M - 1)];
           }
           if constexpr (NQ <= 4) {
 #pragma unroll
@@ -473,11 +476,15 @@ LoraPlan plan_lora(int64_t M, int64_t K, int r, int count, const DeviceInfo& dev
   return p;
 }
 
-// Workgroups that share the adapters of a block: a block of a decode batch may
-// hold one per token, one of a prompt seldom more than one.
-int sharers(int64_t M, int64_t L, int TM) {
-  const int64_t most = M < 16 ? M : M <= 128 ? 16 : 1;
-  return (int)(L < most ? L : most < TM ? most : TM);
+// Workgroups that share the adapters of a block of TM tokens, which may hold
+// one per token: as many as there is room for on the chip.  (They are the
+// grid's slowest dimension: those that find nothing to do end together, and do
+// not leave every other XCD idle.)
+int sharers(int64_t M, int64_t L, int TM, int64_t wide, const DeviceInfo& dev) {
+  int64_t j = up_to(2 * dev.num_cus, wide);
+  j = j < L ? j : L;
+  j = j < TM ? j : TM;
+  return (int)(j < M ? j : M);
 }
 
 template <int TT, int RT>
@@ -529,8 +536,9 @@ hipError_t launch_lora(const LoraProblem& p, const DeviceInfo& dev, hipStream_t 
   }
   hipError_t e;
   const int64_t ranks = up_to(a.r, 16 * pl.RT);
-  a.J = sharers(p.M, p.L, pl.TD);
-  const dim3 down((unsigned)(up_to(p.M, pl.TD) * a.J), (unsigned)(a.count * ranks), (unsigned)pl.splits);
+  const int64_t td = up_to(p.M, pl.TD);
+  a.J = sharers(p.M, p.L, pl.TD, td * a.count * ranks * pl.splits, dev);
+  const dim3 down((unsigned)td, (unsigned)(a.count * ranks), (unsigned)(pl.splits * a.J));
   switch (pl.RT * 100 + pl.TD) {
     case 116: e = launch_down<1, 1>(a, down, vec_k, stream); break;
     case 216: e = launch_down<1, 2>(a, down, vec_k, stream); break;
@@ -546,13 +554,14 @@ hipError_t launch_lora(const LoraProblem& p, const DeviceInfo& dev, hipStream_t 
     e = launch_kernel(k_lora_fold, dim3((unsigned)up_to(p.M * p.count, 4)), dim3(256), 0, stream, a);
     if (e != hipSuccess) return e;
   }
-  a.J = sharers(p.M, p.L, pl.TU);
   // several slices share what a workgroup makes of the low-rank values, where
   // enough workgroups are left
   const int64_t blocks = up_to(p.M, pl.TU) * p.count, slices = up_to(most_n, kSlice);
   a.slices = 1;
   while (a.slices < 8 && blocks * up_to(slices, 2 * a.slices) >= 4 * dev.num_cus) a.slices *= 2;
-  const dim3 up((unsigned)(up_to(p.M, pl.TU) * a.J), (unsigned)up_to(slices, a.slices), (unsigned)p.count);
+  const int64_t tu = up_to(p.M, pl.TU), ny = up_to(slices, a.slices);
+  a.J = sharers(p.M, p.L, pl.TU, tu * ny * a.count, dev);
+  const dim3 up((unsigned)tu, (unsigned)ny, (unsigned)(a.count * a.J));
   if (pl.TU == 16)
     return a.r <= 16   ? launch_up<16, 1>(a, up, vec_r, stream)
            : a.r <= 64 ? launch_up<16, 4>(a, up, vec_r, stream)
