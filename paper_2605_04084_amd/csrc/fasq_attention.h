@@ -40,7 +40,7 @@ struct AttentionArgs {
   int capacity;  // max_pages * page_size
   const int32_t* q_start;
   const int32_t* kv_len;
-  float c;  // |scale| * log2(e)
+  float c;  // |scale| * log2(e), at least 1e-30 so that -inf stays -inf
   bool negate;  // scale < 0: the queries change sign instead
   bool causal;
   bool q_vec, out_vec;  // 16-byte loads of q, 8-byte stores of out
@@ -252,6 +252,30 @@ __device__ __forceinline__ void copy16_to_lds(const uint16_t* src, void* lds) {
   __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
+// Values of a tile that some of its rows do not see: a weight of zero leaves a
+// finite value out of a sum, but not NaN or an infinity.  Where rows of a tile
+// see different keys (only there), the tile's values are cut to finite ones in
+// LDS before they are used.  Returns whether any was not (in any lane): then
+// rows are checked key by key at the end (SlowRow).  One wave, rows [0, ROWS)
+// of DP values that it has copied itself.
+template <int DP, int ROWS>
+__device__ __forceinline__ bool cut_to_finite(uint16_t* values) {
+  constexpr int N = ROWS * DP / 8 / kWave;
+  const half_t most = static_cast<half_t>(65504.f);
+  half8_t bad = {};
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    half8_t* at = reinterpret_cast<half8_t*>(values) + i * kWave + threadIdx.x % kWave;
+    const half8_t v = *at;
+    bad += v * half8_t{};  // NaN where v is not finite
+    *at = __builtin_elementwise_min(__builtin_elementwise_max(v, half8_t(-most)), half8_t(most));
+  }
+  bool nan = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) nan = nan || !(bad[e] == static_cast<half_t>(0.f));
+  return __any(nan);
+}
+
 // ---------------------------------------------------------------------------
 // One wave: 32 rows against KB blocks of 32 keys at a time
 // ---------------------------------------------------------------------------
@@ -259,17 +283,16 @@ template <int DP, int KB>
 struct WaveTile {
   half8_t q[DP / 16];
   float16_t o[DP / 32];
-  float m, mc, l;  // running maximum of the scores (this row), m * c, sum of this lane's weights
-  half8_t bad;     // NaN where a value of a masked tile was not finite
+  float m, mc, l;  // running maximum of the scores (this row), m * c (0 without one), sum of this lane's weights
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    m = mc = -INFINITY;
+    m = -INFINITY;
+    mc = 0.f;
     l = 0.f;
-    bad = half8_t{};
   }
 
   // Row `row` of the request (lane l and l ^ 32 hold one row; rows past the
@@ -281,15 +304,15 @@ struct WaveTile {
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {
       const int d = s * 16 + h * 8;
-      half8_t v;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = static_cast<half_t>(0.f);
+      half8_t v = {};
       if (live && d < a.D) {
         if (a.q_vec) {
           v = *reinterpret_cast<const half8_t*>(src + d);
         } else {
+          u32x4 w = {};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(half_t, src[d + e]);
+          for (int e = 0; e < 8; ++e) w[e / 2] |= (uint32_t)src[d + e] << (e % 2 * 16);
+          v = __builtin_bit_cast(half8_t, w);
         }
         if (a.negate) v = -v;
       }
@@ -298,35 +321,67 @@ struct WaveTile {
   }
 
   // keys, values: the tile's rows in LDS (KB * 32 of them); key0: its first
-  // key.  A row sees keys [begin, end).  MASKED: not every live row sees all
-  // of them; the values are then cut to finite ones, since a weight of zero
-  // leaves those out but not NaN and infinities, and `bad` remembers the cut.
-  template <bool MASKED>
+  // key.  A row sees keys [begin, end); `masked` (uniform): not every live row
+  // sees all of the tile.  Operands are read from LDS a step or two ahead of
+  // the products that take them; the scheduling barriers keep them there.
   __device__ __forceinline__ void step(const uint16_t* keys, const uint16_t* values, int key0, int begin, int end,
-                                       float c) {
+                                       bool masked, float c) {
     const int lane = threadIdx.x % kWave, l32 = lane % 32, h = lane / 32;
+    constexpr int KT = DP / 16, AHEAD = 2;
+    const uint32_t k_at = lds_address(keys) + l32 * (DP * 2) + (h ^ chunk_swap<DP>(l32)) * 16;
+    half8_t k[AHEAD + 1][KB];
+    auto read_k = [&](int t) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+        k[t % (AHEAD + 1)][kb] = *(lds_half8)(uintptr_t)((k_at ^ (t % 8 * 32)) + t / 8 * 256 + kb * 32 * DP * 2);
+    };
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) read_k(t);
     float16_t s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-    const uint32_t k_at = lds_address(keys) + l32 * (DP * 2) + (h ^ chunk_swap<DP>(l32)) * 16;
 #pragma unroll
-    for (int t = 0; t < DP / 16; ++t) {
-      if constexpr (MASKED) __builtin_amdgcn_sched_barrier(0);
+    for (int t = 0; t < KT; ++t) {
+      if (t + AHEAD < KT) read_k(t + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const half8_t k = *(lds_half8)(uintptr_t)((k_at ^ (t % 8 * 32)) + t / 8 * 256 + kb * 32 * DP * 2);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[t], s[kb], 0, 0, 0);
-      }
+      for (int kb = 0; kb < KB; ++kb)
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t % (AHEAD + 1)][kb], q[t], s[kb], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (MASKED) {
+    // rows of V in the order of the score registers: weight j of slab u is
+    // key 16 u + (j / 4) * 8 + h * 4 + j % 4; operands in groups of four
+    // blocks of 32 dimensions
+    constexpr int GI = DP / 32 < 4 ? DP / 32 : 4, GROUPS = 2 * KB * (DP / 32) / GI;
+    const int r = (lane % 16) / 4, x = (lane / 16 & 1) * 2 + (lane & 3) / 2;
+    uint32_t v_at[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = j * 8 + h * 4 + r;
+      v_at[j] = lds_address(values) + row * (DP * 2) + (x ^ chunk_swap<DP>(row)) * 16 + (lane & 1) * 8;
+    }
+    short4_t v[2][GI][2];
+    auto read_v = [&](int g) {
+      const int u = g * GI / (DP / 32), i0 = g * GI % (DP / 32);
+#pragma unroll
+      for (int i = 0; i < GI; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          v[g % 2][i][j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_short4)(uintptr_t)((v_at[j] ^ ((i0 + i) % 4 * 64)) + (i0 + i) / 4 * 256 + u * 16 * DP * 2));
+    };
+    read_v(0);
+    __builtin_amdgcn_sched_barrier(0);
+    if (masked) {
+      const int first = begin - key0 - h * 4, last = end - key0 - h * 4;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int key = key0 + kb * 32 + (e / 4) * 8 + h * 4 + e % 4;
-          if (key < begin || key >= end) s[kb][e] = -INFINITY;
+          const int key = kb * 32 + (e / 4) * 8 + e % 4;
+          s[kb][e] = key < first || key >= last ? -INFINITY : s[kb][e];
         }
     }
     float top = s[0][0];
@@ -341,7 +396,7 @@ struct WaveTile {
     // The maximum need not be the newest one: weights up to 2^8 are as exact
     // in fp16 as weights up to 1, so a row is rescaled only where its maximum
     // has grown by more than that (each row by its own scores alone).
-    const bool grown = (top - m) * c > 8.f || (m == -INFINITY && top > -INFINITY);
+    const bool grown = (top - m) * c > 8.f;  // from -inf too; not from -inf to -inf
     if (__any(grown)) {
       // the weights are 2^(s c - mc) with the rounded product mc, here too
       const float next_c = top * c;
@@ -359,40 +414,27 @@ struct WaveTile {
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        float w = __builtin_amdgcn_exp2f(s[kb][e] * c - mc);
-        if (MASKED && s[kb][e] == -INFINITY) w = 0.f;
+        const float w = __builtin_amdgcn_exp2f(s[kb][e] * c - mc);
         l += w;
         p[2 * kb + e / 8][e % 8] = static_cast<half_t>(w);
       }
-    // rows of V in the order of the score registers: weight j of slab u is
-    // key 16 u + (j / 4) * 8 + h * 4 + j % 4
-    const int r = (lane % 16) / 4, x = (lane / 16 & 1) * 2 + (lane & 3) / 2;
-    uint32_t v_at[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int row = j * 8 + h * 4 + r;
-      v_at[j] = lds_address(values) + row * (DP * 2) + (x ^ chunk_swap<DP>(row)) * 16 + (lane & 1) * 8;
-    }
+    for (int g = 0; g < GROUPS; ++g) {
+      if (g + 1 < GROUPS) read_v(g + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const int u = g * GI / (DP / 32), i0 = g * GI % (DP / 32);
 #pragma unroll
-    for (int u = 0; u < 2 * KB; ++u)
-#pragma unroll
-      for (int i = 0; i < DP / 32; ++i) {
-        if constexpr (MASKED) __builtin_amdgcn_sched_barrier(0);  // few registers, seldom run
-        short4_t part[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_short4)(uintptr_t)((v_at[j] ^ (i % 4 * 64)) + i / 4 * 256 + u * 16 * DP * 2));
-        }
-        half8_t v = __builtin_bit_cast(half8_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
-        if constexpr (MASKED) {
-          const half_t most = static_cast<half_t>(65504.f);
-          bad += v * half8_t{};
-          v = __builtin_elementwise_min(__builtin_elementwise_max(v, half8_t(-most)), half8_t(most));
-        }
-        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[u], o[i], 0, 0, 0);
+      for (int i = 0; i < GI; ++i) {
+        const half8_t vv = __builtin_bit_cast(
+            half8_t, __builtin_shufflevector(v[g % 2][i][0], v[g % 2][i][1], 0, 1, 2, 3, 4, 5, 6, 7));
+        o[i0 + i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vv, p[u], o[i0 + i], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
+
+  // The maximum as partial results hold it, in powers of two.
+  __device__ __forceinline__ float top() const { return m == -INFINITY ? m : mc; }
 
   // Sum of the row's weights, in both its lanes.
   __device__ __forceinline__ float total() const {
@@ -400,17 +442,9 @@ struct WaveTile {
     return __uint_as_float(w[0]) + __uint_as_float(w[1]);
   }
 
-  // Whether a masked tile held values that are not finite (uniform).
-  __device__ __forceinline__ bool suspect() const {
-    bool nan = false;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) nan = nan || !(bad[e] == static_cast<half_t>(0.f));
-    return __any(nan);
-  }
-
   // Whether this lane's part of the row holds a value that is not finite.
   __device__ __forceinline__ bool broken() const {
-    float z = (l - l) + (mc == -INFINITY ? 0.f : mc - mc);
+    float z = (l - l) + (mc - mc);
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
 #pragma unroll

@@ -133,6 +133,8 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
     const Span s0 = token_span(a, p.r, row0 / a.G), s1 = token_span(a, p.r, (row0 + live - 1) / a.G);
     const int all_begin = s0.begin > s1.begin ? s0.begin : s1.begin;
     int all_end = s0.end < s1.end ? s0.end : s1.end;
+    const bool mixed = s0.begin != s1.begin || s0.end != s1.end;  // rows see different keys
+    bool suspect = false;
     if (mine.end > hi) mine.end = hi;
     if (all_end > hi) all_end = hi;
     const int32_t* pages = a.pages + p.b * a.page_row_stride;
@@ -165,11 +167,10 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
       } else {
         wait_loads<0>();
       }
-      const uint16_t* keys = ring + stage * (2 * 32 * DP);
-      if (k0 < all_begin || k0 + 32 > all_end)
-        t.template step<true>(keys, keys + 32 * DP, k0, alive ? mine.begin : 0, alive ? mine.end : 0, a.c);
-      else
-        t.template step<false>(keys, keys + 32 * DP, k0, 0, 0, a.c);
+      uint16_t* keys = ring + stage * (2 * 32 * DP);
+      const bool masked = k0 < all_begin || k0 + 32 > all_end;
+      if (masked && mixed) suspect |= cut_to_finite<DP, 32>(keys + 32 * DP);
+      t.step(keys, keys + 32 * DP, k0, alive ? mine.begin : 0, alive ? mine.end : 0, masked, a.c);
     }
     // ---- join the waves
     __syncthreads();
@@ -183,11 +184,10 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
           *reinterpret_cast<float4_t*>(o + i * 32 + e * 8 + h * 4) =
               float4_t{t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
       if (h == 0) {
-        jm[wave * 32 + l32] = t.mc;
+        jm[wave * 32 + l32] = t.top();
         jl[wave * 32 + l32] = l;
       }
     }
-    const bool suspect = t.suspect();
     if (lane == 0) flag[32 + wave] = suspect;
     if (threadIdx.x < 32) flag[threadIdx.x] = 0;
     __syncthreads();
@@ -251,6 +251,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l32 = lane % 32, h = lane / 32;
   uint16_t* ring = reinterpret_cast<uint16_t*>(smem);
+  int* flag = reinterpret_cast<int*>(smem + 512 * DP);  // a value of a mixed tile was not finite
 
   const bool shared = a.part_o != nullptr;
   const int64_t head_len = head_length<ROWS, STEP>(a, shared);
@@ -289,9 +290,16 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       all = {s0.begin > s1.begin ? s0.begin : s1.begin, s0.end < s1.end ? s0.end : s1.end};
       any = {s0.begin < s1.begin ? s0.begin : s1.begin, s0.end > s1.end ? s0.end : s1.end};
     }
+    // over the four waves: whether rows see different keys, and which all see
+    const int tile_rows = rows - p.tile * ROWS < ROWS ? rows - p.tile * ROWS : ROWS;
+    const Span f0 = token_span(a, p.r, p.tile * ROWS / a.G), f1 = token_span(a, p.r, (p.tile * ROWS + tile_rows - 1) / a.G);
+    const bool mixed = f0.begin != f1.begin || f0.end != f1.end;
+    const int most_begin = f0.begin > f1.begin ? f0.begin : f1.begin, least_end = f0.end < f1.end ? f0.end : f1.end;
     const bool sees = mine.begin < mine.end;
     if (mine.end > hi) mine.end = hi;
     if (all.end > hi) all.end = hi;
+    if (threadIdx.x == 0) *flag = 0;
+    __syncthreads();
     const int32_t* pages = a.pages + p.b * a.page_row_stride;
     const int64_t head_off = head * a.head_stride;
 
@@ -314,6 +322,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     for (int k0 = lo; k0 < hi; k0 += STEP, stage ^= 1) {
       wait_lds();
       wait_loads<0>();  // this wave's copies of this stage
+      if (mixed && (k0 < most_begin || k0 + STEP > least_end)) {
+        if (cut_to_finite<DP, 16>(ring + stage * (2 * 64 * DP) + 64 * DP + wave * 16 * DP)) *flag = 1;
+        wait_lds();
+      }
       barrier_only();   // everyone's; nobody reads the other stage any more
       if (k0 + STEP < hi) {
         issue(k0 + STEP, page, stage ^ 1);
@@ -321,10 +333,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       }
       if (k0 < any.end && k0 + STEP > any.begin) {
         const uint16_t* keys = ring + stage * (2 * 64 * DP);
-        if (k0 < all.begin || k0 + STEP > all.end)
-          t.template step<true>(keys, keys + 64 * DP, k0, mine.begin, mine.end, a.c);
-        else
-          t.template step<false>(keys, keys + 64 * DP, k0, 0, 0, a.c);
+        t.step(keys, keys + 64 * DP, k0, mine.begin, mine.end, k0 < all.begin || k0 + STEP > all.end, a.c);
       }
     }
     const float l = t.total();
@@ -340,7 +349,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
             *reinterpret_cast<float4_t*>(a.part_o + at * DP + i * 32 + e * 8 + h * 4) =
                 float4_t{t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
         if (h == 0) {
-          a.part_ml[at * 2] = t.mc;
+          a.part_ml[at * 2] = t.top();
           a.part_ml[at * 2 + 1] = l;
         }
       } else {
@@ -353,12 +362,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
             const float v[4] = {t.o[i][4 * e] * f, t.o[i][4 * e + 1] * f, t.o[i][4 * e + 2] * f, t.o[i][4 * e + 3] * f};
             store4(a, dst, i * 32 + e * 8 + h * 4, v);
           }
-        if (h == 0 && a.lse != nullptr) a.lse[lse_at(a, p.r, head, row0 + l32)] = row_lse(t.mc, l, sees);
+        if (h == 0 && a.lse != nullptr) a.lse[lse_at(a, p.r, head, row0 + l32)] = row_lse(t.top(), l, sees);
       }
     }
     uint64_t broken = __ballot(alive && t.broken());
     broken = (broken | broken >> 32) & 0xFFFFFFFFu;
-    uint64_t again = t.suspect() && live > 0 ? (uint64_t(1) << live) - 1 : broken;
+    __syncthreads();
+    uint64_t again = *flag != 0 && live > 0 ? (uint64_t(1) << live) - 1 : broken;
     if (again != 0) {
       wait_loads<0>();  // the stores above come first
       while (again != 0) {
@@ -496,7 +506,7 @@ hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipSt
                          stream, a);
   }
   if ((e = prepare_kernel(k_attention_tile<DP>)) != hipSuccess) return e;
-  e = launch_kernel(k_attention_tile<DP>, dim3((unsigned)blocks), dim3(256), 512 * DP, stream, a);
+  e = launch_kernel(k_attention_tile<DP>, dim3((unsigned)blocks), dim3(256), 512 * DP + 16, stream, a);
   if (e != hipSuccess || !shared) return e;
   return launch_kernel(k_attention_join<DP, 128, 64, kTileShare, 8>, dim3((unsigned)blocks - 1, 8), dim3(256), 0, stream,
                        a);
@@ -535,6 +545,7 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
   a.q_start = p.q_start;
   a.kv_len = p.kv_len;
   a.c = (float)(std::fabs((double)p.scale) * 1.4426950408889634074);
+  if (a.c < 1e-30f) a.c = 1e-30f;
   a.negate = p.scale < 0.f;
   a.causal = p.causal;
   a.window = p.window < INT32_MAX / 2 ? (int)p.window : 0;  // wider than any cache: none
