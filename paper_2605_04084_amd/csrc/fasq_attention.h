@@ -44,6 +44,7 @@ struct AttentionArgs {
   bool negate;  // scale < 0: the queries change sign instead
   bool causal;
   bool q_vec, out_vec;  // 16-byte loads of q, 8-byte stores of out
+  bool whole_units;     // pages hold whole units of 16 keys, within 2^31 bytes
   int window;  // 0: none
   float* lse;
   // Split over workgroups (part_o != nullptr): workgroup w of `parts` takes
@@ -248,9 +249,61 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-__device__ __forceinline__ void copy16_to_lds(const uint16_t* src, void* lds) {
-  __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+// Copies of 16 bytes a lane from memory to LDS (address `to`, uniform, plus 16
+// bytes a lane).  Written out because the compiler holds every transposing
+// read of LDS back until all copies it knows of have landed, also those of
+// other stages; the kernels wait for their copies themselves (wait_loads).
+__device__ __forceinline__ void copy16_to_lds(const uint16_t* src, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory");
 }
+// The same from a uniform base and a byte offset per lane.
+__device__ __forceinline__ void copy16_to_lds(const uint16_t* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base)
+               : "memory");
+}
+
+// Copies of 16 rows of a cache head to LDS by one wave, INSTR copies of RPI rows.
+template <int DP>
+struct RowCopy {
+  static constexpr int CH = DP / 8, RPI = kWave / CH, INSTR = 16 / RPI;
+  uint32_t offset[INSTR];  // of this lane, where the 16 rows lie in one page
+  uint32_t on;             // bit i: copy i brings a chunk below D
+
+  __device__ __forceinline__ explicit RowCopy(const AttentionArgs& a) {
+    const int lane = threadIdx.x % kWave;
+    on = 0;
+#pragma unroll
+    for (int i = 0; i < INSTR; ++i) {
+      const int row = i * RPI + lane / CH, chunk = (lane % CH) ^ chunk_swap<DP>(row);
+      offset[i] = (uint32_t)(row * a.slot_stride + chunk * 8) * 2;
+      on |= (chunk * 8 < a.D ? 1u : 0u) << i;
+    }
+  }
+
+  // Keys k .. k + 15 (k a multiple of 16), those outside [first, last] in the
+  // place of the nearest inside.  `page`: lane l's page of key k + l % 16 as cut
+  // (page_of).  to: the LDS address of the first row.
+  __device__ __forceinline__ void run(const AttentionArgs& a, const uint16_t* cache, int64_t head_off, int page, int k,
+                                      int first, int last, uint32_t to) const {
+    if (a.whole_units && k >= first && k + 15 <= last) {  // one page, every key there
+      const uint16_t* base = cache + uniform(key_offset(a, uniform(page), k) + head_off);
+#pragma unroll
+      for (int i = 0; i < INSTR; ++i)
+        if (a.D == DP || (on >> i & 1)) copy16_to_lds(base, offset[i], to + i * 1024);
+      return;
+    }
+    const int lane = threadIdx.x % kWave, j = k + lane % 16;
+    const int64_t own = key_offset(a, page, j < first ? first : j < last ? j : last) + head_off;
+    int64_t off[INSTR];
+#pragma unroll
+    for (int i = 0; i < INSTR; ++i) off[i] = __shfl(own, i * RPI + lane / CH, kWave);
+#pragma unroll
+    for (int i = 0; i < INSTR; ++i) {
+      const int chunk = (lane % CH) ^ chunk_swap<DP>(i * RPI + lane / CH);
+      if (on >> i & 1) copy16_to_lds(cache + off[i] + chunk * 8, to + i * 1024);
+    }
+  }
+};
 
 // Values of a tile that some of its rows do not see: a weight of zero leaves a
 // finite value out of a sum, but not NaN or an infinity.  Where rows of a tile
@@ -339,16 +392,12 @@ struct WaveTile {
     for (int t = 0; t < AHEAD; ++t) read_k(t);
     float16_t s[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-#pragma unroll
     for (int t = 0; t < KT; ++t) {
       if (t + AHEAD < KT) read_k(t + AHEAD);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t % (AHEAD + 1)][kb], q[t], s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t % (AHEAD + 1)][kb], q[t], t == 0 ? float16_t{} : s[kb], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
     // rows of V in the order of the score registers: weight j of slab u is
@@ -431,6 +480,157 @@ struct WaveTile {
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+  }
+
+  // -------------------------------------------------------------------------
+  // The same as a pipeline of blocks of 32 keys, for rows whose work the
+  // matrix cores bound: while the vector ALUs turn block b's scores into
+  // weights, the matrix cores compute the scores of block b + 1 and add the
+  // weighted values of block b - 1.  The two do not depend on each other, and
+  // one step is one MFMA (32 cycles), its share of the block's 16 scores per
+  // lane, and the LDS reads of an operand three steps ahead.
+  // -------------------------------------------------------------------------
+  static constexpr int N = DP / 16;  // products of a block with the keys, and with the values
+  static constexpr int OPS = 4;      // operands held: the current one and three ahead
+  u32x4 ops[OPS];
+
+  // Operand i of a block: key operand i, or value operand i - N.
+  __device__ __forceinline__ void read_op(uint32_t k_at, const uint32_t (&v_at)[2], int i) {
+    if (i < N) {
+      ops[i % OPS] = __builtin_bit_cast(u32x4, *(lds_half8)(uintptr_t)((k_at ^ (i % 8 * 32)) + i / 8 * 256));
+      return;
+    }
+    const int u = (i - N) / (DP / 32), d = (i - N) % (DP / 32);
+    short4_t part[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_short4)(uintptr_t)((v_at[j] ^ (d % 4 * 64)) + d / 4 * 256 + u * 16 * DP * 2));
+    ops[i % OPS] = __builtin_bit_cast(u32x4, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+
+  // This lane's first addresses in a block of 32 rows of keys and of values.
+  static __device__ __forceinline__ uint32_t key_lane(const uint16_t* keys) {
+    const int lane = threadIdx.x % kWave, l32 = lane % 32;
+    return lds_address(keys) + l32 * (DP * 2) + (lane / 32 ^ chunk_swap<DP>(l32)) * 16;
+  }
+  static __device__ __forceinline__ uint32_t value_lane(const uint16_t* values, int j) {
+    const int lane = threadIdx.x % kWave, x = (lane / 16 & 1) * 2 + (lane & 3) / 2;
+    const int row = j * 8 + lane / 32 * 4 + lane % 16 / 4;
+    return lds_address(values) + row * (DP * 2) + (x ^ chunk_swap<DP>(row)) * 16 + (lane & 1) * 8;
+  }
+
+  // Scores of a block alone.
+  __device__ __forceinline__ void scores(uint32_t k_at, float16_t& s) {
+    const uint32_t none[2] = {0, 0};
+#pragma unroll
+    for (int t = 0; t < OPS - 1; ++t) read_op(k_at, none, t);
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      if (t + OPS - 1 < N) read_op(k_at, none, t + OPS - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, ops[t % OPS]), q[t],
+                                                 t == 0 ? float16_t{} : s, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // Weights of scores alone.
+  __device__ __forceinline__ void weights(const float16_t& s, half8_t (&p)[2], float c) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) weight(s, p, e, c);
+  }
+  __device__ __forceinline__ void weight(const float16_t& s, half8_t (&p)[2], int e, float c) {
+    const float w = __builtin_amdgcn_exp2f(s[e] * c - mc);
+    l += w;
+    p[e / 8][e % 8] = static_cast<half_t>(w);
+  }
+
+  // Before a block's weights: its mask and the running maximum.  p: weights
+  // that have not met their values yet.
+  __device__ __forceinline__ void settle(float16_t& s, float top, half8_t (&p)[2], int key0, int begin, int end,
+                                         bool masked, float c) {
+    if (masked) {
+      const int h4 = threadIdx.x % kWave / 32 * 4, first = begin - key0 - h4, last = end - key0 - h4;
+      top = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = (e / 4) * 8 + e % 4;
+        s[e] = key < first || key >= last ? -INFINITY : s[e];
+        top = fmaxf(top, s[e]);
+      }
+    }
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+    const bool grown = (top - m) * c > 8.f;  // as in step()
+    if (__any(grown)) {
+      const float next_c = top * c;
+      const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= keep;
+      // these weights are now below 2^-8 of the largest: one more rounding of theirs is nothing
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[e / 8][e % 8] = static_cast<half_t>((float)p[e / 8][e % 8] * keep);
+      m = grown ? top : m;
+      mc = grown ? next_c : mc;
+    }
+  }
+
+  // One block: the weights `made` of its scores s, the scores `next` of the
+  // block at k_at, the values at v_at weighted with `p`, and next's largest score of
+  // this lane.  The operands of the first three steps are there; those of the
+  // block after this one are read if `more` (at k_more and v_more).
+  __device__ __forceinline__ float block(const float16_t& s, float16_t& next, const half8_t (&p)[2], half8_t (&made)[2],
+                                         uint32_t k_at, const uint32_t (&v_at)[2], bool more, uint32_t k_more, float c) {
+    float top = -INFINITY;
+    constexpr int STEPS = 2 * N;
+    float w[16];
+    u32x4 packed[2];
+    auto add = [&](int e) {
+      l += w[e];
+      asm volatile("" : "+v"(l));
+      if (e % 2 == 1) {
+        typedef _Float16 pair_t __attribute__((ext_vector_type(2)));
+        uint32_t pair = __builtin_bit_cast(uint32_t, pair_t{static_cast<half_t>(w[e - 1]), static_cast<half_t>(w[e])});
+        asm volatile("" : "+v"(pair));
+        packed[e / 8][e % 8 / 2] = pair;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int j = i + OPS - 1;
+      if (j < STEPS) read_op(k_at, v_at, j);
+      else if (more) read_op(k_more, v_at, j - STEPS);
+      __builtin_amdgcn_sched_barrier(0);
+      const half8_t op = __builtin_bit_cast(half8_t, ops[i % OPS]);
+      if (i < N) next = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, q[i < N ? i : 0], i == 0 ? float16_t{} : next, 0, 0, 0);
+      else {
+        const int u = (i - N) / (DP / 32), d = (i - N) % (DP / 32);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, p[u], o[d], 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 16 * i / STEPS; e < 16 * (i + 1) / STEPS; ++e) {
+        // computed here, not where it is used: the compiler would move it
+        // there (the empty asm statements); a weight is added up a step later,
+        // when the exponential is there
+        w[e] = __builtin_amdgcn_exp2f(s[e] * c - mc);
+        asm volatile("" : "+v"(w[e]));
+        if (e >= 1) add(e - 1);
+      }
+      if (i == STEPS - 3 || i == STEPS - 1) {
+#pragma unroll
+        for (int e = i == STEPS - 1 ? 8 : 0; e < (i == STEPS - 1 ? 16 : 8); ++e) top = fmaxf(top, next[e]);
+        asm volatile("" : "+v"(top));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    add(15);
+    made[0] = __builtin_bit_cast(half8_t, packed[0]);
+    made[1] = __builtin_bit_cast(half8_t, packed[1]);
+    return top;
   }
 
   // The maximum as partial results hold it, in powers of two.

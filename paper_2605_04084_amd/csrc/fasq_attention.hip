@@ -36,29 +36,6 @@ __device__ __forceinline__ int64_t lse_at(const AttentionArgs& a, const Request&
   return (int64_t)(r.q0 + row / a.G) * a.Hq + head * a.G + row % a.G;
 }
 
-// Copies rows (keys k0 + row, cut to [first, last]) of a cache head to LDS,
-// one wave's share of INSTR wave-wide copies of 64 16-byte chunks, from row
-// `row0` on.  `page`: the page of key k0 + row0 + lane (lanes below the rows
-// copied).
-template <int DP, int INSTR>
-__device__ __forceinline__ void copy_rows(const AttentionArgs& a, int64_t head_off, int page, int k0, int first, int last,
-                                          int row0, uint16_t* keys, uint16_t* values) {
-  constexpr int CH = DP / 8, RPI = kWave / CH;  // chunks of a row, rows of a copy
-  const int lane = threadIdx.x % kWave;
-  const int j = k0 + row0 + lane;
-  const int64_t own = key_offset(a, page, j < first ? first : j < last ? j : last) + head_off;
-#pragma unroll
-  for (int i = 0; i < INSTR; ++i) {
-    const int row = row0 + i * RPI + lane / CH;
-    const int chunk = (lane % CH) ^ chunk_swap<DP>(row);
-    const int64_t off = __shfl(own, i * RPI + lane / CH, kWave) + chunk * 8;
-    if (chunk * 8 < a.D) {
-      copy16_to_lds(a.ck + off, keys + (row0 + i * RPI) * DP);
-      copy16_to_lds(a.cv + off, values + (row0 + i * RPI) * DP);
-    }
-  }
-}
-
 // Chunks past D are zero and stay so.
 template <int DP>
 __device__ __forceinline__ void clear_lds(const AttentionArgs& a, uint16_t* at, int rows) {
@@ -81,6 +58,7 @@ __device__ __forceinline__ int64_t share_of(int64_t total, int parts, int least)
   return s <= least ? least : (s + STEP - 1) / STEP * STEP;
 }
 
+constexpr int kXcds = 8;
 constexpr int kFewShare = 128;   // keys a share has at least
 constexpr int kTileShare = 256;
 
@@ -91,7 +69,7 @@ constexpr int kTileShare = 256;
 // ---------------------------------------------------------------------------
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a) {
-  constexpr int ROWS = 32, STEP = NW * 32, INSTR = DP / 16, OS = DP + 4;
+  constexpr int ROWS = 32, STEP = NW * 32, OS = DP + 4, COPIES = 4 * RowCopy<DP>::INSTR;  // of a stage
   extern __shared__ uint8_t smem[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l32 = lane % 32, h = lane / 32;
@@ -101,6 +79,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
   float* jl = jm + NW * 32;                             // [NW][32]
   int* flag = reinterpret_cast<int*>(jl + NW * 32);     // [32], then [NW] of the waves
 
+  const RowCopy<DP> copy(a);
   const bool shared = a.part_o != nullptr;
   const int64_t head_len = head_length<ROWS, STEP>(a, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
@@ -149,9 +128,13 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
       const int j = k + l32;
       return k < hi ? page_of(a, pages, j < span.begin ? span.begin : j < hi ? j : hi - 1) : 0;
     };
-    auto issue = [&](int k, int page, int stage) {
-      copy_rows<DP, INSTR>(a, head_off, page, k, span.begin, hi - 1, 0, ring + stage * (2 * 32 * DP),
-                           ring + stage * (2 * 32 * DP) + 32 * DP);
+    auto issue = [&](int k, int page, int stage) {  // page: lane l's of key k + l % 32
+      const uint32_t to = lds_address(ring) + stage * (2 * 32 * DP * 2);
+      const int page1 = __shfl_down(page, 16, kWave);
+      copy.run(a, a.ck, head_off, page, k, span.begin, hi - 1, to);
+      copy.run(a, a.ck, head_off, page1, k + 16, span.begin, hi - 1, to + 16 * DP * 2);
+      copy.run(a, a.cv, head_off, page, k, span.begin, hi - 1, to + 32 * DP * 2);
+      copy.run(a, a.cv, head_off, page1, k + 16, span.begin, hi - 1, to + 48 * DP * 2);
     };
     int page = page_at(k0), stage = 0;
     if (k0 < hi) issue(k0, page, 0);
@@ -163,7 +146,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
         page = page_at(next + STEP);
         wait_lds();  // the other stage's readers are done
         issue(next, now, stage ^ 1);
-        wait_loads<2 * INSTR>();  // the copies of this stage
+        wait_loads<COPIES>();  // the copies of this stage
       } else {
         wait_loads<0>();
       }
@@ -246,17 +229,22 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
 // ---------------------------------------------------------------------------
 template <int DP>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(AttentionArgs a) {
-  constexpr int ROWS = 128, STEP = 64, INSTR = DP / 32;
+  constexpr int ROWS = 128, STEP = 64;
   extern __shared__ uint8_t smem[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l32 = lane % 32, h = lane / 32;
   uint16_t* ring = reinterpret_cast<uint16_t*>(smem);
   int* flag = reinterpret_cast<int*>(smem + 512 * DP);  // a value of a mixed tile was not finite
 
+  const RowCopy<DP> copy(a);
   const bool shared = a.part_o != nullptr;
   const int64_t head_len = head_length<ROWS, STEP>(a, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   if (shared) {
+    // Workgroups go to the XCDs in turn, and each XCD has its own L2: its
+    // shares lie side by side, so that they read the keys of few heads (2048
+    // tokens after 6144, 8 heads: one head an XCD; 332 us without).
+    if (a.parts % kXcds == 0) w = w % kXcds * (a.parts / kXcds) + w / kXcds;
     share = share_of<STEP>(head_len * a.Hkv, a.parts, kTileShare);
     pos = w * share;
     pos_end = pos + share < head_len * a.Hkv ? pos + share : head_len * a.Hkv;
@@ -305,36 +293,80 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 
     clear_lds<DP>(a, ring + wave * (64 * DP), 64);
     if (a.D != DP) __syncthreads();
-    WaveTile<DP, 2> t;
+    WaveTile<DP, 1> t;
     t.clear();
     t.load_q(a, p.r, head, row0 + l32, alive);
     auto page_at = [&](int k) {
       const int j = k + wave * 16 + lane % 16;
       return k < hi ? page_of(a, pages, j < span.begin ? span.begin : j < hi ? j : hi - 1) : 0;
     };
-    auto issue = [&](int k, int page, int stage) {
-      copy_rows<DP, INSTR>(a, head_off, page, k, span.begin, hi - 1, wave * 16, ring + stage * (2 * 64 * DP),
-                           ring + stage * (2 * 64 * DP) + 64 * DP);
+    // Keys and values have two stages each.  Keys run a tile ahead: while the
+    // pipeline takes the scores of tile i + 1 it weights the values of tile i.
+    const uint32_t rows_at = lds_address(ring) + wave * (16 * DP * 2);
+    uint16_t* vring = ring + 2 * 64 * DP;
+    auto copy_keys = [&](int k, int page, int stage) {
+      copy.run(a, a.ck, head_off, page, k + wave * 16, span.begin, hi - 1, rows_at + stage * (64 * DP * 2));
     };
-    int page = page_at(lo), stage = 0;
-    if (lo < hi) issue(lo, page, 0);
-    page = page_at(lo + STEP);
-    for (int k0 = lo; k0 < hi; k0 += STEP, stage ^= 1) {
-      wait_lds();
-      wait_loads<0>();  // this wave's copies of this stage
-      if (mixed && (k0 < most_begin || k0 + STEP > least_end)) {
-        if (cut_to_finite<DP, 16>(ring + stage * (2 * 64 * DP) + 64 * DP + wave * 16 * DP)) *flag = 1;
+    auto copy_values = [&](int k, int page, int stage) {
+      copy.run(a, a.cv, head_off, page, k + wave * 16, span.begin, hi - 1, rows_at + (2 + stage) * (64 * DP * 2));
+    };
+    // values that some rows do not see are cut to finite ones by the wave that copied them
+    auto cut_values = [&](int k, int stage) {
+      if (mixed && (k < most_begin || k + STEP > least_end)) {
+        if (cut_to_finite<DP, 16>(vring + stage * (64 * DP) + wave * 16 * DP)) *flag = 1;
+      }
+    };
+    auto masked = [&](int k) { return k < all.begin || k + 32 > all.end; };
+    if (lo < hi) {
+      int page = page_at(lo), page1 = page_at(lo + STEP);
+      copy_keys(lo, page, 0);
+      copy_keys(lo + STEP, page1, 1);  // behind the end: the last key, masked
+      copy_values(lo, page, 0);
+      page = page1;
+      page1 = page_at(lo + 2 * STEP);
+      wait_loads<0>();
+      barrier_only();
+      float16_t s0, s1;
+      half8_t p0[2], p1[2] = {};
+      t.scores(WaveTile<DP, 1>::key_lane(ring), s0);
+      t.scores(WaveTile<DP, 1>::key_lane(ring + 32 * DP), s1);
+      float top = s0[0], top1 = s1[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) {
+        top = fmaxf(top, s0[e]);
+        top1 = fmaxf(top1, s1[e]);
+      }
+      t.settle(s0, top, p1, lo, mine.begin, mine.end, masked(lo), a.c);
+      t.weights(s0, p0, a.c);
+      t.settle(s1, top1, p0, lo + 32, mine.begin, mine.end, masked(lo + 32), a.c);
+      int stage = 0;
+      for (int k0 = lo; k0 < hi; k0 += STEP, stage ^= 1) {
+        // here: values of tile k0 in `stage`, keys of the next in the other
+        // one; p0, s1: weights and scores of the tile's two blocks
         wait_lds();
+        wait_loads<0>();  // this wave's copies
+        cut_values(k0, stage);
+        wait_lds();
+        barrier_only();   // everyone's; nobody reads what is overwritten now
+        copy_keys(k0 + 2 * STEP, page1, stage);
+        copy_values(k0 + STEP, page, stage ^ 1);
+        page = page1;
+        page1 = page_at(k0 + 3 * STEP);
+        const uint32_t kn = WaveTile<DP, 1>::key_lane(ring + (stage ^ 1) * (64 * DP));
+        uint32_t v[2], v32[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          v[j] = WaveTile<DP, 1>::value_lane(vring + stage * (64 * DP), j);
+          v32[j] = v[j] + 32 * DP * 2;
+        }
+#pragma unroll
+        for (int i = 0; i < WaveTile<DP, 1>::OPS - 1; ++i) t.read_op(kn, v, i);
+        top = t.block(s1, s0, p0, p1, kn, v, true, kn + 32 * DP * 2, a.c);
+        t.settle(s0, top, p1, k0 + STEP, mine.begin, mine.end, masked(k0 + STEP), a.c);
+        top = t.block(s0, s1, p1, p0, kn + 32 * DP * 2, v32, false, 0, a.c);
+        t.settle(s1, top, p0, k0 + STEP + 32, mine.begin, mine.end, masked(k0 + STEP + 32), a.c);
       }
-      barrier_only();   // everyone's; nobody reads the other stage any more
-      if (k0 + STEP < hi) {
-        issue(k0 + STEP, page, stage ^ 1);
-        page = page_at(k0 + 2 * STEP);
-      }
-      if (k0 < any.end && k0 + STEP > any.begin) {
-        const uint16_t* keys = ring + stage * (2 * 64 * DP);
-        t.step(keys, keys + 64 * DP, k0, mine.begin, mine.end, k0 < all.begin || k0 + STEP > all.end, a.c);
-      }
+      wait_loads<0>();  // copies behind the end
     }
     const float l = t.total();
     const bool cut = shared && (t0 < pos || seg_end < t1);
@@ -554,6 +586,7 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
   };
   a.q_vec = aligned(p.q, 16);
   a.out_vec = aligned(p.out, 8);
+  a.whole_units = p.cache.page_size % 16 == 0 && p.cache.slot_stride < int64_t(1) << 25;
   a.lse = p.lse;
   if (pl.split && p.workspace != nullptr && p.workspace_bytes >= pl.bytes) {
     a.parts = pl.parts;
