@@ -262,8 +262,9 @@ __device__ __forceinline__ void copy16_to_lds(const uint16_t* base, uint32_t off
                : "memory");
 }
 
-// Copies of 16 rows of a cache head to LDS by one wave, INSTR copies of RPI rows.
-template <int DP>
+// Copies of 16 rows of a cache head to LDS by one wave, INSTR copies of RPI
+// rows.  FULL: D is DP.
+template <int DP, bool FULL>
 struct RowCopy {
   static constexpr int CH = DP / 8, RPI = kWave / CH, INSTR = 16 / RPI;
   uint32_t offset[INSTR];  // of this lane, where the 16 rows lie in one page
@@ -280,18 +281,23 @@ struct RowCopy {
     }
   }
 
-  // Keys k .. k + 15 (k a multiple of 16), those outside [first, last] in the
-  // place of the nearest inside.  `page`: lane l's page of key k + l % 16 as cut
-  // (page_of).  to: the LDS address of the first row.
-  __device__ __forceinline__ void run(const AttentionArgs& a, const uint16_t* cache, int64_t head_off, int page, int k,
-                                      int first, int last, uint32_t to) const {
-    if (a.whole_units && k >= first && k + 15 <= last) {  // one page, every key there
-      const uint16_t* base = cache + uniform(key_offset(a, uniform(page), k) + head_off);
-#pragma unroll
-      for (int i = 0; i < INSTR; ++i)
-        if (a.D == DP || (on >> i & 1)) copy16_to_lds(base, offset[i], to + i * 1024);
-      return;
-    }
+  // Whether keys k .. k + 15 (k a multiple of 16) lie in one page and in
+  // [first, last], so that they can be copied from one base.
+  __device__ __forceinline__ static bool whole(const AttentionArgs& a, int k, int first, int last) {
+    return a.whole_units && k >= first && k + 15 <= last;
+  }
+  // Their offset in the cache: `page` is their page, in any lane.
+  __device__ __forceinline__ static int64_t whole_offset(const AttentionArgs& a, int64_t head_off, int page, int k) {
+    return uniform(key_offset(a, uniform(page), k) + head_off);
+  }
+  // Copy i of them.  to: the LDS address of the first row.
+  __device__ __forceinline__ void one(const uint16_t* base, int i, uint32_t to) const {
+    if (FULL || (on >> i & 1)) copy16_to_lds(base, offset[i], to + i * 1024);
+  }
+  // Any keys k .. k + 15, those outside [first, last] in the place of the
+  // nearest inside.  `page`: lane l's page of key k + l % 16 as cut (page_of).
+  __device__ __forceinline__ void each(const AttentionArgs& a, const uint16_t* cache, int64_t head_off, int page, int k,
+                                       int first, int last, uint32_t to) const {
     const int lane = threadIdx.x % kWave, j = k + lane % 16;
     const int64_t own = key_offset(a, page, j < first ? first : j < last ? j : last) + head_off;
     int64_t off[INSTR];
@@ -300,7 +306,17 @@ struct RowCopy {
 #pragma unroll
     for (int i = 0; i < INSTR; ++i) {
       const int chunk = (lane % CH) ^ chunk_swap<DP>(i * RPI + lane / CH);
-      if (on >> i & 1) copy16_to_lds(cache + off[i] + chunk * 8, to + i * 1024);
+      if (FULL || (on >> i & 1)) copy16_to_lds(cache + off[i] + chunk * 8, to + i * 1024);
+    }
+  }
+  __device__ __forceinline__ void run(const AttentionArgs& a, const uint16_t* cache, int64_t head_off, int page, int k,
+                                      int first, int last, uint32_t to) const {
+    if (whole(a, k, first, last)) {
+      const uint16_t* from = cache + whole_offset(a, head_off, page, k);
+#pragma unroll
+      for (int i = 0; i < INSTR; ++i) one(from, i, to);
+    } else {
+      each(a, cache, head_off, page, k, first, last, to);
     }
   }
 };
@@ -546,10 +562,18 @@ struct WaveTile {
     p[e / 8][e % 8] = static_cast<half_t>(w);
   }
 
-  // Before a block's weights: its mask and the running maximum.  p: weights
-  // that have not met their values yet.
-  __device__ __forceinline__ void settle(float16_t& s, float top, half8_t (&p)[2], int key0, int begin, int end,
-                                         bool masked, float c) {
+  // The larger of this lane's value and the other's of its row.
+  static __device__ __forceinline__ float row_max(float top) {
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  }
+
+  // Before a block's weights: its mask and the running maximum.  top, over:
+  // the row's largest score, and by how much it passes the maximum, in powers
+  // of two (where nothing is masked).  p: weights that have not met their
+  // values yet.
+  __device__ __forceinline__ void settle(float16_t& s, float top, float over, half8_t (&p)[2], int key0, int begin,
+                                         int end, bool masked, float c) {
     if (masked) {
       const int h4 = threadIdx.x % kWave / 32 * 4, first = begin - key0 - h4, last = end - key0 - h4;
       top = -INFINITY;
@@ -559,10 +583,10 @@ struct WaveTile {
         s[e] = key < first || key >= last ? -INFINITY : s[e];
         top = fmaxf(top, s[e]);
       }
+      top = row_max(top);
+      over = (top - m) * c;
     }
-    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-    top = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
-    const bool grown = (top - m) * c > 8.f;  // as in step()
+    const bool grown = over > 8.f;  // as in step()
     if (__any(grown)) {
       const float next_c = top * c;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
@@ -580,12 +604,14 @@ struct WaveTile {
   }
 
   // One block: the weights `made` of its scores s, the scores `next` of the
-  // block at k_at, the values at v_at weighted with `p`, and next's largest score of
-  // this lane.  The operands of the first three steps are there; those of the
-  // block after this one are read if `more` (at k_more and v_more).
-  __device__ __forceinline__ float block(const float16_t& s, float16_t& next, const half8_t (&p)[2], half8_t (&made)[2],
-                                         uint32_t k_at, const uint32_t (&v_at)[2], bool more, uint32_t k_more, float c) {
-    float top = -INFINITY;
+  // block at k_at, the values at v_at weighted with `p`, and next's largest score
+  // of the row (top) and by how much it passes the maximum (over).  The operands
+  // of the first three steps are there; those of the block after this one are
+  // read if `more` (at k_more).  at_step(i): what else step i issues.
+  template <typename F>
+  __device__ __forceinline__ void block(const float16_t& s, float16_t& next, const half8_t (&p)[2], half8_t (&made)[2],
+                                        uint32_t k_at, const uint32_t (&v_at)[2], bool more, uint32_t k_more, float c,
+                                        float& top, float& over, F at_step) {
     constexpr int STEPS = 2 * N;
     float w[16];
     u32x4 packed[2];
@@ -620,17 +646,23 @@ struct WaveTile {
         asm volatile("" : "+v"(w[e]));
         if (e >= 1) add(e - 1);
       }
-      if (i == STEPS - 3 || i == STEPS - 1) {
+      // the maximum, from the second step after the scores are complete on
+      if (i == N + 1 || i == N + 2) {
 #pragma unroll
-        for (int e = i == STEPS - 1 ? 8 : 0; e < (i == STEPS - 1 ? 16 : 8); ++e) top = fmaxf(top, next[e]);
+        for (int e = i == N + 1 ? 0 : 8; e < (i == N + 1 ? 8 : 16); ++e) top = e == 0 ? next[0] : fmaxf(top, next[e]);
         asm volatile("" : "+v"(top));
       }
+      if (i == N + 3) {
+        top = row_max(top);
+        over = (top - m) * c;
+        asm volatile("" : "+v"(top), "+v"(over));
+      }
+      at_step(i);
       __builtin_amdgcn_sched_barrier(0);
     }
     add(15);
     made[0] = __builtin_bit_cast(half8_t, packed[0]);
     made[1] = __builtin_bit_cast(half8_t, packed[1]);
-    return top;
   }
 
   // The maximum as partial results hold it, in powers of two.

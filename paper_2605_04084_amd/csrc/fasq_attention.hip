@@ -38,8 +38,7 @@ __device__ __forceinline__ int64_t lse_at(const AttentionArgs& a, const Request&
 
 // Chunks past D are zero and stay so.
 template <int DP>
-__device__ __forceinline__ void clear_lds(const AttentionArgs& a, uint16_t* at, int rows) {
-  if (a.D == DP) return;
+__device__ __forceinline__ void clear_lds(uint16_t* at, int rows) {
   const u32x4 zero = {0, 0, 0, 0};
   for (int i = threadIdx.x % kWave; i < rows * DP / 8; i += kWave) reinterpret_cast<u32x4*>(at)[i] = zero;
   wait_lds();  // before copies that land beside them
@@ -67,9 +66,9 @@ constexpr int kTileShare = 256;
 // LDS, so that no wave waits for another until the end, where their results
 // are joined in wave order.
 // ---------------------------------------------------------------------------
-template <int DP, int NW>
+template <int DP, int NW, bool FULL>
 __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a) {
-  constexpr int ROWS = 32, STEP = NW * 32, OS = DP + 4, COPIES = 4 * RowCopy<DP>::INSTR;  // of a stage
+  constexpr int ROWS = 32, STEP = NW * 32, OS = DP + 4, COPIES = 4 * RowCopy<DP, FULL>::INSTR;  // of a stage
   extern __shared__ uint8_t smem[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l32 = lane % 32, h = lane / 32;
@@ -79,7 +78,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
   float* jl = jm + NW * 32;                             // [NW][32]
   int* flag = reinterpret_cast<int*>(jl + NW * 32);     // [32], then [NW] of the waves
 
-  const RowCopy<DP> copy(a);
+  const RowCopy<DP, FULL> copy(a);
   const bool shared = a.part_o != nullptr;
   const int64_t head_len = head_length<ROWS, STEP>(a, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
@@ -119,7 +118,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
     const int32_t* pages = a.pages + p.b * a.page_row_stride;
     const int64_t head_off = head * a.head_stride;
 
-    clear_lds<DP>(a, ring, 2 * 2 * 32);
+    if constexpr (!FULL) clear_lds<DP>(ring, 2 * 2 * 32);
     WaveTile<DP, 1> t;
     t.clear();
     t.load_q(a, p.r, head, row0 + l32, alive);
@@ -227,7 +226,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
 // ---------------------------------------------------------------------------
 // 128 rows: four waves of 32 rows over shared tiles of 64 keys, two stages.
 // ---------------------------------------------------------------------------
-template <int DP>
+template <int DP, bool FULL>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(AttentionArgs a) {
   constexpr int ROWS = 128, STEP = 64;
   extern __shared__ uint8_t smem[];
@@ -236,7 +235,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
   uint16_t* ring = reinterpret_cast<uint16_t*>(smem);
   int* flag = reinterpret_cast<int*>(smem + 512 * DP);  // a value of a mixed tile was not finite
 
-  const RowCopy<DP> copy(a);
+  const RowCopy<DP, FULL> copy(a);
   const bool shared = a.part_o != nullptr;
   const int64_t head_len = head_length<ROWS, STEP>(a, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
@@ -291,8 +290,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     const int32_t* pages = a.pages + p.b * a.page_row_stride;
     const int64_t head_off = head * a.head_stride;
 
-    clear_lds<DP>(a, ring + wave * (64 * DP), 64);
-    if (a.D != DP) __syncthreads();
+    if constexpr (!FULL) {
+      clear_lds<DP>(ring + wave * (64 * DP), 64);
+      __syncthreads();
+    }
     WaveTile<DP, 1> t;
     t.clear();
     t.load_q(a, p.r, head, row0 + l32, alive);
@@ -318,12 +319,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     };
     auto masked = [&](int k) { return k < all.begin || k + 32 > all.end; };
     if (lo < hi) {
-      int page = page_at(lo), page1 = page_at(lo + STEP);
-      copy_keys(lo, page, 0);
-      copy_keys(lo + STEP, page1, 1);  // behind the end: the last key, masked
-      copy_values(lo, page, 0);
-      page = page1;
-      page1 = page_at(lo + 2 * STEP);
+      int page[3] = {page_at(lo), page_at(lo + STEP), 0};
+      copy_keys(lo, page[0], 0);
+      copy_keys(lo + STEP, page[1], 1);  // behind the end: any key, masked
+      copy_values(lo, page[0], 0);
+      // offsets of the units that the next tile's copies bring: values of tile
+      // 1, keys of tile 2; pages of this one and the next two
+      int page_v = page[1];
+      int64_t off_v = copy.whole_offset(a, head_off, page_v, lo + STEP + wave * 16);
+      page[0] = page_at(lo + 2 * STEP);
+      page[1] = page_at(lo + 3 * STEP);
+      int64_t off_k = copy.whole_offset(a, head_off, page[0], lo + 2 * STEP + wave * 16);
       wait_loads<0>();
       barrier_only();
       float16_t s0, s1;
@@ -336,9 +342,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
         top = fmaxf(top, s0[e]);
         top1 = fmaxf(top1, s1[e]);
       }
-      t.settle(s0, top, p1, lo, mine.begin, mine.end, masked(lo), a.c);
+      top = t.row_max(top);
+      top1 = t.row_max(top1);
+      t.settle(s0, top, (top - t.m) * a.c, p1, lo, mine.begin, mine.end, masked(lo), a.c);
       t.weights(s0, p0, a.c);
-      t.settle(s1, top1, p0, lo + 32, mine.begin, mine.end, masked(lo + 32), a.c);
+      t.settle(s1, top1, (top1 - t.m) * a.c, p0, lo + 32, mine.begin, mine.end, masked(lo + 32), a.c);
       int stage = 0;
       for (int k0 = lo; k0 < hi; k0 += STEP, stage ^= 1) {
         // here: values of tile k0 in `stage`, keys of the next in the other
@@ -348,10 +356,31 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
         cut_values(k0, stage);
         wait_lds();
         barrier_only();   // everyone's; nobody reads what is overwritten now
-        copy_keys(k0 + 2 * STEP, page1, stage);
-        copy_values(k0 + STEP, page, stage ^ 1);
-        page = page1;
-        page1 = page_at(k0 + 3 * STEP);
+        // The next copies: one every third step below, since memory takes a
+        // copy in 16 cycles and the eight waves of a compute unit would stand
+        // in line for it here (1784 of 5370 cycles a tile); all at once where
+        // keys lie in several pages or past the end.
+        const int kk = k0 + 2 * STEP + wave * 16;
+        const bool spread = copy.whole(a, kk, span.begin, hi - 1);  // then the values' unit is whole too
+        const uint16_t *from_k = a.ck + off_k, *from_v = a.cv + off_v;
+        if (!spread) {
+          copy_keys(k0 + 2 * STEP, page[0], stage);
+          copy_values(k0 + STEP, page_v, stage ^ 1);
+        }
+        const uint32_t to_k = rows_at + stage * (64 * DP * 2), to_v = rows_at + (2 + (stage ^ 1)) * (64 * DP * 2);
+        page[2] = page_at(k0 + 4 * STEP);
+        auto at_step = [&](int i) {
+          constexpr int C = RowCopy<DP, FULL>::INSTR;
+          const int n = i / 3;
+          if (i == 6 * C + 1) {  // the next tile's offsets; its page came a tile ago
+            off_v = off_k;
+            off_k = copy.whole_offset(a, head_off, page[1], kk + STEP);
+            asm volatile("" : "+s"(off_k));
+          }
+          if (i % 3 != 0 || n >= 2 * C || !spread) return;
+          if (n < C) copy.one(from_k, n, to_k);
+          else copy.one(from_v, n - C, to_v);
+        };
         const uint32_t kn = WaveTile<DP, 1>::key_lane(ring + (stage ^ 1) * (64 * DP));
         uint32_t v[2], v32[2];
 #pragma unroll
@@ -361,10 +390,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
         }
 #pragma unroll
         for (int i = 0; i < WaveTile<DP, 1>::OPS - 1; ++i) t.read_op(kn, v, i);
-        top = t.block(s1, s0, p0, p1, kn, v, true, kn + 32 * DP * 2, a.c);
-        t.settle(s0, top, p1, k0 + STEP, mine.begin, mine.end, masked(k0 + STEP), a.c);
-        top = t.block(s0, s1, p1, p0, kn + 32 * DP * 2, v32, false, 0, a.c);
-        t.settle(s1, top, p0, k0 + STEP + 32, mine.begin, mine.end, masked(k0 + STEP + 32), a.c);
+        float over = 0.f;
+        t.block(s1, s0, p0, p1, kn, v, true, kn + 32 * DP * 2, a.c, top, over, at_step);
+        t.settle(s0, top, over, p1, k0 + STEP, mine.begin, mine.end, masked(k0 + STEP), a.c);
+        t.block(s0, s1, p1, p0, kn + 32 * DP * 2, v32, false, 0, a.c, top, over,
+                [&](int i) { at_step(i + DP / 8); });
+        t.settle(s1, top, over, p0, k0 + STEP + 32, mine.begin, mine.end, masked(k0 + STEP + 32), a.c);
+        page_v = page[0];
+        page[0] = page[1];
+        page[1] = page[2];
       }
       wait_loads<0>();  // copies behind the end
     }
@@ -524,21 +558,21 @@ AttentionPlan plan_attention(int64_t T, int64_t B, int Hq, int Hkv, int D, const
   return p;
 }
 
-template <int DP>
+template <int DP, bool FULL>
 hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipStream_t stream) {
   constexpr int NW = DP == 256 ? 2 : 4;
   const bool shared = a.part_o != nullptr;
   const int64_t blocks = shared ? pl.parts : pl.tiles * a.Hkv;
   hipError_t e;
   if (pl.few) {
-    if ((e = prepare_kernel(k_attention_few<DP, NW>)) != hipSuccess) return e;
-    e = launch_kernel(k_attention_few<DP, NW>, dim3((unsigned)blocks), dim3(NW * kWave), NW * 256 * DP, stream, a);
+    if ((e = prepare_kernel(k_attention_few<DP, NW, FULL>)) != hipSuccess) return e;
+    e = launch_kernel(k_attention_few<DP, NW, FULL>, dim3((unsigned)blocks), dim3(NW * kWave), NW * 256 * DP, stream, a);
     if (e != hipSuccess || !shared) return e;
     return launch_kernel(k_attention_join<DP, 32, NW * 32, kFewShare, 1>, dim3((unsigned)blocks - 1), dim3(256), 0,
                          stream, a);
   }
-  if ((e = prepare_kernel(k_attention_tile<DP>)) != hipSuccess) return e;
-  e = launch_kernel(k_attention_tile<DP>, dim3((unsigned)blocks), dim3(256), 512 * DP + 16, stream, a);
+  if ((e = prepare_kernel(k_attention_tile<DP, FULL>)) != hipSuccess) return e;
+  e = launch_kernel(k_attention_tile<DP, FULL>, dim3((unsigned)blocks), dim3(256), 512 * DP + 16, stream, a);
   if (e != hipSuccess || !shared) return e;
   return launch_kernel(k_attention_join<DP, 128, 64, kTileShare, 8>, dim3((unsigned)blocks - 1, 8), dim3(256), 0, stream,
                        a);
@@ -593,10 +627,11 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
     a.part_o = static_cast<float*>(p.workspace);
     a.part_ml = a.part_o + int64_t(2) * pl.parts * pl.rows * pl.DP;
   }
+  const bool full = p.D == pl.DP;
   switch (pl.DP) {
-    case 64: return launch_planned<64>(pl, a, stream);
-    case 128: return launch_planned<128>(pl, a, stream);
-    default: return launch_planned<256>(pl, a, stream);
+    case 64: return full ? launch_planned<64, true>(pl, a, stream) : launch_planned<64, false>(pl, a, stream);
+    case 128: return full ? launch_planned<128, true>(pl, a, stream) : launch_planned<128, false>(pl, a, stream);
+    default: return full ? launch_planned<256, true>(pl, a, stream) : launch_planned<256, false>(pl, a, stream);
   }
 }
 
