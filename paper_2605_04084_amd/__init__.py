@@ -14,6 +14,7 @@ weights by k-means.
 
 from __future__ import annotations
 
+import array
 import ctypes
 import math
 import os
@@ -212,8 +213,8 @@ def lib() -> ctypes.CDLL:
         L.fasq_paged_attention_workspace_bytes.argtypes = [_c_i64, _c_i64, _c_int, _c_int, _c_int]
         L.fasq_residual_norm.argtypes = [_c_vp, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, ctypes.c_float, _c_vp,
                                          ctypes.c_float, _c_vp, _c_vp, _c_vp]
-        L.fasq_lora_batched.argtypes = [_c_vp, _c_i64, _c_i64, _c_vp, _c_i64, _c_int, _c_vp, _c_int, _pi64, _pp, _pp,
-                                        _pp, _pp, _c_vp, _c_i64, _c_vp]
+        L.fasq_lora_batched.argtypes = [_c_vp, _c_i64, _c_i64, _c_vp, _c_i64, _c_int, _c_vp, _c_int, _c_vp, _c_vp,
+                                        _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]
         L.fasq_lora_workspace_bytes.argtypes = [_c_i64, _c_i64, _c_int, _c_int]
         for name in ("fasq_rope_table", "fasq_rope_append", "fasq_paged_attention", "fasq_residual_norm",
                      "fasq_lora_batched"):
@@ -590,6 +591,10 @@ def pq_gemm_ex(x, idx, idx_bits: int, d: int, codebook, out=None, workspace=None
 # Between the projections: rotary positions, attention, norms, adapters
 # ---------------------------------------------------------------------------
 
+# As above, most of what a small call costs is its host side (a norm of one row:
+# 2.5 us on the GPU), so a tensor is looked at in one expression, and the
+# functions that name what is wrong run only where it fails.
+
 def _require_rows(t, name, dtype, ndim):
     """As ``_require``, but only the last dimension has to be contiguous."""
     torch = _torch()
@@ -611,20 +616,60 @@ def _same_device(device, *tensors):
             raise ValueError("all tensors must be on one device")
 
 
+def _check_tensor(t, name, dtype, shape, device):
+    """A contiguous tensor of that type and shape on that device."""
+    if not (isinstance(t, _torch().Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == device
+            and t.is_contiguous()):
+        _require(t, name, dtype, len(shape))
+        if t.shape != shape:
+            raise ValueError(f"{name} must be [{' x '.join(map(str, shape))}], got {list(t.shape)}")
+        _same_device(device, t)
+
+
+def _check_rows(t, name, dtype, shape, device):
+    """The same, with any strides but the last."""
+    if not (isinstance(t, _torch().Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == device
+            and (t.stride(-1) == 1 or shape[-1] == 1)):
+        _require_rows(t, name, dtype, len(shape))
+        if t.shape != shape:
+            raise ValueError(f"{name} must be [{' x '.join(map(str, shape))}], got {list(t.shape)}")
+        _same_device(device, t)
+
+
 def _ptr(t):
     return 0 if t is None else t.data_ptr()
 
 
-def _kv_cache(k_cache, v_cache):
+def _kv_cache(k_cache, v_cache, device, Hkv=None, D=None):
     """The structure of two caches [pages x page_size x heads x D] (any strides but the last)."""
     torch = _torch()
     _require_rows(k_cache, "k_cache", torch.float16, 4)
-    _require_rows(v_cache, "v_cache", torch.float16, 4)
-    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
-        raise ValueError("k_cache and v_cache must have the same shape and strides")
-    pages, page_size, _, _ = k_cache.shape
-    sp, ss, sh, _ = k_cache.stride()
-    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size, sp, ss, sh)
+    shape, strides = k_cache.shape, k_cache.stride()
+    pages, page_size, heads, d = shape
+    if (Hkv is not None and heads != Hkv) or (D is not None and d != D):
+        raise ValueError("the caches must be [pages x page_size x Hkv x D]")
+    if not (isinstance(v_cache, torch.Tensor) and v_cache.dtype is torch.float16 and v_cache.shape == shape
+            and v_cache.stride() == strides and v_cache.get_device() == device):
+        _require_rows(v_cache, "v_cache", torch.float16, 4)
+        if v_cache.shape != shape or v_cache.stride() != strides:
+            raise ValueError("k_cache and v_cache must have the same shape and strides")
+        _same_device(device, v_cache)
+    if k_cache.get_device() != device:
+        _same_device(device, k_cache)
+    return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size, strides[0], strides[1], strides[2])
+
+
+def _workspace(workspace, need, device):
+    """The workspace to use and its bytes: the caller's, or a new one."""
+    if workspace is None:
+        if need <= 0:
+            return None, 0
+        torch = _torch()
+        return torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", device)), need
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
+    _same_device(device, workspace)
+    return workspace, workspace.numel() * workspace.element_size()
 
 
 def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
@@ -704,62 +749,52 @@ def rope_append(q, k, v, table, positions, slots, k_cache, v_cache, interleaved:
     ``slots`` and the caches).  ``table`` None: no rotation.  See
     ``fasq_rope_append``."""
     torch = _torch()
+    f16, i32 = torch.float16, torch.int32
     some = q if q is not None else k
     if some is None:
         raise ValueError("q or k must be given")
     if (k is None) != (v is None):
         raise ValueError("k and v are given together or not at all")
-    _require_rows(some, "q" if q is not None else "k", torch.float16, 3)
-    T, _, D = some.shape
+    _require_rows(some, "q" if q is not None else "k", f16, 3)
+    T, Hq, D = some.shape
     device = some.get_device()
-    Hq = Hkv = rot = rows = 0
+    Hkv = rot = rows = kp = vp = sp = 0
     qs = qos = ks = vs = (0, 0)
     cache = None
     if q is not None:
-        Hq = q.shape[1]
         if out is None:
-            out = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device)
+            out = q.new_empty((T, Hq, D))
         else:
-            _require_rows(out, "out", torch.float16, 3)
-            if out.shape != q.shape:
-                raise ValueError("out must have the shape of q")
+            _check_rows(out, "out", f16, q.shape, device)
         qs, qos = q.stride(), out.stride()
-    elif out is not None:
-        raise ValueError("out needs q")
+    else:
+        Hq = 0
+        if out is not None:
+            raise ValueError("out needs q")
     if k is not None:
-        _require_rows(k, "k", torch.float16, 3)
-        _require_rows(v, "v", torch.float16, 3)
+        _require_rows(k, "k", f16, 3)
         Hkv = k.shape[1]
-        if k.shape != v.shape or k.shape[0] != T or k.shape[2] != D:
-            raise ValueError("k and v must be [T x Hkv x D]")
-        cache = _kv_cache(k_cache, v_cache)
-        if k_cache.shape[2] != Hkv or k_cache.shape[3] != D:
-            raise ValueError("the caches must be [pages x page_size x Hkv x D]")
-        _require(slots, "slots", torch.int32, 1)
-        if slots.shape[0] != T:
-            raise ValueError("slots must be [T]")
-        ks, vs = k.stride(), v.stride()
-        _same_device(device, k, v, k_cache, v_cache, slots)
+        _check_rows(k, "k", f16, (T, Hkv, D), device)
+        _check_rows(v, "v", f16, (T, Hkv, D), device)
+        cache = _kv_cache(k_cache, v_cache, device, Hkv, D)
+        _check_tensor(slots, "slots", i32, (T,), device)
+        ks, vs, kp, vp, sp = k.stride(), v.stride(), k.data_ptr(), v.data_ptr(), slots.data_ptr()
     if table is not None:
         _require(table, "table", torch.float32, 3)
-        _require(positions, "positions", torch.int32, 1)
         rows, half, two = table.shape
         rot = 2 * half
         if two != 2 or rot > D:
             raise ValueError("table must be [positions x rot / 2 x 2] with rot <= D")
-        if positions.shape[0] != T:
-            raise ValueError("positions must be [T]")
-        _same_device(device, table, positions)
-    for w, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-        if w is not None:
-            _require(w, name, torch.float16, 1)
-            if w.shape[0] != D:
-                raise ValueError(f"{name} must be [D]")
-    _same_device(device, out, q_norm, k_norm)
-    _check(_on_device(device, lib().fasq_rope_append, _ptr(q), qs[0], qs[1], Hq, _ptr(out), qos[0], qos[1], _ptr(k),
-                      ks[0], ks[1], _ptr(v), vs[0], vs[1], Hkv, T, D, _ptr(table), rows, rot, int(interleaved),
-                      _ptr(positions) if table is not None else 0, _ptr(slots) if k is not None else 0, _ptr(q_norm),
-                      _ptr(k_norm), eps, cache))
+        if table.get_device() != device:
+            _same_device(device, table)
+        _check_tensor(positions, "positions", i32, (T,), device)
+    if q_norm is not None:
+        _check_tensor(q_norm, "q_norm", f16, (D,), device)
+    if k_norm is not None:
+        _check_tensor(k_norm, "k_norm", f16, (D,), device)
+    _check(_on_device(device, lib().fasq_rope_append, _ptr(q), qs[0], qs[1], Hq, _ptr(out), qos[0], qos[1], kp, ks[0],
+                      ks[1], vp, vs[0], vs[1], Hkv, T, D, _ptr(table), rows, rot, interleaved,
+                      positions.data_ptr() if table is not None else 0, sp, _ptr(q_norm), _ptr(k_norm), eps, cache))
     return out
 
 
@@ -777,39 +812,39 @@ def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional
     of the softmax sums [T x Hq].  ``scale`` is ``D ** -0.5`` unless given;
     ``window`` 0 sees everything.  See ``fasq_paged_attention``."""
     torch = _torch()
+    i32 = torch.int32
     _require_rows(q, "q", torch.float16, 3)
     T, Hq, D = q.shape
-    cache = _kv_cache(k_cache, v_cache)
-    Hkv = k_cache.shape[2]
-    if k_cache.shape[3] != D or Hkv < 1 or Hq % Hkv:
-        raise ValueError("the caches must be [pages x page_size x Hkv x D], Hq a multiple of Hkv")
-    _require_rows(pages, "pages", torch.int32, 2)
-    _require(q_start, "q_start", torch.int32, 1)
-    _require(kv_len, "kv_len", torch.int32, 1)
-    B = kv_len.shape[0]
-    if pages.shape[0] != B or q_start.shape[0] != B + 1:
-        raise ValueError("pages must be [B x max_pages], q_start [B + 1] and kv_len [B]")
     device = q.get_device()
+    cache = _kv_cache(k_cache, v_cache, device, None, D)
+    Hkv = k_cache.shape[2]
+    if Hkv < 1 or Hq % Hkv:
+        raise ValueError("the caches must be [pages x page_size x Hkv x D], Hq a multiple of Hkv")
+    _require(kv_len, "kv_len", i32, 1)
+    B = kv_len.shape[0]
+    _check_tensor(q_start, "q_start", i32, (B + 1,), device)
+    _require_rows(pages, "pages", i32, 2)
+    if pages.shape[0] != B:
+        raise ValueError("pages must be [B x max_pages], q_start [B + 1] and kv_len [B]")
+    if kv_len.get_device() != device or pages.get_device() != device:
+        _same_device(device, kv_len, pages)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device)
+        out = q.new_empty((T, Hq, D))
     else:
-        _require_rows(out, "out", torch.float16, 3)
-        if out.shape != q.shape:
-            raise ValueError("out must have the shape of q")
+        _check_rows(out, "out", torch.float16, q.shape, device)
     lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if return_lse else None
-    _same_device(device, k_cache, v_cache, pages, q_start, kv_len, out, workspace)
-    if workspace is None:
-        need = _on_device(device, lambda stream: paged_attention_workspace_bytes(T, B, Hq, Hkv, D))
-        if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    elif not (workspace.is_cuda and workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous device tensor")
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     qs, os_ = q.stride(), out.stride()
-    _check(_on_device(device, lib().fasq_paged_attention, q.data_ptr(), qs[0], qs[1], T, Hq, cache, Hkv, D,
-                      pages.data_ptr(), pages.stride(0), pages.shape[1], q_start.data_ptr(), kv_len.data_ptr(), B,
-                      D ** -0.5 if scale is None else scale, int(causal), window, out.data_ptr(), os_[0], os_[1],
-                      _ptr(lse), _ptr(workspace), ws_bytes))
+    L = lib()
+
+    def call(stream):
+        need = L.fasq_paged_attention_workspace_bytes(T, B, Hq, Hkv, D) if workspace is None else 0
+        ws, ws_bytes = _workspace(workspace, need, device)
+        return L.fasq_paged_attention(q.data_ptr(), qs[0], qs[1], T, Hq, cache, Hkv, D, pages.data_ptr(),
+                                      pages.stride(0), pages.shape[1], q_start.data_ptr(), kv_len.data_ptr(), B,
+                                      D ** -0.5 if scale is None else scale, causal, window, out.data_ptr(), os_[0],
+                                      os_[1], _ptr(lse), _ptr(ws), ws_bytes, stream)
+
+    _check(_on_device(device, call))
     return (out, lse) if return_lse else out
 
 
@@ -821,37 +856,31 @@ def residual_norm(x, y=None, weight=None, eps: float = 1e-5, post_weight=None, g
     [M x N].  Returns ``(x_new, h)``; ``x_new`` is None without ``y`` (unless
     ``x_out`` is given), ``h`` is None without ``weight``.  See
     ``fasq_residual_norm``."""
-    torch = _torch()
-    _require(x, "x", torch.float16, 2)
-    M, N = x.shape
+    f16 = _torch().float16
+    _require(x, "x", f16, 2)
+    shape = x.shape
+    M, N = shape
     device = x.get_device()
     stride = 0
     if y is not None:
-        _require(y, "y", torch.float16, 2)
-        if y.shape != x.shape:
-            raise ValueError("y must have the shape of x")
+        _check_tensor(y, "y", f16, shape, device)
         if x_out is None:
-            x_out = torch.empty_like(x)
-    for w, name in ((weight, "weight"), (post_weight, "post_weight")):
-        if w is not None:
-            _require(w, name, torch.float16, 1)
-            if w.shape[0] != N:
-                raise ValueError(f"{name} must be [N]")
+            x_out = x.new_empty(shape)
+        else:
+            _check_tensor(x_out, "x_out", f16, shape, device)
+    elif x_out is not None:
+        _check_tensor(x_out, "x_out", f16, shape, device)
+    if weight is not None:
+        _check_tensor(weight, "weight", f16, (N,), device)
+        if out is None:
+            out = x.new_empty(shape)
+    if out is not None:
+        _check_tensor(out, "out", f16, shape, device)
+    if post_weight is not None:
+        _check_tensor(post_weight, "post_weight", f16, (N,), device)
     if gate is not None:
-        if not isinstance(gate, torch.Tensor) or gate.dim() not in (1, 2):
-            raise ValueError("gate must be [N] or [M x N]")
-        _require(gate, "gate", torch.float16, gate.dim())
-        if gate.shape[-1] != N or (gate.dim() == 2 and gate.shape[0] != M):
-            raise ValueError("gate must be [N] or [M x N]")
-        stride = N if gate.dim() == 2 else 0
-    if weight is not None and out is None:
-        out = torch.empty_like(x)
-    for t, name in ((x_out, "x_out"), (out, "out")):
-        if t is not None:
-            _require(t, name, torch.float16, 2)
-            if t.shape != x.shape:
-                raise ValueError(f"{name} must have the shape of x")
-    _same_device(device, y, weight, post_weight, gate, x_out, out)
+        stride = N if getattr(gate, "ndim", 1) == 2 else 0
+        _check_tensor(gate, "gate", f16, shape if stride else (N,), device)
     _check(_on_device(device, lib().fasq_residual_norm, x.data_ptr(), _ptr(y), M, N, _ptr(post_weight), _ptr(gate),
                       stride, scale, _ptr(weight), eps, _ptr(x_out), _ptr(out)))
     return x_out, out
@@ -869,51 +898,54 @@ def lora_batched(x, adapters, As, Bs, scales, bases, outs=None, workspace=None):
     ``scales`` fp32 [L].  ``outs[i]`` may be ``bases[i]``.  Returns the list of
     outputs; see ``fasq_lora_batched``."""
     torch = _torch()
-    _require(x, "x", torch.float16, 2)
-    _require(adapters, "adapters", torch.int32, 1)
+    f16 = torch.float16
+    _require(x, "x", f16, 2)
     _require(scales, "scales", torch.float32, 1)
     M, K = x.shape
+    device = x.get_device()
+    _check_tensor(adapters, "adapters", torch.int32, (M,), device)
+    if scales.get_device() != device:
+        _same_device(device, scales)
     L, n = scales.shape[0], len(As)
     if not (len(Bs) == len(bases) == n and (outs is None or len(outs) == n)) or n < 1:
         raise ValueError("As, Bs, bases and outs must have equal lengths, at least 1")
-    if adapters.shape[0] != M:
-        raise ValueError("adapters must be [M]")
-    device = x.get_device()
-    _same_device(device, adapters, scales, workspace)
-    r, ys = 0, []
-    for i, (A, B, base) in enumerate(zip(As, Bs, bases)):
-        _require(A, f"A[{i}]", torch.float16, 3)
-        _require(B, f"B[{i}]", torch.float16, 3)
-        N = B.shape[1]
-        if i == 0:
+    r, ys, sizes, a_ptrs, b_ptrs, base_ptrs, y_ptrs = -1, [], [], [], [], [], []
+    for i in range(n):
+        A, B, base = As[i], Bs[i], bases[i]
+        if r < 0:
+            _require(A, "A[0]", f16, 3)
             r = A.shape[1]
-        if tuple(A.shape) != (L, r, K) or tuple(B.shape) != (L, N, r):
-            raise ValueError(f"A[{i}] must be [L x r x K] and B[{i}] [L x N x r], with the L of scales and one r")
+        _require(B, f"B[{i}]", f16, 3)
+        N = B.shape[1]
+        _check_tensor(A, f"A[{i}]", f16, (L, r, K), device)
+        _check_tensor(B, f"B[{i}]", f16, (L, N, r), device)
         if base is not None:
-            _require(base, f"base[{i}]", torch.float16, 2)
-            if tuple(base.shape) != (M, N):
-                raise ValueError(f"base[{i}] must be [M x N]")
+            _check_tensor(base, f"base[{i}]", f16, (M, N), device)
+            base_ptrs.append(base.data_ptr())
+        else:
+            base_ptrs.append(0)
         if outs is None:
             y = x.new_empty((M, N))
         else:
             y = outs[i]
-            _require(y, f"out[{i}]", torch.float16, 2)
-            if tuple(y.shape) != (M, N):
-                raise ValueError(f"out[{i}] must be [M x N]")
-        _same_device(device, A, B, base, y)
+            _check_tensor(y, f"out[{i}]", f16, (M, N), device)
         ys.append(y)
-    if workspace is None:
-        need = _on_device(device, lambda stream: lora_workspace_bytes(M, K, r, n))
-        if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    elif not (workspace.is_cuda and workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous device tensor")
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    arr_p, arr_i = _c_vp * n, _c_i64 * n
-    _check(_on_device(device, lib().fasq_lora_batched, x.data_ptr(), M, K, adapters.data_ptr(), L, r,
-                      scales.data_ptr(), n, arr_i(*[B.shape[1] for B in Bs]), arr_p(*[A.data_ptr() for A in As]),
-                      arr_p(*[B.data_ptr() for B in Bs]), arr_p(*[_ptr(b) for b in bases]),
-                      arr_p(*[y.data_ptr() for y in ys]), _ptr(workspace), ws_bytes))
+        sizes.append(N)
+        a_ptrs.append(A.data_ptr())
+        b_ptrs.append(B.data_ptr())
+        y_ptrs.append(y.data_ptr())
+    # sizes and addresses side by side in one host array
+    host = array.array("q", sizes + a_ptrs + b_ptrs + base_ptrs + y_ptrs)
+    at, step = host.buffer_info()[0], 8 * n
+    c = lib()
+
+    def call(stream):
+        need = c.fasq_lora_workspace_bytes(M, K, r, n) if workspace is None else 0
+        ws, ws_bytes = _workspace(workspace, need, device)
+        return c.fasq_lora_batched(x.data_ptr(), M, K, adapters.data_ptr(), L, r, scales.data_ptr(), n, at, at + step,
+                                   at + 2 * step, at + 3 * step, at + 4 * step, _ptr(ws), ws_bytes, stream)
+
+    _check(_on_device(device, call))
     return ys
 
 
