@@ -458,7 +458,8 @@ fasq_status fasq_rope_append(const void* q, int64_t q_token_stride, int64_t q_he
  * what is stored past kv_len is never used.
  *
  *   q, out      fp16 [T x Hq x D] with token and head strides; tokens outside
- *               every request are neither read nor written
+ *               every request are neither read nor written;
+ *               T * (Hq / Hkv) <= 2^30
  *   cache       16-byte aligned, strides multiples of 8
  *   D           a multiple of 8, 8 <= D <= 256
  *   pages       int32 [B x max_pages], row stride page_row_stride; entries
@@ -468,7 +469,7 @@ fasq_status fasq_rope_append(const void* q, int64_t q_token_stride, int64_t q_he
  *   kv_len      int32 [B], at most max_pages * page_size (more is cut there)
  *   lse         fp32 [T x Hq], contiguous, or NULL
  *   workspace   device scratch of fasq_paged_attention_workspace_bytes()
- *               bytes (16-byte aligned) for the fp32 partial results where
+ *               bytes (16-byte aligned) for the fp32 partial results, where
  *               the keys of a tile are split over workgroups; joined in a
  *               fixed order by a second kernel.  NULL or a smaller one: no
  *               split (slower where there are few tokens and long caches)

@@ -25,6 +25,19 @@ namespace fasq {
 
 typedef short short4_t __attribute__((ext_vector_type(4)));
 
+// A request as the kernels read it: lengths cut to what exists.
+struct Request {
+  int q0, n, kv;
+};
+
+// A tile whose keys several shares of the batch hold (see Place), as its first
+// share's workgroup leaves it for k_attention_join.
+struct CutTile {
+  int64_t start, end, share;
+  Request r;
+  int tile, head, cut;  // cut = 0: none starts in that share
+};
+
 struct AttentionArgs {
   HeadsView q, out;
   int64_t T, B;
@@ -34,6 +47,7 @@ struct AttentionArgs {
   int num_pages;
   uint32_t page_size;
   int page_shift;  // log2(page_size), -1 where it is no power of two
+  int g_shift;     // the same of G
   int64_t page_stride, slot_stride, head_stride;
   const int32_t* pages;
   int64_t page_row_stride;
@@ -52,16 +66,22 @@ struct AttentionArgs {
   int parts;
   float* part_o;  // [2 * parts][rows][DP], not divided by the sum
   float* part_ml;  // [2 * parts][rows][2]: maximum (in powers of two), sum
+  CutTile* cuts;   // [parts]
 };
 
 // ---------------------------------------------------------------------------
 // Where work lies
 // ---------------------------------------------------------------------------
 
-// A request as the kernels read it: lengths cut to what exists.
-struct Request {
-  int q0, n, kv;
-};
+// Quotients without the long way round that a 64-bit division, or one by a
+// value that is no constant, takes (about a microsecond of a short call).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
+}
+__device__ __forceinline__ int token_of(const AttentionArgs& a, int row) {
+  return a.g_shift >= 0 ? row >> a.g_shift : (int)((uint32_t)row / (uint32_t)a.G);
+}
 
 __device__ __forceinline__ Request read_request(const AttentionArgs& a, int64_t b) {
   const int T = (int)a.T;
@@ -71,6 +91,19 @@ __device__ __forceinline__ Request read_request(const AttentionArgs& a, int64_t 
   kv = kv < 0 ? 0 : kv > a.capacity ? a.capacity : kv;
   return {q0, q1 - q0, kv};
 }
+
+// The batch as a wave sees it: lane l keeps requests l, l + 64, ..., the first
+// of them in registers (all there are in most batches).
+struct Batch {
+  Request first;
+  __device__ __forceinline__ explicit Batch(const AttentionArgs& a) {
+    const int lane = threadIdx.x % kWave;
+    first = lane < a.B ? read_request(a, lane) : Request{0, 0, 0};
+  }
+  __device__ __forceinline__ Request of(const AttentionArgs& a, int64_t b) const {
+    return b < kWave ? first : read_request(a, b);
+  }
+};
 
 // Keys [begin, end) that token i of a request sees.
 struct Span {
@@ -90,7 +123,7 @@ template <int ROWS>
 __device__ __forceinline__ Span tile_span(const AttentionArgs& a, const Request& r, int t) {
   const int rows = r.n * a.G;
   const int last = (t + 1) * ROWS < rows ? (t + 1) * ROWS : rows;
-  const Span s0 = token_span(a, r, t * ROWS / a.G), s1 = token_span(a, r, (last - 1) / a.G);
+  const Span s0 = token_span(a, r, token_of(a, t * ROWS)), s1 = token_span(a, r, token_of(a, last - 1));
   return {s0.begin < s1.begin ? s0.begin : s1.begin, s1.end > s0.end ? s1.end : s0.end};
 }
 
@@ -112,7 +145,7 @@ __device__ __forceinline__ int64_t tile_length(const AttentionArgs& a, const Req
   if (!shared) return 1;
   int keys = r.kv;
   if (a.window > 0) {
-    const int most = a.window + ROWS / a.G + 32;  // of the tile's tokens, from a multiple of 32 on
+    const int most = a.window + token_of(a, ROWS) + 32;  // of the tile's tokens, from a multiple of 32 on
     keys = keys < most ? keys : most;
   }
   return keys <= STEP ? STEP : ((int64_t)keys + STEP - 1) / STEP * STEP;
@@ -144,10 +177,10 @@ __device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r
 
 // Positions of one cache head.
 template <int ROWS, int STEP>
-__device__ __forceinline__ int64_t head_length(const AttentionArgs& a, bool shared) {
+__device__ __forceinline__ int64_t head_length(const AttentionArgs& a, const Batch& batch, bool shared) {
   int64_t sum = 0;
   for (int64_t b = threadIdx.x % kWave; b < a.B; b += kWave) {
-    const Request r = read_request(a, b);
+    const Request r = batch.of(a, b);
     sum += tiles_of<ROWS>(a, r) * tile_length<ROWS, STEP>(a, r, shared);
   }
   return a.B == 1 ? lane_value(sum, 0) : uniform(wave_total(sum));
@@ -156,7 +189,7 @@ __device__ __forceinline__ int64_t head_length(const AttentionArgs& a, bool shar
 // The tile at a position within a head's stretch, in every lane of the wave.
 // pos < head_length.
 template <int ROWS, int STEP>
-__device__ __forceinline__ Place locate(const AttentionArgs& a, int64_t pos, bool shared) {
+__device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& batch, int64_t pos, bool shared) {
   Place p = {};
   int64_t base = 0;
   for (int64_t b0 = 0; b0 < a.B; b0 += kWave) {
@@ -164,7 +197,7 @@ __device__ __forceinline__ Place locate(const AttentionArgs& a, int64_t pos, boo
     Request r = {};
     int64_t one = 0, own = 0;
     if (b < a.B) {
-      r = read_request(a, b);
+      r = batch.of(a, b);
       one = tile_length<ROWS, STEP>(a, r, shared);
       own = tiles_of<ROWS>(a, r) * one;
     }
@@ -185,7 +218,7 @@ __device__ __forceinline__ Place locate(const AttentionArgs& a, int64_t pos, boo
       p.r.kv = lane_value(r.kv, l);
       one = lane_value(one, l);
       const int64_t first = base + lane_value(upto - own, l);
-      p.tile = (int)((pos - first) / one);
+      p.tile = (int)quotient(pos - first, one);
       p.start = first + p.tile * one;
       p.end = p.start + one;
       return p;
@@ -369,7 +402,10 @@ struct WaveTile {
   __device__ __forceinline__ void load_q(const AttentionArgs& a, const Request& r, int head, int row, bool live) {
     const int h = (threadIdx.x % kWave) / 32;
     const uint16_t* src = nullptr;
-    if (live) src = a.q.p + (r.q0 + row / a.G) * a.q.ts + (head * a.G + row % a.G) * a.q.hs;
+    if (live) {
+      const int t = token_of(a, row);
+      src = a.q.p + (r.q0 + t) * a.q.ts + (head * a.G + row - t * a.G) * a.q.hs;
+    }
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {
       const int d = s * 16 + h * 8;
@@ -763,12 +799,13 @@ struct SlowRow {
       return;
     }
     const float f = row_factor(l, sees);
-    uint16_t* dst = a.out.p + (r.q0 + row / a.G) * a.out.ts + (head * a.G + row % a.G) * a.out.hs;
+    const int t = token_of(a, row);
+    uint16_t* dst = a.out.p + (r.q0 + t) * a.out.ts + (head * a.G + row - t * a.G) * a.out.hs;
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (lane + i * kWave < a.D) dst[lane + i * kWave] = f32_to_f16_bits(o[i] * f);
     if (lane == 0 && a.lse != nullptr)
-      a.lse[(int64_t)(r.q0 + row / a.G) * a.Hq + head * a.G + row % a.G] = row_lse(m, l, sees);
+      a.lse[(int64_t)(r.q0 + t) * a.Hq + head * a.G + row - t * a.G] = row_lse(m, l, sees);
   }
 };
 

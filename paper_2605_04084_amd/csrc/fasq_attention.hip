@@ -29,11 +29,18 @@ __device__ __forceinline__ void store4(const AttentionArgs& a, uint16_t* dst, in
 }
 
 __device__ __forceinline__ uint16_t* out_row(const AttentionArgs& a, const Request& r, int head, int row) {
-  return a.out.p + (r.q0 + row / a.G) * a.out.ts + (head * a.G + row % a.G) * a.out.hs;
+  const int t = token_of(a, row);
+  return a.out.p + (r.q0 + t) * a.out.ts + (head * a.G + row - t * a.G) * a.out.hs;
+}
+
+__device__ __forceinline__ const uint16_t* query_row(const AttentionArgs& a, const Request& r, int head, int row) {
+  const int t = token_of(a, row);
+  return a.q.p + (r.q0 + t) * a.q.ts + (head * a.G + row - t * a.G) * a.q.hs;
 }
 
 __device__ __forceinline__ int64_t lse_at(const AttentionArgs& a, const Request& r, int head, int row) {
-  return (int64_t)(r.q0 + row / a.G) * a.Hq + head * a.G + row % a.G;
+  const int t = token_of(a, row);
+  return (int64_t)(r.q0 + t) * a.Hq + head * a.G + row - t * a.G;
 }
 
 // Chunks past D are zero and stay so.
@@ -51,9 +58,16 @@ __device__ __forceinline__ int64_t slot_of(int64_t w, int64_t share, int64_t til
   return 2 * w + (tile_start > w * share ? 1 : 0);
 }
 
+// Leaves the tile that starts in share w and goes on past it for the join (or
+// that there is none).  One thread.
+__device__ __forceinline__ void leave_cut(const AttentionArgs& a, int64_t w, int64_t share, const Place& p, int head,
+                                          int64_t t0, int64_t t1, bool cut) {
+  a.cuts[w] = CutTile{t0, t1, share, p.r, p.tile, head, cut ? 1 : 0};
+}
+
 template <int STEP>
 __device__ __forceinline__ int64_t share_of(int64_t total, int parts, int least) {
-  const int64_t s = (total + parts - 1) / parts;
+  const int64_t s = quotient(total + parts - 1, parts);
   return s <= least ? least : (s + STEP - 1) / STEP * STEP;
 }
 
@@ -80,20 +94,26 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
 
   const RowCopy<DP, FULL> copy(a);
   const bool shared = a.part_o != nullptr;
-  const int64_t head_len = head_length<ROWS, STEP>(a, shared);
+  const Batch batch(a);
+  const int64_t head_len = head_length<ROWS, STEP>(a, batch, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   if (shared) {
     share = share_of<STEP>(head_len * a.Hkv, a.parts, kFewShare);
     pos = w * share;
     pos_end = pos + share < head_len * a.Hkv ? pos + share : head_len * a.Hkv;
   } else {
-    pos = (w % a.Hkv) * head_len + w / a.Hkv;
-    pos_end = w / a.Hkv < head_len ? pos + 1 : pos;
+    const int64_t tile = quotient(w, a.Hkv);
+    pos = (w - tile * a.Hkv) * head_len + tile;
+    pos_end = tile < head_len ? pos + 1 : pos;
   }
+  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(a, w, share, Place{}, 0, 0, 0, false);
   while (pos < pos_end) {
-    const int head = (int)(pos / head_len);
-    const Place p = locate<ROWS, STEP>(a, pos - head * head_len, shared);
-    if (p.b < 0) return;
+    const int head = (int)quotient(pos, head_len);
+    const Place p = locate<ROWS, STEP>(a, batch, pos - head * head_len, shared);
+    if (p.b < 0) {
+      if (shared && threadIdx.x == 0) leave_cut(a, w, share, p, 0, 0, 0, false);
+      return;
+    }
     const int64_t t0 = head * head_len + p.start, t1 = head * head_len + p.end;
     const int64_t seg_end = t1 < pos_end ? t1 : pos_end;
     const Span span = tile_span<ROWS>(a, p.r, p.tile);
@@ -106,9 +126,9 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
     }
     const int rows = p.r.n * a.G, row0 = p.tile * ROWS, live = rows - row0 < ROWS ? rows - row0 : ROWS;
     const bool alive = l32 < live;
-    Span mine = token_span(a, p.r, (row0 + (alive ? l32 : live - 1)) / a.G);
+    Span mine = token_span(a, p.r, token_of(a, row0 + (alive ? l32 : live - 1)));
     // keys that every live row sees
-    const Span s0 = token_span(a, p.r, row0 / a.G), s1 = token_span(a, p.r, (row0 + live - 1) / a.G);
+    const Span s0 = token_span(a, p.r, token_of(a, row0)), s1 = token_span(a, p.r, token_of(a, row0 + live - 1));
     const int all_begin = s0.begin > s1.begin ? s0.begin : s1.begin;
     int all_end = s0.end < s1.end ? s0.end : s1.end;
     const bool mixed = s0.begin != s1.begin || s0.end != s1.end;  // rows see different keys
@@ -175,6 +195,8 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
     __syncthreads();
     const bool cut = shared && (t0 < pos || seg_end < t1);
     const int64_t slot = cut ? slot_of(w, share, t0) : 0;
+    if (shared && seg_end == pos_end && threadIdx.x == 0)
+      leave_cut(a, w, share, p, head, t0, t1, t0 >= w * share && t1 > seg_end);
     for (int u = threadIdx.x; u < live * (DP / 4); u += NW * kWave) {
       const int row = u / (DP / 4), d = u % (DP / 4) * 4;
       float top = jm[row];
@@ -198,7 +220,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
           a.part_ml[(slot * ROWS + row) * 2 + 1] = sum;
         }
       } else {
-        const Span s = token_span(a, p.r, (row0 + row) / a.G);
+        const Span s = token_span(a, p.r, token_of(a, row0 + row));
         const float f = row_factor(sum, s.begin < s.end);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] *= f;
@@ -212,10 +234,10 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
     for (int i = 0; i < NW; ++i) any_suspect |= flag[32 + i];
     for (int row = wave; row < live; row += NW) {
       if ((flag[row] | any_suspect) == 0) continue;
-      const Span s = token_span(a, p.r, (row0 + row) / a.G);
+      const Span s = token_span(a, p.r, token_of(a, row0 + row));
       SlowRow<DP> slow;
-      slow.run(a, a.q.p + (p.r.q0 + (row0 + row) / a.G) * a.q.ts + (head * a.G + (row0 + row) % a.G) * a.q.hs, head_off,
-               pages, s.begin > lo ? s.begin : lo, s.end < hi ? s.end : hi);
+      slow.run(a, query_row(a, p.r, head, row0 + row), head_off, pages, s.begin > lo ? s.begin : lo,
+               s.end < hi ? s.end : hi);
       slow.template store<ROWS>(a, p.r, head, row0 + row, row, cut ? slot : -1, s.begin < s.end, flag[row] != 0);
     }
     __syncthreads();
@@ -237,7 +259,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 
   const RowCopy<DP, FULL> copy(a);
   const bool shared = a.part_o != nullptr;
-  const int64_t head_len = head_length<ROWS, STEP>(a, shared);
+  const Batch batch(a);
+  const int64_t head_len = head_length<ROWS, STEP>(a, batch, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   if (shared) {
     // Workgroups go to the XCDs in turn, and each XCD has its own L2: its
@@ -248,13 +271,18 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     pos = w * share;
     pos_end = pos + share < head_len * a.Hkv ? pos + share : head_len * a.Hkv;
   } else {
-    pos = (w % a.Hkv) * head_len + w / a.Hkv;
-    pos_end = w / a.Hkv < head_len ? pos + 1 : pos;
+    const int64_t tile = quotient(w, a.Hkv);
+    pos = (w - tile * a.Hkv) * head_len + tile;
+    pos_end = tile < head_len ? pos + 1 : pos;
   }
+  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(a, w, share, Place{}, 0, 0, 0, false);
   while (pos < pos_end) {
-    const int head = (int)(pos / head_len);
-    Place p = locate<ROWS, STEP>(a, pos - head * head_len, shared);
-    if (p.b < 0) return;
+    const int head = (int)quotient(pos, head_len);
+    Place p = locate<ROWS, STEP>(a, batch, pos - head * head_len, shared);
+    if (p.b < 0) {
+      if (shared && threadIdx.x == 0) leave_cut(a, w, share, p, 0, 0, 0, false);
+      return;
+    }
     // the tiles with the most keys first
     if (!shared) p.tile = tiles_of<ROWS>(a, p.r) - 1 - p.tile;
     const int64_t t0 = head * head_len + p.start, t1 = head * head_len + p.end;
@@ -272,14 +300,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     const bool alive = l32 < live;
     Span mine = {0, 0}, all = {0, 0}, any = {0, 0};
     if (live > 0) {
-      if (alive) mine = token_span(a, p.r, (row0 + l32) / a.G);
-      const Span s0 = token_span(a, p.r, row0 / a.G), s1 = token_span(a, p.r, (row0 + live - 1) / a.G);
+      if (alive) mine = token_span(a, p.r, token_of(a, row0 + l32));
+      const Span s0 = token_span(a, p.r, token_of(a, row0)), s1 = token_span(a, p.r, token_of(a, row0 + live - 1));
       all = {s0.begin > s1.begin ? s0.begin : s1.begin, s0.end < s1.end ? s0.end : s1.end};
       any = {s0.begin < s1.begin ? s0.begin : s1.begin, s0.end > s1.end ? s0.end : s1.end};
     }
     // over the four waves: whether rows see different keys, and which all see
     const int tile_rows = rows - p.tile * ROWS < ROWS ? rows - p.tile * ROWS : ROWS;
-    const Span f0 = token_span(a, p.r, p.tile * ROWS / a.G), f1 = token_span(a, p.r, (p.tile * ROWS + tile_rows - 1) / a.G);
+    const Span f0 = token_span(a, p.r, token_of(a, p.tile * ROWS));
+    const Span f1 = token_span(a, p.r, token_of(a, p.tile * ROWS + tile_rows - 1));
     const bool mixed = f0.begin != f1.begin || f0.end != f1.end;
     const int most_begin = f0.begin > f1.begin ? f0.begin : f1.begin, least_end = f0.end < f1.end ? f0.end : f1.end;
     const bool sees = mine.begin < mine.end;
@@ -405,6 +434,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     const float l = t.total();
     const bool cut = shared && (t0 < pos || seg_end < t1);
     const int64_t slot = cut ? slot_of(w, share, t0) : 0;
+    if (shared && seg_end == pos_end && threadIdx.x == 0)
+      leave_cut(a, w, share, p, head, t0, t1, t0 >= w * share && t1 > seg_end);
     if (alive) {
       if (cut) {
         const int64_t at = slot * ROWS + wave * 32 + l32;
@@ -440,9 +471,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       while (again != 0) {
         const int i = __ffsll((unsigned long long)again) - 1, row = row0 + i;
         again &= again - 1;
-        const Span s = token_span(a, p.r, row / a.G);
+        const Span s = token_span(a, p.r, token_of(a, row));
         SlowRow<DP> slow;
-        slow.run(a, a.q.p + (p.r.q0 + row / a.G) * a.q.ts + (head * a.G + row % a.G) * a.q.hs, head_off, pages,
+        slow.run(a, query_row(a, p.r, head, row), head_off, pages,
                  s.begin > lo ? s.begin : lo, s.end < hi ? s.end : hi);
         slow.template store<ROWS>(a, p.r, head, row, wave * 32 + i, cut ? slot : -1, s.begin < s.end,
                                   (broken >> i & 1) != 0);
@@ -454,26 +485,19 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 }
 
 // ---------------------------------------------------------------------------
-// Joins the shares of one cut tile: workgroup x takes the tile that contains
-// the border between shares x and x + 1, if it is that tile's first border;
-// y cuts the tile's rows.  Shares are added in their order, by groups of
-// threads that take every PG-th share where there are few rows.
+// Joins the shares of one cut tile: workgroup x takes the one that starts in
+// share x, y cuts the tile's rows.  Shares are added in their order, by groups
+// of threads that take every PG-th share where there are few rows.
 // ---------------------------------------------------------------------------
-template <int DP, int ROWS, int STEP, int LEAST, int YS>
+template <int DP, int ROWS, int YS>
 __global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a) {
   constexpr int TH = 256, CH = DP / 4;
   __shared__ float so[TH * 4], sm[TH], sl[TH];
-  const int64_t head_len = head_length<ROWS, STEP>(a, true), total = head_len * a.Hkv;
-  const int64_t share = share_of<STEP>(total, a.parts, LEAST);
-  const int64_t pos = (blockIdx.x + 1) * share;
-  if (pos >= total) return;
-  const int head = (int)(pos / head_len);
-  const Place p = locate<ROWS, STEP>(a, pos - head * head_len, true);
-  if (p.b < 0) return;
-  const int64_t t0 = head * head_len + p.start, t1 = head * head_len + p.end;
-  if (t0 == pos || pos - share > t0) return;
-  const int64_t w0 = t0 / share, w1 = (t1 - 1) / share;
-  const int nparts = (int)(w1 - w0 + 1);
+  const CutTile p = a.cuts[blockIdx.x];
+  if (!p.cut) return;
+  const int head = p.head;
+  const int64_t t0 = p.start, t1 = p.end, share = p.share, w0 = blockIdx.x;
+  const int nparts = (int)(quotient(t1 - 1, share) - w0 + 1);
   constexpr int YROWS = ROWS / YS;
   const int rows = p.r.n * a.G, row0 = p.tile * ROWS, first = blockIdx.y * YROWS;
   const int live = (rows - row0 < ROWS ? rows - row0 : ROWS) - first < YROWS ? rows - row0 - first : YROWS;
@@ -522,7 +546,7 @@ __global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a) {
       }
     }
     if (!active) continue;
-    const Span s = token_span(a, p.r, (row0 + row) / a.G);
+    const Span s = token_span(a, p.r, token_of(a, row0 + row));
     const float f = row_factor(l, s.begin < s.end);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] *= f;
@@ -554,7 +578,8 @@ AttentionPlan plan_attention(int64_t T, int64_t B, int Hq, int Hkv, int D, const
   p.parts = dev.num_cus * (p.few ? (p.DP == 64 ? 2 : 1) : (p.DP == 256 ? 1 : 2));
   // with twice as many whole tiles as the chip holds a split gains nothing
   p.split = p.few || rows / p.rows * Hkv < 2 * p.parts;
-  p.bytes = p.split ? int64_t(2) * p.parts * p.rows * (p.DP + 2) * (int64_t)sizeof(float) : 0;
+  const int64_t of_share = int64_t(2) * p.rows * (p.DP + 2) * (int64_t)sizeof(float) + (int64_t)sizeof(CutTile);
+  p.bytes = p.split ? p.parts * of_share : 0;
   return p;
 }
 
@@ -568,14 +593,12 @@ hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipSt
     if ((e = prepare_kernel(k_attention_few<DP, NW, FULL>)) != hipSuccess) return e;
     e = launch_kernel(k_attention_few<DP, NW, FULL>, dim3((unsigned)blocks), dim3(NW * kWave), NW * 256 * DP, stream, a);
     if (e != hipSuccess || !shared) return e;
-    return launch_kernel(k_attention_join<DP, 32, NW * 32, kFewShare, 1>, dim3((unsigned)blocks - 1), dim3(256), 0,
-                         stream, a);
+    return launch_kernel(k_attention_join<DP, 32, 1>, dim3((unsigned)blocks - 1), dim3(256), 0, stream, a);
   }
   if ((e = prepare_kernel(k_attention_tile<DP, FULL>)) != hipSuccess) return e;
   e = launch_kernel(k_attention_tile<DP, FULL>, dim3((unsigned)blocks), dim3(256), 512 * DP + 16, stream, a);
   if (e != hipSuccess || !shared) return e;
-  return launch_kernel(k_attention_join<DP, 128, 64, kTileShare, 8>, dim3((unsigned)blocks - 1, 8), dim3(256), 0, stream,
-                       a);
+  return launch_kernel(k_attention_join<DP, 128, 8>, dim3((unsigned)blocks - 1, 8), dim3(256), 0, stream, a);
 }
 
 }  // namespace
@@ -602,6 +625,9 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
   a.page_shift = -1;
   for (int s = 0; s < 31; ++s)
     if (p.cache.page_size == int64_t(1) << s) a.page_shift = s;
+  a.g_shift = -1;
+  for (int s = 0; s < 31; ++s)
+    if (a.G == 1 << s) a.g_shift = s;
   a.page_stride = p.cache.page_stride;
   a.slot_stride = p.cache.slot_stride;
   a.head_stride = p.cache.head_stride;
@@ -626,6 +652,7 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
     a.parts = pl.parts;
     a.part_o = static_cast<float*>(p.workspace);
     a.part_ml = a.part_o + int64_t(2) * pl.parts * pl.rows * pl.DP;
+    a.cuts = reinterpret_cast<CutTile*>(a.part_ml + int64_t(2) * pl.parts * pl.rows * 2);
   }
   const bool full = p.D == pl.DP;
   switch (pl.DP) {

@@ -90,7 +90,7 @@ def _attend(L, **kw):
     (dict(q=0), "NULL"), (dict(out=0), "NULL"), (dict(pages=0), "NULL"), (dict(q_start=0), "NULL"),
     (dict(kv_len=0), "NULL"), (dict(cache=None), "cache is NULL"), (dict(max_pages=1 << 28), "31 bits"),
     (dict(cache=_cache(k=DUMMY + 8)), "16-byte"), (dict(cache=_cache(slot_stride=100)), "multiples of 8"),
-    (dict(out=DUMMY + 1), "2-byte"), (dict(qs=-1), "strides"),
+    (dict(out=DUMMY + 1), "2-byte"), (dict(qs=-1), "strides"), (dict(T=1 << 24, Hq=256), "2^30"),
 ])
 def test_attention_refuses(L, args, why):
     _refused(_attend(L, **args), why)
