@@ -24,6 +24,7 @@
 namespace fasq {
 
 typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef half8_t half8_any __attribute__((aligned(2)));
 
 // A request as the kernels read it: lengths cut to what exists.
 struct Request {
@@ -57,7 +58,7 @@ struct AttentionArgs {
   float c;  // |scale| * log2(e), at least 1e-30 so that -inf stays -inf
   bool negate;  // scale < 0: the queries change sign instead
   bool causal;
-  bool q_vec, out_vec;  // 16-byte loads of q, 8-byte stores of out
+  bool out_vec;  // 8-byte stores of out
   bool whole_units;     // pages hold whole units of 16 keys, within 2^31 bytes
   int window;  // 0: none
   float* lse;
@@ -68,6 +69,16 @@ struct AttentionArgs {
   float* part_ml;  // [2 * parts][rows][2]: maximum (in powers of two), sum
   CutTile* cuts;   // [parts]
 };
+
+// The kernel's arguments (its only parameter), as if read for the first time:
+// where a kernel starts a new phase it reads what it needs again, a scalar load
+// or two, instead of holding all of it and what follows from it in registers
+// from the start on (which cost hundreds of instructions before the first key).
+__device__ __forceinline__ const AttentionArgs& fresh_args() {
+  auto p = (__attribute__((address_space(4))) const AttentionArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const AttentionArgs*)p;
+}
 
 // ---------------------------------------------------------------------------
 // Where work lies
@@ -397,31 +408,25 @@ struct WaveTile {
     l = 0.f;
   }
 
-  // Row `row` of the request (lane l and l ^ 32 hold one row; rows past the
-  // end, and values past D, are zero).
+  // Row `row` of the request, which exists (lane l and l ^ 32 hold one row;
+  // zeros unless `live`, and past D).
   __device__ __forceinline__ void load_q(const AttentionArgs& a, const Request& r, int head, int row, bool live) {
     const int h = (threadIdx.x % kWave) / 32;
-    const uint16_t* src = nullptr;
-    if (live) {
-      const int t = token_of(a, row);
-      src = a.q.p + (r.q0 + t) * a.q.ts + (head * a.G + row - t * a.G) * a.q.hs;
-    }
+    const int t = token_of(a, row);
+    const uint16_t* src = a.q.p + (r.q0 + t) * a.q.ts + (head * a.G + row - t * a.G) * a.q.hs;
+    // all loads first (wherever rows start), then what they have to wait for
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {
       const int d = s * 16 + h * 8;
-      half8_t v = {};
-      if (live && d < a.D) {
-        if (a.q_vec) {
-          v = *reinterpret_cast<const half8_t*>(src + d);
-        } else {
-          u32x4 w = {};
+      q[s] = *reinterpret_cast<const half8_any*>(src + (d < a.D ? d : 0));
+    }
+    const uint32_t flip = a.negate ? 0x80008000u : 0u;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w[e / 2] |= (uint32_t)src[d + e] << (e % 2 * 16);
-          v = __builtin_bit_cast(half8_t, w);
-        }
-        if (a.negate) v = -v;
-      }
-      q[s] = v;
+    for (int s = 0; s < DP / 16; ++s) {
+      u32x4 w = __builtin_bit_cast(u32x4, q[s]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = live && s * 16 + h * 8 < a.D ? w[e] ^ flip : 0u;
+      q[s] = __builtin_bit_cast(half8_t, w);
     }
   }
 
@@ -546,13 +551,26 @@ struct WaveTile {
   static constexpr int OPS = 4;      // operands held: the current one and three ahead
   u32x4 ops[OPS];
 
-  // Operand i of a block: key operand i, or value operand i - N.
+  // The steps: a product with the keys adds to the one before it, and the matrix
+  // cores take one that has to wait for its sum at half their rate, so two
+  // of them are followed by one with the values (which add to DP / 32 sums in
+  // turn); at DP = 64, where the scores would come too late for their maximum,
+  // the keys come first.
+  static constexpr bool MIXED = N > 4;
+  static constexpr bool is_key(int i) { return MIXED ? i < N / 2 * 3 && i % 3 < 2 : i < N; }
+  static constexpr int nth(int i) {  // of its kind
+    return !MIXED ? i % N : i >= N / 2 * 3 ? i - N : i % 3 < 2 ? i / 3 * 2 + i % 3 : i / 3;
+  }
+  static constexpr int SCORED = MIXED ? N / 2 * 3 - 2 : N - 1;  // the last step with the keys
+
+  // The operand of step i.
   __device__ __forceinline__ void read_op(uint32_t k_at, const uint32_t (&v_at)[2], int i) {
-    if (i < N) {
-      ops[i % OPS] = __builtin_bit_cast(u32x4, *(lds_half8)(uintptr_t)((k_at ^ (i % 8 * 32)) + i / 8 * 256));
+    if (is_key(i)) {
+      const int t = nth(i);
+      ops[i % OPS] = __builtin_bit_cast(u32x4, *(lds_half8)(uintptr_t)((k_at ^ (t % 8 * 32)) + t / 8 * 256));
       return;
     }
-    const int u = (i - N) / (DP / 32), d = (i - N) % (DP / 32);
+    const int u = nth(i) / (DP / 32), d = nth(i) % (DP / 32);
     short4_t part[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -574,12 +592,14 @@ struct WaveTile {
 
   // Scores of a block alone.
   __device__ __forceinline__ void scores(uint32_t k_at, float16_t& s) {
-    const uint32_t none[2] = {0, 0};
+    auto read = [&](int t) {
+      ops[t % OPS] = __builtin_bit_cast(u32x4, *(lds_half8)(uintptr_t)((k_at ^ (t % 8 * 32)) + t / 8 * 256));
+    };
 #pragma unroll
-    for (int t = 0; t < OPS - 1; ++t) read_op(k_at, none, t);
+    for (int t = 0; t < OPS - 1; ++t) read(t);
 #pragma unroll
     for (int t = 0; t < N; ++t) {
-      if (t + OPS - 1 < N) read_op(k_at, none, t + OPS - 1);
+      if (t + OPS - 1 < N) read(t + OPS - 1);
       __builtin_amdgcn_sched_barrier(0);
       s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, ops[t % OPS]), q[t],
                                                  t == 0 ? float16_t{} : s, 0, 0, 0);
@@ -643,10 +663,11 @@ struct WaveTile {
   // block at k_at, the values at v_at weighted with `p`, and next's largest score
   // of the row (top) and by how much it passes the maximum (over).  The operands
   // of the first three steps are there; those of the block after this one are
-  // read if `more` (at k_more).  at_step(i): what else step i issues.
+  // read if `more` (at k_more, v_more).  at_step(i): what else step i issues.
   template <typename F>
   __device__ __forceinline__ void block(const float16_t& s, float16_t& next, const half8_t (&p)[2], half8_t (&made)[2],
-                                        uint32_t k_at, const uint32_t (&v_at)[2], bool more, uint32_t k_more, float c,
+                                        uint32_t k_at, const uint32_t (&v_at)[2], bool more, uint32_t k_more,
+                                        const uint32_t (&v_more)[2], float c,
                                         float& top, float& over, F at_step) {
     constexpr int STEPS = 2 * N;
     float w[16];
@@ -665,12 +686,12 @@ struct WaveTile {
     for (int i = 0; i < STEPS; ++i) {
       const int j = i + OPS - 1;
       if (j < STEPS) read_op(k_at, v_at, j);
-      else if (more) read_op(k_more, v_at, j - STEPS);
+      else if (more) read_op(k_more, v_more, j - STEPS);
       __builtin_amdgcn_sched_barrier(0);
       const half8_t op = __builtin_bit_cast(half8_t, ops[i % OPS]);
-      if (i < N) next = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, q[i < N ? i : 0], i == 0 ? float16_t{} : next, 0, 0, 0);
+      if (is_key(i)) next = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, q[nth(i)], i == 0 ? float16_t{} : next, 0, 0, 0);
       else {
-        const int u = (i - N) / (DP / 32), d = (i - N) % (DP / 32);
+        const int u = nth(i) / (DP / 32), d = nth(i) % (DP / 32);
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, p[u], o[d], 0, 0, 0);
       }
 #pragma unroll
@@ -683,12 +704,12 @@ struct WaveTile {
         if (e >= 1) add(e - 1);
       }
       // the maximum, from the second step after the scores are complete on
-      if (i == N + 1 || i == N + 2) {
+      if (i == SCORED + 2 || i == SCORED + 3) {
 #pragma unroll
-        for (int e = i == N + 1 ? 0 : 8; e < (i == N + 1 ? 8 : 16); ++e) top = e == 0 ? next[0] : fmaxf(top, next[e]);
+        for (int e = i == SCORED + 2 ? 0 : 8; e < (i == SCORED + 2 ? 8 : 16); ++e) top = e == 0 ? next[0] : fmaxf(top, next[e]);
         asm volatile("" : "+v"(top));
       }
-      if (i == N + 3) {
+      if (i == SCORED + 4) {
         top = row_max(top);
         over = (top - m) * c;
         asm volatile("" : "+v"(top), "+v"(over));

@@ -81,7 +81,8 @@ constexpr int kTileShare = 256;
 // are joined in wave order.
 // ---------------------------------------------------------------------------
 template <int DP, int NW, bool FULL>
-__global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a) {
+__global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) {
+  const AttentionArgs given = fresh_args();
   constexpr int ROWS = 32, STEP = NW * 32, OS = DP + 4, COPIES = 4 * RowCopy<DP, FULL>::INSTR;  // of a stage
   extern __shared__ uint8_t smem[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -92,22 +93,23 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
   float* jl = jm + NW * 32;                             // [NW][32]
   int* flag = reinterpret_cast<int*>(jl + NW * 32);     // [32], then [NW] of the waves
 
-  const RowCopy<DP, FULL> copy(a);
-  const bool shared = a.part_o != nullptr;
-  const Batch batch(a);
-  const int64_t head_len = head_length<ROWS, STEP>(a, batch, shared);
+  const RowCopy<DP, FULL> copy(given);
+  const bool shared = given.part_o != nullptr;
+  const Batch batch(given);
+  const int64_t head_len = head_length<ROWS, STEP>(given, batch, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   if (shared) {
-    share = share_of<STEP>(head_len * a.Hkv, a.parts, kFewShare);
+    share = share_of<STEP>(head_len * given.Hkv, given.parts, kFewShare);
     pos = w * share;
-    pos_end = pos + share < head_len * a.Hkv ? pos + share : head_len * a.Hkv;
+    pos_end = pos + share < head_len * given.Hkv ? pos + share : head_len * given.Hkv;
   } else {
-    const int64_t tile = quotient(w, a.Hkv);
-    pos = (w - tile * a.Hkv) * head_len + tile;
+    const int64_t tile = quotient(w, given.Hkv);
+    pos = (w - tile * given.Hkv) * head_len + tile;
     pos_end = tile < head_len ? pos + 1 : pos;
   }
-  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(a, w, share, Place{}, 0, 0, 0, false);
+  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(given, w, share, Place{}, 0, 0, 0, false);
   while (pos < pos_end) {
+    const AttentionArgs a = fresh_args();
     const int head = (int)quotient(pos, head_len);
     const Place p = locate<ROWS, STEP>(a, batch, pos - head * head_len, shared);
     if (p.b < 0) {
@@ -140,8 +142,6 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
 
     if constexpr (!FULL) clear_lds<DP>(ring, 2 * 2 * 32);
     WaveTile<DP, 1> t;
-    t.clear();
-    t.load_q(a, p.r, head, row0 + l32, alive);
     int k0 = lo + wave * 32;
     auto page_at = [&](int k) {
       const int j = k + l32;
@@ -156,6 +156,8 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
       copy.run(a, a.cv, head_off, page1, k + 16, span.begin, hi - 1, to + 48 * DP * 2);
     };
     int page = page_at(k0), stage = 0;
+    t.load_q(a, p.r, head, row0 + (alive ? l32 : live - 1), alive);
+    t.clear();
     if (k0 < hi) issue(k0, page, 0);
     page = page_at(k0 + STEP);
     for (; k0 < hi; k0 += STEP, stage ^= 1) {
@@ -249,7 +251,8 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs a
 // 128 rows: four waves of 32 rows over shared tiles of 64 keys, two stages.
 // ---------------------------------------------------------------------------
 template <int DP, bool FULL>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(AttentionArgs a) {
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(AttentionArgs) {
+  const AttentionArgs given = fresh_args();
   constexpr int ROWS = 128, STEP = 64;
   extern __shared__ uint8_t smem[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -257,26 +260,32 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
   uint16_t* ring = reinterpret_cast<uint16_t*>(smem);
   int* flag = reinterpret_cast<int*>(smem + 512 * DP);  // a value of a mixed tile was not finite
 
-  const RowCopy<DP, FULL> copy(a);
-  const bool shared = a.part_o != nullptr;
-  const Batch batch(a);
-  const int64_t head_len = head_length<ROWS, STEP>(a, batch, shared);
+  const RowCopy<DP, FULL> copy(given);
+  const bool shared = given.part_o != nullptr;
+  const Batch batch(given);
+  const int64_t head_len = head_length<ROWS, STEP>(given, batch, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   if (shared) {
     // Workgroups go to the XCDs in turn, and each XCD has its own L2: its
     // shares lie side by side, so that they read the keys of few heads (2048
     // tokens after 6144, 8 heads: one head an XCD; 332 us without).
-    if (a.parts % kXcds == 0) w = w % kXcds * (a.parts / kXcds) + w / kXcds;
-    share = share_of<STEP>(head_len * a.Hkv, a.parts, kTileShare);
+    if (given.parts % kXcds == 0) {
+      const int per = given.parts / kXcds;
+      int v = (int)w / kXcds;
+      if (DP <= 128 && v >= per / 2) v = per / 2 + (per - 1 - v);
+      w = w % kXcds * per + v;
+    }
+    share = share_of<STEP>(head_len * given.Hkv, given.parts, kTileShare);
     pos = w * share;
-    pos_end = pos + share < head_len * a.Hkv ? pos + share : head_len * a.Hkv;
+    pos_end = pos + share < head_len * given.Hkv ? pos + share : head_len * given.Hkv;
   } else {
-    const int64_t tile = quotient(w, a.Hkv);
-    pos = (w - tile * a.Hkv) * head_len + tile;
+    const int64_t tile = quotient(w, given.Hkv);
+    pos = (w - tile * given.Hkv) * head_len + tile;
     pos_end = tile < head_len ? pos + 1 : pos;
   }
-  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(a, w, share, Place{}, 0, 0, 0, false);
+  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(given, w, share, Place{}, 0, 0, 0, false);
   while (pos < pos_end) {
+    const AttentionArgs a = fresh_args();
     const int head = (int)quotient(pos, head_len);
     Place p = locate<ROWS, STEP>(a, batch, pos - head * head_len, shared);
     if (p.b < 0) {
@@ -324,8 +333,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       __syncthreads();
     }
     WaveTile<DP, 1> t;
-    t.clear();
-    t.load_q(a, p.r, head, row0 + l32, alive);
     auto page_at = [&](int k) {
       const int j = k + wave * 16 + lane % 16;
       return k < hi ? page_of(a, pages, j < span.begin ? span.begin : j < hi ? j : hi - 1) : 0;
@@ -347,8 +354,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       }
     };
     auto masked = [&](int k) { return k < all.begin || k + 32 > all.end; };
+    int page[3] = {page_at(lo), page_at(lo + STEP), 0};
+    t.load_q(a, p.r, head, alive ? row0 + l32 : p.tile * ROWS, alive);
+    t.clear();
     if (lo < hi) {
-      int page[3] = {page_at(lo), page_at(lo + STEP), 0};
+      asm volatile("" : "+v"(page[0]), "+v"(page[1]));  // one wait for both, and not for copies
       copy_keys(lo, page[0], 0);
       copy_keys(lo + STEP, page[1], 1);  // behind the end: any key, masked
       copy_values(lo, page[0], 0);
@@ -420,9 +430,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 #pragma unroll
         for (int i = 0; i < WaveTile<DP, 1>::OPS - 1; ++i) t.read_op(kn, v, i);
         float over = 0.f;
-        t.block(s1, s0, p0, p1, kn, v, true, kn + 32 * DP * 2, a.c, top, over, at_step);
+        t.block(s1, s0, p0, p1, kn, v, true, kn + 32 * DP * 2, v32, a.c, top, over, at_step);
         t.settle(s0, top, over, p1, k0 + STEP, mine.begin, mine.end, masked(k0 + STEP), a.c);
-        t.block(s0, s1, p1, p0, kn + 32 * DP * 2, v32, false, 0, a.c, top, over,
+        t.block(s0, s1, p1, p0, kn + 32 * DP * 2, v32, false, 0, v32, a.c, top, over,
                 [&](int i) { at_step(i + DP / 8); });
         t.settle(s1, top, over, p0, k0 + STEP + 32, mine.begin, mine.end, masked(k0 + STEP + 32), a.c);
         page_v = page[0];
@@ -432,10 +442,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       wait_loads<0>();  // copies behind the end
     }
     const float l = t.total();
+    const AttentionArgs end = fresh_args();
     const bool cut = shared && (t0 < pos || seg_end < t1);
     const int64_t slot = cut ? slot_of(w, share, t0) : 0;
     if (shared && seg_end == pos_end && threadIdx.x == 0)
-      leave_cut(a, w, share, p, head, t0, t1, t0 >= w * share && t1 > seg_end);
+      leave_cut(end, w, share, p, head, t0, t1, t0 >= w * share && t1 > seg_end);
     if (alive) {
       if (cut) {
         const int64_t at = slot * ROWS + wave * 32 + l32;
@@ -443,23 +454,23 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
         for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<float4_t*>(a.part_o + at * DP + i * 32 + e * 8 + h * 4) =
+            *reinterpret_cast<float4_t*>(end.part_o + at * DP + i * 32 + e * 8 + h * 4) =
                 float4_t{t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
         if (h == 0) {
-          a.part_ml[at * 2] = t.top();
-          a.part_ml[at * 2 + 1] = l;
+          end.part_ml[at * 2] = t.top();
+          end.part_ml[at * 2 + 1] = l;
         }
       } else {
         const float f = row_factor(l, sees);
-        uint16_t* dst = out_row(a, p.r, head, row0 + l32);
+        uint16_t* dst = out_row(end, p.r, head, row0 + l32);
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float v[4] = {t.o[i][4 * e] * f, t.o[i][4 * e + 1] * f, t.o[i][4 * e + 2] * f, t.o[i][4 * e + 3] * f};
-            store4(a, dst, i * 32 + e * 8 + h * 4, v);
+            store4(end, dst, i * 32 + e * 8 + h * 4, v);
           }
-        if (h == 0 && a.lse != nullptr) a.lse[lse_at(a, p.r, head, row0 + l32)] = row_lse(t.top(), l, sees);
+        if (h == 0 && end.lse != nullptr) end.lse[lse_at(end, p.r, head, row0 + l32)] = row_lse(t.top(), l, sees);
       }
     }
     uint64_t broken = __ballot(alive && t.broken());
@@ -471,11 +482,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       while (again != 0) {
         const int i = __ffsll((unsigned long long)again) - 1, row = row0 + i;
         again &= again - 1;
-        const Span s = token_span(a, p.r, token_of(a, row));
+        const Span s = token_span(end, p.r, token_of(end, row));
         SlowRow<DP> slow;
-        slow.run(a, query_row(a, p.r, head, row), head_off, pages,
+        slow.run(end, query_row(end, p.r, head, row), head_off, pages,
                  s.begin > lo ? s.begin : lo, s.end < hi ? s.end : hi);
-        slow.template store<ROWS>(a, p.r, head, row, wave * 32 + i, cut ? slot : -1, s.begin < s.end,
+        slow.template store<ROWS>(end, p.r, head, row, wave * 32 + i, cut ? slot : -1, s.begin < s.end,
                                   (broken >> i & 1) != 0);
       }
     }
@@ -644,7 +655,6 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
   auto aligned = [](const HeadsView& v, int bytes) {
     return reinterpret_cast<uintptr_t>(v.p) % bytes == 0 && v.ts % (bytes / 2) == 0 && v.hs % (bytes / 2) == 0;
   };
-  a.q_vec = aligned(p.q, 16);
   a.out_vec = aligned(p.out, 8);
   a.whole_units = p.cache.page_size % 16 == 0 && p.cache.slot_stride < int64_t(1) << 25;
   a.lse = p.lse;
