@@ -267,8 +267,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   if (shared) {
     // Workgroups go to the XCDs in turn, and each XCD has its own L2: its
-    // shares lie side by side, so that they read the keys of few heads (2048
-    // tokens after 6144, 8 heads: one head an XCD; 332 us without).
+    // shares lie side by side, so that they read the keys of few heads.  A
+    // compute unit gets two of them, half of the XCD's shares apart: the second
+    // half runs backwards, so that a share with a prompt's last tiles, which
+    // see the most keys, meets one with its first.
     if (given.parts % kXcds == 0) {
       const int per = given.parts / kXcds;
       int v = (int)w / kXcds;
