@@ -286,6 +286,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     pos_end = tile < head_len ? pos + 1 : pos;
   }
   if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(given, w, share, Place{}, 0, 0, 0, false);
+  if constexpr (!FULL) {
+    clear_lds<DP>(ring + wave * (64 * DP), 64);
+    __syncthreads();
+  }
   while (pos < pos_end) {
     const AttentionArgs a = fresh_args();
     const int head = (int)quotient(pos, head_len);
@@ -330,10 +334,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     const int32_t* pages = a.pages + p.b * a.page_row_stride;
     const int64_t head_off = head * a.head_stride;
 
-    if constexpr (!FULL) {
-      clear_lds<DP>(ring + wave * (64 * DP), 64);
-      __syncthreads();
-    }
     WaveTile<DP, 1> t;
     auto page_at = [&](int k) {
       const int j = k + wave * 16 + lane % 16;
@@ -611,7 +611,7 @@ hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipSt
   if ((e = prepare_kernel(k_attention_tile<DP, FULL>)) != hipSuccess) return e;
   e = launch_kernel(k_attention_tile<DP, FULL>, dim3((unsigned)blocks), dim3(256), 512 * DP + 16, stream, a);
   if (e != hipSuccess || !shared) return e;
-  return launch_kernel(k_attention_join<DP, 128, 8>, dim3((unsigned)blocks - 1, 8), dim3(256), 0, stream, a);
+  return launch_kernel(k_attention_join<DP, 128, 16>, dim3((unsigned)blocks - 1, 16), dim3(256), 0, stream, a);
 }
 
 }  // namespace
