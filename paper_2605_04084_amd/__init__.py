@@ -315,8 +315,8 @@ def _stream_of(device: int) -> int:
 def _on_device(device: int, fn, *args) -> int:
     """``fn(*args, stream)`` with that device current."""
     torch = _torch()
-    if torch.cuda.current_device() == device:
-        return fn(*args, _stream_of(device))
+    if torch._C._cuda_getDevice() == device:  # there is a tensor on it, so torch's runtime is up
+        return fn(*args, torch._C._cuda_getCurrentRawStream(device))
     with torch.cuda.device(device):
         return fn(*args, _stream_of(device))
 
@@ -659,13 +659,13 @@ def _kv_cache(k_cache, v_cache, device, Hkv=None, D=None):
     return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size, strides[0], strides[1], strides[2])
 
 
-def _workspace(workspace, need, device):
-    """The workspace to use and its bytes: the caller's, or a new one."""
+def _workspace(workspace, need, device, like):
+    """The workspace to use and its bytes: the caller's, or a new one on the tensor ``like``'s device."""
     if workspace is None:
         if need <= 0:
             return None, 0
         torch = _torch()
-        return torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", device)), need
+        return like.new_empty(need, dtype=torch.uint8), need
     if not (workspace.is_cuda and workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous device tensor")
     _same_device(device, workspace)
@@ -763,7 +763,7 @@ def rope_append(q, k, v, table, positions, slots, k_cache, v_cache, interleaved:
     cache = None
     if q is not None:
         if out is None:
-            out = q.new_empty((T, Hq, D))
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
             _check_rows(out, "out", f16, q.shape, device)
         qs, qos = q.stride(), out.stride()
@@ -829,7 +829,7 @@ def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional
     if kv_len.get_device() != device or pages.get_device() != device:
         _same_device(device, kv_len, pages)
     if out is None:
-        out = q.new_empty((T, Hq, D))
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
         _check_rows(out, "out", torch.float16, q.shape, device)
     lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if return_lse else None
@@ -838,7 +838,7 @@ def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional
 
     def call(stream):
         need = L.fasq_paged_attention_workspace_bytes(T, B, Hq, Hkv, D) if workspace is None else 0
-        ws, ws_bytes = _workspace(workspace, need, device)
+        ws, ws_bytes = _workspace(workspace, need, device, q)
         return L.fasq_paged_attention(q.data_ptr(), qs[0], qs[1], T, Hq, cache, Hkv, D, pages.data_ptr(),
                                       pages.stride(0), pages.shape[1], q_start.data_ptr(), kv_len.data_ptr(), B,
                                       D ** -0.5 if scale is None else scale, causal, window, out.data_ptr(), os_[0],
@@ -856,7 +856,8 @@ def residual_norm(x, y=None, weight=None, eps: float = 1e-5, post_weight=None, g
     [M x N].  Returns ``(x_new, h)``; ``x_new`` is None without ``y`` (unless
     ``x_out`` is given), ``h`` is None without ``weight``.  See
     ``fasq_residual_norm``."""
-    f16 = _torch().float16
+    torch = _torch()
+    f16 = torch.float16
     _require(x, "x", f16, 2)
     shape = x.shape
     M, N = shape
@@ -865,7 +866,7 @@ def residual_norm(x, y=None, weight=None, eps: float = 1e-5, post_weight=None, g
     if y is not None:
         _check_tensor(y, "y", f16, shape, device)
         if x_out is None:
-            x_out = x.new_empty(shape)
+            x_out = torch.empty_like(x)
         else:
             _check_tensor(x_out, "x_out", f16, shape, device)
     elif x_out is not None:
@@ -873,7 +874,7 @@ def residual_norm(x, y=None, weight=None, eps: float = 1e-5, post_weight=None, g
     if weight is not None:
         _check_tensor(weight, "weight", f16, (N,), device)
         if out is None:
-            out = x.new_empty(shape)
+            out = torch.empty_like(x)
     if out is not None:
         _check_tensor(out, "out", f16, shape, device)
     if post_weight is not None:
@@ -925,7 +926,7 @@ def lora_batched(x, adapters, As, Bs, scales, bases, outs=None, workspace=None):
         else:
             base_ptrs.append(0)
         if outs is None:
-            y = x.new_empty((M, N))
+            y = x.new_empty((M, N)) if base is None else torch.empty_like(base)
         else:
             y = outs[i]
             _check_tensor(y, f"out[{i}]", f16, (M, N), device)
@@ -941,7 +942,7 @@ def lora_batched(x, adapters, As, Bs, scales, bases, outs=None, workspace=None):
 
     def call(stream):
         need = c.fasq_lora_workspace_bytes(M, K, r, n) if workspace is None else 0
-        ws, ws_bytes = _workspace(workspace, need, device)
+        ws, ws_bytes = _workspace(workspace, need, device, x)
         return c.fasq_lora_batched(x.data_ptr(), M, K, adapters.data_ptr(), L, r, scales.data_ptr(), n, at, at + step,
                                    at + 2 * step, at + 3 * step, at + 4 * step, _ptr(ws), ws_bytes, stream)
 
