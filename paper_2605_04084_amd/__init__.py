@@ -910,26 +910,32 @@ def lora_batched(x, adapters, As, Bs, scales, bases, outs=None, workspace=None):
     L, n = scales.shape[0], len(As)
     if not (len(Bs) == len(bases) == n and (outs is None or len(outs) == n)) or n < 1:
         raise ValueError("As, Bs, bases and outs must have equal lengths, at least 1")
+    Tensor = torch.Tensor
     r, ys, sizes, a_ptrs, b_ptrs, base_ptrs, y_ptrs = -1, [], [], [], [], [], []
     for i in range(n):
         A, B, base = As[i], Bs[i], bases[i]
         if r < 0:
             _require(A, "A[0]", f16, 3)
             r = A.shape[1]
-        _require(B, f"B[{i}]", f16, 3)
-        N = B.shape[1]
-        _check_tensor(A, f"A[{i}]", f16, (L, r, K), device)
-        _check_tensor(B, f"B[{i}]", f16, (L, N, r), device)
-        if base is not None:
+        N = B.shape[1] if isinstance(B, Tensor) and B.dim() == 3 else -1
+        # what _check_tensor asks, of both at once: this loop is most of a short call
+        if not (N >= 0 and isinstance(A, Tensor) and A.dtype is f16 and B.dtype is f16 and A.shape == (L, r, K)
+                and B.shape == (L, N, r) and A.get_device() == device and B.get_device() == device
+                and A.is_contiguous() and B.is_contiguous()):
+            _require(B, f"B[{i}]", f16, 3)
+            _check_tensor(A, f"A[{i}]", f16, (L, r, K), device)
+            _check_tensor(B, f"B[{i}]", f16, (L, N, r), device)
+        if base is None:
+            base_ptrs.append(0)
+        else:
             _check_tensor(base, f"base[{i}]", f16, (M, N), device)
             base_ptrs.append(base.data_ptr())
-        else:
-            base_ptrs.append(0)
         if outs is None:
             y = x.new_empty((M, N)) if base is None else torch.empty_like(base)
         else:
             y = outs[i]
-            _check_tensor(y, f"out[{i}]", f16, (M, N), device)
+            if y is not base:
+                _check_tensor(y, f"out[{i}]", f16, (M, N), device)
         ys.append(y)
         sizes.append(N)
         a_ptrs.append(A.data_ptr())
