@@ -2,7 +2,7 @@
 // y = base + s_a B_a (A_a x), two or three launches.
 //
 //   k_lora_down  t = A_a x, fp32 in the workspace, K split over workgroups
-//   k_lora_fold  beyond 128 tokens: t summed over the splits and in the form
+//   k_lora_fold  beyond 128 tokens and 16 ranks: t summed over the splits and in the form
 //                the matrix cores take, which k_lora_up makes itself otherwise
 //   k_lora_up    y = base + s_a B_a t, one pass over the projection's output
 //
@@ -462,9 +462,13 @@ int64_t up_to(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
 LoraPlan plan_lora(int64_t M, int64_t K, int r, int count, const DeviceInfo& dev) {
   LoraPlan p;
-  // more tokens share what a block reads of an adapter
-  p.TD = M > 512 ? 32 : 16;
-  p.TU = M > 128 ? 128 : 16;
+  // More tokens share what a block reads of an adapter (700 tokens 30.5 us,
+  // 31.8 with blocks of 16; 37 tokens 12.4, 12.7 with blocks of 32).
+  p.TD = M > 64 ? 32 : 16;
+  // Up to 16 ranks a workgroup sums its few low-rank values itself (1000 tokens
+  // of 16 ranks 24.8 us, 32.8 folded in blocks of 128; 400 tokens of 64 ranks
+  // 50 and 40).
+  p.TU = M > 128 && r > 16 ? 128 : 16;
   p.RT = r <= 16 ? 1 : r <= 32 ? 2 : 4;
   // splits of at least 512 values, up to a workgroup a compute unit
   const int64_t wide = up_to(M, p.TD) * count * up_to(r, 16 * p.RT);
@@ -556,19 +560,25 @@ hipError_t launch_lora(const LoraProblem& p, const DeviceInfo& dev, hipStream_t 
   }
   // several slices share what a workgroup makes of the low-rank values, where
   // enough workgroups are left
-  const int64_t blocks = up_to(p.M, pl.TU) * p.count, slices = up_to(most_n, kSlice);
+  const int64_t slices = up_to(most_n, kSlice);
+  // blocks of 64 where those of 128 leave compute units without work (200 tokens
+  // of 64 ranks 29.6 us, 34 with 128; 1000 tokens 79 and 71)
+  int64_t all_slices = 0;
+  for (int i = 0; i < p.count; ++i) all_slices += up_to(p.N[i], kSlice);
+  const int TU = pl.TU > 16 && 2 * up_to(p.M, 128) * all_slices < 3 * dev.num_cus ? 64 : pl.TU;
+  const int64_t blocks = up_to(p.M, TU) * p.count;
   a.slices = 1;
   while (a.slices < 8 && blocks * up_to(slices, 2 * a.slices) >= 4 * dev.num_cus) a.slices *= 2;
-  const int64_t tu = up_to(p.M, pl.TU), ny = up_to(slices, a.slices);
-  a.J = sharers(p.M, p.L, pl.TU, tu * ny * a.count, dev);
+  const int64_t tu = up_to(p.M, TU), ny = up_to(slices, a.slices);
+  a.J = sharers(p.M, p.L, TU, tu * ny * a.count, dev);
   const dim3 up((unsigned)tu, (unsigned)ny, (unsigned)(a.count * a.J));
-  if (pl.TU == 16)
+  if (TU == 16)
     return a.r <= 16   ? launch_up<16, 1>(a, up, vec_r, stream)
            : a.r <= 64 ? launch_up<16, 4>(a, up, vec_r, stream)
                        : launch_up<16, 16>(a, up, vec_r, stream);
-  return a.r <= 16   ? launch_up<128, 1>(a, up, vec_r, stream)
-         : a.r <= 64 ? launch_up<128, 4>(a, up, vec_r, stream)
-                     : launch_up<128, 16>(a, up, vec_r, stream);
+  if (TU == 64)
+    return a.r <= 64 ? launch_up<64, 4>(a, up, vec_r, stream) : launch_up<64, 16>(a, up, vec_r, stream);
+  return a.r <= 64 ? launch_up<128, 4>(a, up, vec_r, stream) : launch_up<128, 16>(a, up, vec_r, stream);
 }
 
 }  // namespace fasq

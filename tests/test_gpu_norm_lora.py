@@ -245,3 +245,22 @@ def test_lora_binding_refuses():
         with pytest.raises(error):
             fasq.lora_batched(**{**ok, **change})
     assert tuple(fasq.lora_batched(h(0, 16), ids[:0], ok["As"], ok["Bs"], scales, [h(0, 8)])[0].shape) == (0, 8)
+
+
+@pytest.mark.parametrize("M,K,Ns,r,L,ids", [
+    # blocks of 128 tokens (many features), of 64 and of 16, each beyond 128 tokens
+    (1030, 128, (22016,), 40, 3, "blocks"),
+    (1025, 136, (11011, 11003), 33, 4, "random"),
+    (1030, 72, (22016,), 130, 3, "random"),
+    (1000, 256, (520, 64), 17, 6, "random"),
+    (193, 1000, (1531,), 20, 3, "random"),
+    (320, 200, (136,), 129, 2, "blocks"),
+    (1000, 333, (264, 5), 16, 5, "random"),
+    (2051, 64, (72,), 1, 9, "blocks"),
+])
+def test_lora_blocks(M, K, Ns, r, L, ids):
+    case = _lora_case(M, K, Ns, r, L, ids)
+    got = _run_lora(*case)
+    _check_lora(case, got)
+    again = _run_lora(*case)
+    assert all(np.array_equal(a.view(np.uint16), b.view(np.uint16)) for a, b in zip(got, again))
