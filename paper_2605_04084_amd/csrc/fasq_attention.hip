@@ -583,14 +583,22 @@ AttentionPlan plan_attention(int64_t T, int64_t B, int Hq, int Hkv, int D, const
   AttentionPlan p;
   const int64_t G = Hq / Hkv, rows = T * G;
   p.DP = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  // up to 32 rows of a request on average: a tile of 32
-  p.few = rows <= 32 * B;
+  // Tiles of 32 rows for up to 32 of a request on average (16 requests of one
+  // token 37 us, 42 in tiles of 128), or 64 in all: keys split further make up
+  // for keys read twice (16 tokens of one request on 4000 keys 20 us, 35; on
+  // 40000 keys 71, 65; 32 tokens there 117, 71).
+  p.few = rows <= 32 * B || rows <= 64;
   p.rows = p.few ? 32 : 128;
-  p.tiles = rows / p.rows + (B < T ? B : T);
-  // workgroups that the chip holds at once (by LDS)
+  p.tiles = (rows + (p.rows - 1) * (B < T ? B : T)) / p.rows;
+  // Workgroups that the chip holds at once (by LDS).  16 requests of one token,
+  // 64 dimensions: 23.2 us with two a compute unit, 26.6 with one.
   p.parts = dev.num_cus * (p.few ? (p.DP == 64 ? 2 : 1) : (p.DP == 256 ? 1 : 2));
-  // with twice as many whole tiles as the chip holds a split gains nothing
-  p.split = p.few || rows / p.rows * Hkv < 2 * p.parts;
+  // Whole tiles are left whole where they fill the chip: at least twice (4096
+  // tokens of 32 heads on 8 take 182 us, split 215), or one request's, once
+  // (2048 tokens 67 us, split 71).
+  const int64_t whole = rows / p.rows * Hkv;
+  const bool once = B == 1 && p.tiles * Hkv <= p.parts && 16 * whole >= 15 * p.parts;
+  p.split = p.few || !(once || whole >= 2 * p.parts);
   const int64_t of_share = int64_t(2) * p.rows * (p.DP + 2) * (int64_t)sizeof(float) + (int64_t)sizeof(CutTile);
   p.bytes = p.split ? p.parts * of_share : 0;
   return p;
@@ -598,7 +606,7 @@ AttentionPlan plan_attention(int64_t T, int64_t B, int Hq, int Hkv, int D, const
 
 template <int DP, bool FULL>
 hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipStream_t stream) {
-  constexpr int NW = DP == 256 ? 2 : 4;
+  constexpr int NW = DP == 256 ? 2 : 4, JY = 8;
   const bool shared = a.part_o != nullptr;
   const int64_t blocks = shared ? pl.parts : pl.tiles * a.Hkv;
   hipError_t e;
@@ -606,7 +614,7 @@ hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipSt
     if ((e = prepare_kernel(k_attention_few<DP, NW, FULL>)) != hipSuccess) return e;
     e = launch_kernel(k_attention_few<DP, NW, FULL>, dim3((unsigned)blocks), dim3(NW * kWave), NW * 256 * DP, stream, a);
     if (e != hipSuccess || !shared) return e;
-    return launch_kernel(k_attention_join<DP, 32, 1>, dim3((unsigned)blocks - 1), dim3(256), 0, stream, a);
+    return launch_kernel(k_attention_join<DP, 32, JY>, dim3((unsigned)blocks - 1, JY), dim3(256), 0, stream, a);
   }
   if ((e = prepare_kernel(k_attention_tile<DP, FULL>)) != hipSuccess) return e;
   e = launch_kernel(k_attention_tile<DP, FULL>, dim3((unsigned)blocks), dim3(256), 512 * DP + 16, stream, a);

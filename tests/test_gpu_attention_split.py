@@ -66,3 +66,11 @@ def test_lengths_that_end_on_a_share():
     for kv in range(500, 1700, 37):
         b = Batch([(1, kv), (1, 512), (1, 1024 - kv % 256)], 4, 4, 64, 16, seed=kv)
         b.check(b.run())
+
+
+@pytest.mark.parametrize("n,kv,Hq,Hkv,D", [(1024, 1024, 8, 8, 128), (1024, 1500, 16, 8, 64), (16, 4000, 8, 2, 128),
+                                           (17, 4000, 8, 2, 128), (64, 700, 2, 2, 256), (65, 700, 2, 2, 256)])
+def test_around_the_choices_of_tiles(n, kv, Hq, Hkv, D):
+    """Whole tiles that just fill the chip or do not, and tiles of 32 and of 128 rows."""
+    b = Batch([(n, kv)], Hq, Hkv, D, 16, seed=n)
+    b.check(b.run())
