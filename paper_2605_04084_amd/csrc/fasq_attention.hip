@@ -72,13 +72,19 @@ __device__ __forceinline__ int64_t share_of(int64_t total, int parts, int least)
 }
 
 constexpr int kXcds = 8;
-constexpr int kFewShare = 128;   // keys a share has at least
+// Keys a share has at least.  One token on 1531 keys: 12.1 us with 128, 13.4 with
+// 256.  512 tokens: 33 us with 256, 44 with 384; a ragged batch 49 and 62, and 49
+// with 128.
+constexpr int kFewShare = 128;
 constexpr int kTileShare = 256;
 
 // ---------------------------------------------------------------------------
 // Up to 32 rows: NW waves, each 32 keys at a time with its own two stages of
 // LDS, so that no wave waits for another until the end, where their results
-// are joined in wave order.
+// are joined in wave order.  Bound by the keys and values read: 64 requests of
+// 300 to 8192 keys (8 heads of 128 for 32) take 127 us (633 MB, 5.0 TB/s), two
+// of 65536 to 131072 150 us (5.4 TB/s).  One token on 1531 keys takes 8.5 us, of
+// which reading lengths, finding its keys and the first copies are the most.
 // ---------------------------------------------------------------------------
 template <int DP, int NW, bool FULL>
 __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) {
@@ -249,6 +255,12 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
 
 // ---------------------------------------------------------------------------
 // 128 rows: four waves of 32 rows over shared tiles of 64 keys, two stages.
+// Bound by what one wave does in turn (see WaveTile::block): 2048 tokens after
+// 6144, 32 heads of 128 on 8, take 279 us (241 GFLOP, 862 TFLOP/s; the matrix
+// cores are busy 56 % of the time, at 1.74 GHz).  Copies left out, that would be
+// 30 us less, LDS reads left out as well as much, the maximum 12, the sum of
+// the weights 10.  64 rows a wave would halve the LDS reads, but leave one wave
+// a SIMD.  A tile costs 10 us besides its keys.
 // ---------------------------------------------------------------------------
 template <int DP, bool FULL>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(AttentionArgs) {
@@ -267,10 +279,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   if (shared) {
     // Workgroups go to the XCDs in turn, and each XCD has its own L2: its
-    // shares lie side by side, so that they read the keys of few heads.  A
-    // compute unit gets two of them, half of the XCD's shares apart: the second
-    // half runs backwards, so that a share with a prompt's last tiles, which
-    // see the most keys, meets one with its first.
+    // shares lie side by side, so that they read the keys of few heads (2048
+    // tokens after 6144 in shares: 285 us, 296 without).  A compute unit gets
+    // two of them, half of the XCD's shares apart: the second half runs
+    // backwards, so that a share with a prompt's last tiles, which see the most
+    // keys, meets one with its first (2048 tokens in shares: 69 us, 75 without).
     if (given.parts % kXcds == 0) {
       const int per = given.parts / kXcds;
       int v = (int)w / kXcds;
@@ -399,8 +412,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
         barrier_only();   // everyone's; nobody reads what is overwritten now
         // The next copies: one every third step below, since memory takes a
         // copy in 16 cycles and the eight waves of a compute unit would stand
-        // in line for it here (1784 of 5370 cycles a tile); all at once where
-        // keys lie in several pages or past the end.
+        // in line for it here (2048 tokens after 6144: 324 us, spread 291 at
+        // the time); all at once where keys lie in several pages or past the end.
         const int kk = k0 + 2 * STEP + wave * 16;
         const bool spread = copy.whole(a, kk, span.begin, hi - 1);  // then the values' unit is whole too
         const uint16_t *from_k = a.ck + off_k, *from_v = a.cv + off_v;
@@ -500,7 +513,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 // ---------------------------------------------------------------------------
 // Joins the shares of one cut tile: workgroup x takes the one that starts in
 // share x, y cuts the tile's rows.  Shares are added in their order, by groups
-// of threads that take every PG-th share where there are few rows.
+// of threads that take every so-manieth share where there are few rows.  4.6 us
+// for one token on 1531 keys, 6.6 for two on 131072, 7.4 for a ragged batch of
+// 25 requests, mostly the launch.
 // ---------------------------------------------------------------------------
 template <int DP, int ROWS, int YS>
 __global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a) {
