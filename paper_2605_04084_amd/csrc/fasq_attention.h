@@ -566,11 +566,25 @@ struct WaveTile {
   }
   static constexpr int SCORED = MIXED ? N / 2 * 3 - 2 : N - 1;  // the last step with the keys
 
-  // The operand of step i.
-  __device__ __forceinline__ void read_op(uint32_t k_at, const uint32_t (&v_at)[2], int i) {
+  // This lane's addresses of the operands in the first rows of LDS; stages and
+  // blocks of rows are constant offsets from there.
+  struct Lanes {
+    uint32_t k[N < 8 ? N : 8], v[2][DP / 32 < 4 ? DP / 32 : 4];
+    __device__ __forceinline__ explicit Lanes(const uint16_t* first) {
+#pragma unroll
+      for (int t = 0; t < N && t < 8; ++t) k[t] = key_lane(first) ^ (t * 32);
+#pragma unroll
+      for (int d = 0; d < DP / 32 && d < 4; ++d)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) v[j][d] = value_lane(first, j) ^ (d * 64);
+    }
+  };
+
+  // The operand of step i: keys and values at these byte offsets.
+  __device__ __forceinline__ void read_op(const Lanes& at, uint32_t k_off, uint32_t v_off, int i) {
     if (is_key(i)) {
       const int t = nth(i);
-      ops[i % OPS] = __builtin_bit_cast(u32x4, *(lds_half8)(uintptr_t)((k_at ^ (t % 8 * 32)) + t / 8 * 256));
+      ops[i % OPS] = __builtin_bit_cast(u32x4, *(lds_half8)(uintptr_t)(at.k[t % 8] + (k_off + t / 8 * 256)));
       return;
     }
     const int u = nth(i) / (DP / 32), d = nth(i) % (DP / 32);
@@ -578,7 +592,7 @@ struct WaveTile {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       part[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_short4)(uintptr_t)((v_at[j] ^ (d % 4 * 64)) + d / 4 * 256 + u * 16 * DP * 2));
+          (lds_short4)(uintptr_t)(at.v[j][d % 4] + (v_off + d / 4 * 256 + u * 16 * DP * 2)));
     ops[i % OPS] = __builtin_bit_cast(u32x4, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }
 
@@ -663,14 +677,13 @@ struct WaveTile {
   }
 
   // One block: the weights `made` of its scores s, the scores `next` of the
-  // block at k_at, the values at v_at weighted with `p`, and next's largest score
+  // block at k_off, the values at v_off weighted with `p`, and next's largest score
   // of the row (top) and by how much it passes the maximum (over).  The operands
   // of the first three steps are there; those of the block after this one are
-  // read if `more` (at k_more, v_more).  at_step(i): what else step i issues.
+  // read if `more` (32 rows further).  at_step(i): what else step i issues.
   template <typename F>
   __device__ __forceinline__ void block(const float16_t& s, float16_t& next, const half8_t (&p)[2], half8_t (&made)[2],
-                                        uint32_t k_at, const uint32_t (&v_at)[2], bool more, uint32_t k_more,
-                                        const uint32_t (&v_more)[2], float c,
+                                        const Lanes& at, uint32_t k_off, uint32_t v_off, bool more, float c,
                                         float& top, float& over, F at_step) {
     constexpr int STEPS = 2 * N;
     float w[16];
@@ -688,8 +701,8 @@ struct WaveTile {
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       const int j = i + OPS - 1;
-      if (j < STEPS) read_op(k_at, v_at, j);
-      else if (more) read_op(k_more, v_more, j - STEPS);
+      if (j < STEPS) read_op(at, k_off, v_off, j);
+      else if (more) read_op(at, k_off + 32 * DP * 2, v_off + 32 * DP * 2, j - STEPS);
       __builtin_amdgcn_sched_barrier(0);
       const half8_t op = __builtin_bit_cast(half8_t, ops[i % OPS]);
       if (is_key(i)) next = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, q[nth(i)], i == 0 ? float16_t{} : next, 0, 0, 0);

@@ -401,8 +401,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       t.settle(s0, top, (top - t.m) * a.c, p1, lo, mine.begin, mine.end, masked(lo), a.c);
       t.weights(s0, p0, a.c);
       t.settle(s1, top1, (top1 - t.m) * a.c, p0, lo + 32, mine.begin, mine.end, masked(lo + 32), a.c);
-      int stage = 0;
-      for (int k0 = lo; k0 < hi; k0 += STEP, stage ^= 1) {
+      const typename WaveTile<DP, 1>::Lanes lanes(ring);
+      auto turn = [&](int k0, int stage) __attribute__((always_inline)) {
         // here: values of tile k0 in `stage`, keys of the next in the other
         // one; p0, s1: weights and scores of the tile's two blocks
         wait_lds();
@@ -435,24 +435,24 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
           if (n < C) copy.one(from_k, n, to_k);
           else copy.one(from_v, n - C, to_v);
         };
-        const uint32_t kn = WaveTile<DP, 1>::key_lane(ring + (stage ^ 1) * (64 * DP));
-        uint32_t v[2], v32[2];
+        const uint32_t k_off = (stage ^ 1) * (64 * DP * 2), v_off = (2 + stage) * (64 * DP * 2), next = 32 * DP * 2;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          v[j] = WaveTile<DP, 1>::value_lane(vring + stage * (64 * DP), j);
-          v32[j] = v[j] + 32 * DP * 2;
-        }
-#pragma unroll
-        for (int i = 0; i < WaveTile<DP, 1>::OPS - 1; ++i) t.read_op(kn, v, i);
+        for (int i = 0; i < WaveTile<DP, 1>::OPS - 1; ++i) t.read_op(lanes, k_off, v_off, i);
         float over = 0.f;
-        t.block(s1, s0, p0, p1, kn, v, true, kn + 32 * DP * 2, v32, a.c, top, over, at_step);
+        t.block(s1, s0, p0, p1, lanes, k_off, v_off, true, a.c, top, over, at_step);
         t.settle(s0, top, over, p1, k0 + STEP, mine.begin, mine.end, masked(k0 + STEP), a.c);
-        t.block(s0, s1, p1, p0, kn + 32 * DP * 2, v32, false, 0, v32, a.c, top, over,
+        t.block(s0, s1, p1, p0, lanes, k_off + next, v_off + next, false, a.c, top, over,
                 [&](int i) { at_step(i + DP / 8); });
         t.settle(s1, top, over, p0, k0 + STEP + 32, mine.begin, mine.end, masked(k0 + STEP + 32), a.c);
         page_v = page[0];
         page[0] = page[1];
         page[1] = page[2];
+      };
+      // the stages are constants in each half of the loop
+      for (int k0 = lo; k0 < hi; k0 += 2 * STEP) {
+        turn(k0, 0);
+        if (k0 + STEP >= hi) break;
+        turn(k0 + STEP, 1);
       }
       wait_loads<0>();  // copies behind the end
     }
