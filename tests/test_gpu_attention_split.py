@@ -74,3 +74,10 @@ def test_around_the_choices_of_tiles(n, kv, Hq, Hkv, D):
     """Whole tiles that just fill the chip or do not, and tiles of 32 and of 128 rows."""
     b = Batch([(n, kv)], Hq, Hkv, D, 16, seed=n)
     b.check(b.run())
+
+
+@pytest.mark.parametrize("n,kv,B,window,D", [(300, 300, 1, 0, 128), (500, 2000, 1, 100, 64), (200, 900, 4, 33, 96),
+                                             (150, 150, 1, 0, 256), (700, 1000, 1, 200, 256)])
+def test_short_tiles_stay_whole(n, kv, B, window, D):
+    b = Batch([(n, kv)] * B, 4, 2, D, 16, seed=n)
+    b.check(b.run(window=window), window=window)
