@@ -546,7 +546,7 @@ struct WaveTile {
   // weighted values of block b - 1.  The two do not depend on each other, and
   // one step is one MFMA (32 cycles), its share of the block's 16 scores per
   // lane, and the LDS reads of an operand three steps ahead.  A step takes a
-  // wave about 80 cycles whether or not another wave shares the SIMD: the
+  // wave 70 to 80 cycles whether or not another wave shares the SIMD: the
   // exponential, the LDS read, the copies and the wait for the last sum add up in
   // it; two waves, which is what the registers allow, do not disturb each other.
   // -------------------------------------------------------------------------

@@ -256,11 +256,11 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
 // ---------------------------------------------------------------------------
 // 128 rows: four waves of 32 rows over shared tiles of 64 keys, two stages.
 // Bound by what one wave does in turn (see WaveTile::block): 2048 tokens after
-// 6144, 32 heads of 128 on 8, take 279 us (241 GFLOP, 862 TFLOP/s; the matrix
-// cores are busy 56 % of the time, at 1.74 GHz).  Copies left out, that would be
-// 30 us less, LDS reads left out as well as much, the maximum 12, the sum of
-// the weights 10.  64 rows a wave would halve the LDS reads, but leave one wave
-// a SIMD.  A tile costs 10 us besides its keys.
+// 6144, 32 heads of 128 on 8, take 259 us (241 GFLOP, 928 TFLOP/s; the matrix
+// cores are busy about 60 % of the time, at 1.74 GHz).  Of 285 us the copies
+// were 30, the LDS reads 30, the maximum 12, the sum of the weights 10 (each
+// left out, for timing).  64 rows a wave would halve the LDS reads, but leave
+// one wave a SIMD.  A tile costs 10 us besides its keys.
 // ---------------------------------------------------------------------------
 template <int DP, bool FULL>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(AttentionArgs) {
