@@ -665,7 +665,11 @@ def _workspace(workspace, need, device, like):
         if need <= 0:
             return None, 0
         torch = _torch()
-        return like.new_empty(need, dtype=torch.uint8), need
+        workspace = like.new_empty(need, dtype=torch.uint8)
+        kept = getattr(_recording, "kept", None)
+        if kept is not None:  # the recorded launches name it after this call has returned
+            kept.append(workspace)
+        return workspace, need
     if not (workspace.is_cuda and workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous device tensor")
     _same_device(device, workspace)
@@ -960,19 +964,24 @@ def lora_batched(x, adapters, As, Bs, scales, bases, outs=None, workspace=None):
 # Launch lists
 # ---------------------------------------------------------------------------
 
+_recording = threading.local()  # .kept: the workspaces of the list that this thread records
+
+
 class LaunchList:
     """The kernel launches of a sequence of fasq calls, recorded once and
     queued again with :meth:`run` (``fasq_launch_list_*``).
 
     Calls made on this thread inside ``with lst:`` (or between :meth:`begin`
     and :meth:`end`) are checked and planned as usual but only recorded; the
-    buffers they name must stay alive while the list may run.
+    buffers they name must stay alive while the list may run.  A workspace that
+    a call allocates by itself is kept by the list until it is closed.
     """
 
     def __init__(self):
         h = _c_vp()
         _check(lib().fasq_launch_list_create(ctypes.byref(h)))
         self._h = h
+        self._kept = []
 
     @property
     def handle(self) -> int:
@@ -981,9 +990,11 @@ class LaunchList:
 
     def begin(self) -> None:
         _check(lib().fasq_launch_list_begin(self._live()))
+        _recording.kept = self._kept
 
     def end(self) -> None:
         _check(lib().fasq_launch_list_end(self._live()))
+        _recording.kept = None
 
     def __enter__(self) -> "LaunchList":
         self.begin()
@@ -1008,6 +1019,9 @@ class LaunchList:
     def close(self) -> None:
         if self._h is not None and self._h.value:
             lib().fasq_launch_list_destroy(self._h)
+            if getattr(_recording, "kept", None) is self._kept:
+                _recording.kept = None
+            self._kept = []
         self._h = None
 
     def __del__(self):

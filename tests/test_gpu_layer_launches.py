@@ -201,3 +201,25 @@ def test_another_stream(name):
         case.call(case.outputs)
     torch.cuda.current_stream().wait_stream(stream)
     _same(case, want)
+
+
+@pytest.mark.parametrize("name", ["lora-few", "lora-many", "attention-few", "attention-tile"])
+def test_launch_list_keeps_its_workspaces(name):
+    """A workspace that a recorded call allocated is no other tensor's memory
+    while the list may run."""
+    case = MAKE[name]()
+    want = _direct(case)
+    size = case.ws.numel()
+    case.ws = None  # the calls allocate their own
+    torch.cuda.synchronize()
+    lst = fasq.LaunchList()
+    with lst:
+        case.call(case.outputs)
+    # tensors that would take its place
+    others = [torch.full((size,), 255, dtype=torch.uint8, device="cuda:0") for _ in range(3)]
+    for _ in range(2):
+        lst.run()
+        _same(case, want)
+    for t in others:
+        assert bool((t == 255).all())
+    lst.close()
