@@ -270,7 +270,7 @@ __global__ __launch_bounds__(256, 2) void k_lora_up(LoraArgs a) {
   extern __shared__ uint8_t smem[];
   const int j = scalar(blockIdx.z / a.count), i = blockIdx.z - j * a.count;
   const LoraProjection& p = a.p[i];
-    const int n_block = blockIdx.y * (kSlice * a.slices);
+  const int n_block = blockIdx.y * (kSlice * a.slices);
   if (n_block >= p.N) return;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l16 = lane % 16, g = lane / 16;
