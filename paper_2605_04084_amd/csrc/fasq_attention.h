@@ -156,7 +156,9 @@ __device__ __forceinline__ int64_t tile_length(const AttentionArgs& a, const Req
   if (!shared) return 1;
   int keys = r.kv;
   if (a.window > 0) {
-    const int most = a.window + token_of(a, ROWS) + 32;  // of the tile's tokens, from a multiple of 32 on
+    // of the tile's tokens, from a multiple of 32 on; without causality the
+    // request's first token sees the window before it and all that follows
+    const int most = a.window + (a.causal ? token_of(a, ROWS) : r.n) + 32;
     keys = keys < most ? keys : most;
   }
   return keys <= STEP ? STEP : ((int64_t)keys + STEP - 1) / STEP * STEP;

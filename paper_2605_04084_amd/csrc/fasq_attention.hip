@@ -297,7 +297,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     if (given.B == 1) {
       const Request one = {uniform(batch.first.q0), uniform(batch.first.n), uniform(batch.first.kv)};
       length = tile_length<ROWS, STEP>(given, one, true);
-    } else if (given.window > 0) {
+    } else if (given.window > 0 && given.causal) {  // the longest there can be
       length = tile_length<ROWS, STEP>(given, Request{0, 0, INT32_MAX}, true);
     }
     const bool whole = length > 0 && length * DP <= 384 * 128;
