@@ -481,7 +481,7 @@ def pq_encode(w, d: int, idx_bits: int, init_codebook, iters: int, workspace=Non
     if need < 0:
         raise ValueError("invalid encoder sizes")
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=w.device)
+        workspace, _ = _workspace(None, need, w.get_device(), w)
     elif not (workspace.is_cuda and workspace.is_contiguous() and workspace.numel() * workspace.element_size() >= need):
         raise ValueError(f"workspace must be a contiguous device tensor of at least {need} bytes")
     if init_codebook.device != w.device or workspace.device != w.device:
@@ -544,10 +544,11 @@ def pq_gemv_ex(x, idx, idx_bits: int, d: int, codebook, out=None, workspace=None
     need = gemv_ex_workspace_bytes(M, K, N, idx_bits, d, C, stride)
     if need < 0:
         raise ValueError("invalid sizes")
-    if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    if workspace is None:
+        workspace, ws_bytes = _workspace(None, need, x.get_device(), x)
+    else:
+        ws_bytes = workspace.numel() * workspace.element_size()
     ws_ptr = workspace.data_ptr() if workspace is not None else 0
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     device = x.get_device()
     if idx.get_device() != device or codebook.get_device() != device or out.get_device() != device:
         raise ValueError("all tensors must be on one device")
@@ -576,10 +577,11 @@ def pq_gemm_ex(x, idx, idx_bits: int, d: int, codebook, out=None, workspace=None
     need = gemm_ex_workspace_bytes(M, K, N, idx_bits, d, C) if N and C else 0
     if need < 0:
         raise ValueError("invalid sizes")
-    if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    if workspace is None:
+        workspace, ws_bytes = _workspace(None, need, x.get_device(), x)
+    else:
+        ws_bytes = workspace.numel() * workspace.element_size()
     ws_ptr = workspace.data_ptr() if workspace is not None else 0
-    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
 
     def call(xp, M_, K_, N_, ip, bits, dd, cp, C_, yp, stream):
         return lib().fasq_pq_gemm_ex(xp, M_, K_, N_, ip, bits, dd, cp, C_, yp, ws_ptr, ws_bytes, stream)
@@ -664,9 +666,10 @@ def _workspace(workspace, need, device, like):
     if workspace is None:
         if need <= 0:
             return None, 0
-        torch = _torch()
-        workspace = like.new_empty(need, dtype=torch.uint8)
         kept = getattr(_recording, "kept", None)
+        if kept and kept[-1].numel() >= need and kept[-1].get_device() == device:
+            return kept[-1], need  # the launches of a list follow each other
+        workspace = like.new_empty(need, dtype=_torch().uint8)
         if kept is not None:  # the recorded launches name it after this call has returned
             kept.append(workspace)
         return workspace, need
@@ -973,15 +976,20 @@ class LaunchList:
 
     Calls made on this thread inside ``with lst:`` (or between :meth:`begin`
     and :meth:`end`) are checked and planned as usual but only recorded; the
-    buffers they name must stay alive while the list may run.  A workspace that
-    a call allocates by itself is kept by the list until it is closed.
+    buffers they name must stay alive while the list may run.  The workspace of
+    calls that are given none is the list's: one for all of them, kept until the
+    list is closed and every run that was queued before is over.  So runs of one
+    list follow each other, on one stream or on streams that wait for each
+    other and for the one that was current while it recorded; a graph
+    captured of a run needs the list open; a stream given as a handle outlives the list.
     """
 
     def __init__(self):
         h = _c_vp()
         _check(lib().fasq_launch_list_create(ctypes.byref(h)))
         self._h = h
-        self._kept = []
+        self._kept = []  # workspaces; the last is the largest, earlier launches may name the others
+        self._streams = set()  # handles of the streams that they have been used on
 
     @property
     def handle(self) -> int:
@@ -991,6 +999,7 @@ class LaunchList:
     def begin(self) -> None:
         _check(lib().fasq_launch_list_begin(self._live()))
         _recording.kept = self._kept
+        self._streams.clear()
 
     def end(self) -> None:
         _check(lib().fasq_launch_list_end(self._live()))
@@ -1012,6 +1021,12 @@ class LaunchList:
         elif not isinstance(stream, int):
             stream = stream.cuda_stream
         _check(lib().fasq_launch_list_run(self._live(), stream))
+        if self._kept and stream not in self._streams:
+            # torch's allocator waits for this stream before it hands the memory on
+            cuda = _torch().cuda
+            for w in self._kept:  # ExternalStream takes 0 for a new stream
+                w.record_stream(cuda.ExternalStream(stream, device=w.device) if stream else cuda.default_stream(w.device))
+            self._streams.add(stream)
 
     def __len__(self) -> int:
         return int(lib().fasq_launch_list_size(self._live()))
