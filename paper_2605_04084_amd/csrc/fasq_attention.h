@@ -398,7 +398,8 @@ template <int DP, int KB>
 struct WaveTile {
   half8_t q[DP / 16];
   float16_t o[DP / 32];
-  float m, mc, l;  // running maximum of the scores (this row), m * c (0 without one), sum of this lane's weights
+  float m, mc;  // running maximum of the scores (this row), m * c (0 without one)
+  float l, rest;  // sum of this lane's weights, and what its last addition rounded up
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -407,7 +408,20 @@ struct WaveTile {
       for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
     m = -INFINITY;
     mc = 0.f;
-    l = 0.f;
+    l = rest = 0.f;
+  }
+
+  // A block's weights to the sum.  In fp32 alone, 65536 weights of 2^-24.6 beside one
+  // of 1 leave it at 1: it is held with what each addition rounds (compensated
+  // summation), so that it is off by a few roundings whatever the length.
+  __device__ __forceinline__ void add_block(float sum) {
+    const float more = sum - rest, next = l + more;
+    rest = (next - l) - more;
+    l = next;
+  }
+  __device__ __forceinline__ void scale_sum(float keep) {
+    l *= keep;
+    rest *= keep;
   }
 
   // Row `row` of the request, which exists (lane l and l ^ 32 hold one row;
@@ -509,7 +523,7 @@ struct WaveTile {
       // the weights are 2^(s c - mc) with the rounded product mc, here too
       const float next_c = top * c;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
-      l *= keep;
+      scale_sum(keep);
 #pragma unroll
       for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
@@ -518,14 +532,16 @@ struct WaveTile {
       mc = grown ? next_c : mc;
     }
     half8_t p[2 * KB];
+    float sum = 0.f;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float w = __builtin_amdgcn_exp2f(s[kb][e] * c - mc);
-        l += w;
+        sum += w;
         p[2 * kb + e / 8][e % 8] = static_cast<half_t>(w);
       }
+    add_block(sum);
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
       if (g + 1 < GROUPS) read_v(g + 1);
@@ -628,13 +644,14 @@ struct WaveTile {
 
   // Weights of scores alone.
   __device__ __forceinline__ void weights(const float16_t& s, half8_t (&p)[2], float c) {
+    float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) weight(s, p, e, c);
-  }
-  __device__ __forceinline__ void weight(const float16_t& s, half8_t (&p)[2], int e, float c) {
-    const float w = __builtin_amdgcn_exp2f(s[e] * c - mc);
-    l += w;
-    p[e / 8][e % 8] = static_cast<half_t>(w);
+    for (int e = 0; e < 16; ++e) {
+      const float w = __builtin_amdgcn_exp2f(s[e] * c - mc);
+      sum += w;
+      p[e / 8][e % 8] = static_cast<half_t>(w);
+    }
+    add_block(sum);
   }
 
   // The larger of this lane's value and the other's of its row.
@@ -665,7 +682,7 @@ struct WaveTile {
     if (__any(grown)) {
       const float next_c = top * c;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
-      l *= keep;
+      scale_sum(keep);
 #pragma unroll
       for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
@@ -688,11 +705,11 @@ struct WaveTile {
                                         const Lanes& at, uint32_t k_off, uint32_t v_off, bool more, float c,
                                         float& top, float& over, F at_step) {
     constexpr int STEPS = 2 * N;
-    float w[16];
+    float w[16], sum;
     u32x4 packed[2];
     auto add = [&](int e) {
-      l += w[e];
-      asm volatile("" : "+v"(l));
+      sum = e == 0 ? w[0] : sum + w[e];
+      asm volatile("" : "+v"(sum));
       if (e % 2 == 1) {
         typedef _Float16 pair_t __attribute__((ext_vector_type(2)));
         uint32_t pair = __builtin_bit_cast(uint32_t, pair_t{static_cast<half_t>(w[e - 1]), static_cast<half_t>(w[e])});
@@ -736,6 +753,7 @@ struct WaveTile {
       __builtin_amdgcn_sched_barrier(0);
     }
     add(15);
+    add_block(sum);
     made[0] = __builtin_bit_cast(half8_t, packed[0]);
     made[1] = __builtin_bit_cast(half8_t, packed[1]);
   }

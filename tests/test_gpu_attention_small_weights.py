@@ -1,0 +1,62 @@
+"""paged_attention where most of a row's weight lies in many small weights.
+
+Scores are exact: one key (the sink) stands a given number of powers of two
+above all others.  The tolerance of a logarithm of a sum is test_gpu_attention's:
+2^-20 of the sum of |q| |k| and of itself, a few fp32 roundings, whatever the
+number of keys.
+"""
+
+import math
+
+import numpy as np
+import pytest
+
+from oracle import layer_ops as lo
+from test_gpu_attention import Batch
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+fasq = pytest.importorskip("paper_2605_04084_amd")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    fasq.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+def _sink(n, kv, Hq, D, at):
+    b = Batch([(n, kv)], Hq, 1, D, 64, seed=kv)
+    b.q[:] = 0
+    b.q[..., 0] = 1
+    j = np.arange(kv)
+    k, v = np.zeros((kv, 1, D), np.float16), np.ones((kv, 1, D), np.float16)
+    k[at, :, 0] = 1
+    v[at] = 0
+    v[:, :, 1] *= (j % 7)[:, None] / 8
+    b.k[b.slot(0, j)], b.v[b.slot(0, j)] = k, v
+    return b
+
+
+CASES = pytest.mark.parametrize("n,kv,Hq,D,at,split", [
+    (1, 131072, 2, 64, 0, False), (1, 131072, 2, 64, 70000, True), (1, 40000, 1, 256, 5, False),
+    (100, 131072, 2, 64, 0, False), (100, 30000, 2, 128, 4, True), (70, 20000, 2, 256, 19000, False),
+])
+POWERS = pytest.mark.parametrize("powers", [16.0, 22.4, 24.6, 25.5, 28.0])
+
+
+def _both(b, powers, split):
+    scale = powers * math.log(2.0)
+    kw = {} if split else {"workspace": torch.empty(0, dtype=torch.uint8, device="cuda:0")}
+    return b.run(scale=scale, **kw), lo.paged_attention(b.q, b.k, b.v, b.pages, b.q_start, b.kv_len, scale), scale
+
+
+@POWERS
+@CASES
+def test_sum_of_many_weights_far_below_one(n, kv, Hq, D, at, split, powers):
+    (_, lse), (_, want, _), scale = _both(_sink(n, kv, Hq, D, at), powers, split)
+    assert (np.abs(lse - want) <= 2.0 ** -20 * (scale + np.abs(want) + 1)).all(), float(np.abs(lse - want).max())
