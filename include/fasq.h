@@ -456,6 +456,8 @@ fasq_status fasq_rope_append(const void* q, int64_t q_token_stride, int64_t q_he
  * gets out = 0 and lse = -inf.  Keys and values that a token does not see do
  * not reach its output, whatever they hold (NaN and infinities included), and
  * what is stored past kv_len is never used.
+ * The weights exp(s_j - lse) are rounded to fp16 (relative 2^-12 down to 2^-21
+ * of a token's largest one, in steps of at most 2^-31 of it below).
  *
  *   q, out      fp16 [T x Hq x D] with token and head strides; tokens outside
  *               every request are neither read nor written;

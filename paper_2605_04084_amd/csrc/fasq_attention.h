@@ -394,11 +394,22 @@ __device__ __forceinline__ bool cut_to_finite(uint16_t* values) {
 // ---------------------------------------------------------------------------
 // One wave: 32 rows against KB blocks of 32 keys at a time
 // ---------------------------------------------------------------------------
+
+// Weights enter the second product in fp16, 2^kLift times larger than relative
+// to the running maximum: then they have 11 bits down to 2^-21 of the row's
+// largest, and vanish (while the fp32 sum still counts them) only below 2^-32 of it
+// rather than 2^-25, which a sum over 131072 keys beside one far larger shows.
+// With kLift 7 and a maximum up to 2^8 behind they stay below fp16's largest value, but
+// for scores of 2^25 powers of two and more, whose rounding alone passes it:
+// such rows end not finite and are computed again (SlowRow).
+constexpr float kLift = 7.f;
+
 template <int DP, int KB>
 struct WaveTile {
   half8_t q[DP / 16];
   float16_t o[DP / 32];
-  float m, mc;  // running maximum of the scores (this row), m * c (0 without one)
+  // running maximum of the scores (this row), and m * c - kLift (0 without one)
+  float m, mc;
   float l, rest;  // sum of this lane's weights, and what its last addition rounded up
 
   __device__ __forceinline__ void clear() {
@@ -515,13 +526,13 @@ struct WaveTile {
       const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       top = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
     }
-    // The maximum need not be the newest one: weights up to 2^8 are as exact
-    // in fp16 as weights up to 1, so a row is rescaled only where its maximum
-    // has grown by more than that (each row by its own scores alone).
+    // The maximum need not be the newest one: weights up to 2^15 are as exact
+    // in fp16 as weights up to 2^7, so a row is rescaled only where its maximum
+    // has grown by more than 2^8 (each row by its own scores alone).
     const bool grown = (top - m) * c > 8.f;  // from -inf too; not from -inf to -inf
     if (__any(grown)) {
-      // the weights are 2^(s c - mc) with the rounded product mc, here too
-      const float next_c = top * c;
+      // the weights are 2^(s c - mc) with the rounded mc, here too
+      const float next_c = top * c - kLift;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
       scale_sum(keep);
 #pragma unroll
@@ -680,7 +691,7 @@ struct WaveTile {
     }
     const bool grown = over > 8.f;  // as in step()
     if (__any(grown)) {
-      const float next_c = top * c;
+      const float next_c = top * c - kLift;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
       scale_sum(keep);
 #pragma unroll
@@ -758,7 +769,7 @@ struct WaveTile {
     made[1] = __builtin_bit_cast(half8_t, packed[1]);
   }
 
-  // The maximum as partial results hold it, in powers of two.
+  // What partial results' weights are relative to, in powers of two.
   __device__ __forceinline__ float top() const { return m == -INFINITY ? m : mc; }
 
   // Sum of the row's weights, in both its lanes.

@@ -1,9 +1,13 @@
 """paged_attention where most of a row's weight lies in many small weights.
 
 Scores are exact: one key (the sink) stands a given number of powers of two
-above all others.  The tolerance of a logarithm of a sum is test_gpu_attention's:
-2^-20 of the sum of |q| |k| and of itself, a few fp32 roundings, whatever the
-number of keys.
+above all others, whose values alone are not zero.  The tolerance of a
+logarithm of a sum is test_gpu_attention's: 2^-20 of the sum of |q| |k| and of
+itself, a few fp32 roundings, whatever the number of keys.  Of an output: half
+a unit in the last place; 2^-11 of the weighted sum of |v| for weights held in
+fp16, and 2^-14 of it for fp32 scores and sums; and where weights lie among
+fp16's subnormals a step of 2^-24 at a scale where the row's largest is 2^7 or
+more: 2^-32 of the largest |v| per key.
 """
 
 import math
@@ -60,3 +64,12 @@ def _both(b, powers, split):
 def test_sum_of_many_weights_far_below_one(n, kv, Hq, D, at, split, powers):
     (_, lse), (_, want, _), scale = _both(_sink(n, kv, Hq, D, at), powers, split)
     assert (np.abs(lse - want) <= 2.0 ** -20 * (scale + np.abs(want) + 1)).all(), float(np.abs(lse - want).max())
+
+
+@POWERS
+@CASES
+def test_output_of_many_weights_far_below_one(n, kv, Hq, D, at, split, powers):
+    (out, _), (want, _, mass), _ = _both(_sink(n, kv, Hq, D, at), powers, split)
+    tol = np.abs(want) * 2.0 ** -11 * 1.001 + 2.0 ** -25 + mass * (2.0 ** -11 + 2.0 ** -14) + kv * 2.0 ** -32
+    err = np.abs(out.astype(np.float64) - want)
+    assert (err <= tol).all(), (float((err - tol).max()), float((err / np.maximum(want, 1e-30)).max()))
