@@ -210,6 +210,7 @@ struct LowScale {
   __device__ __forceinline__ explicit LowScale(float top) {
     int e = 0;
     if (top > 0.f && top < INFINITY) frexpf(top, &e);
+    if (top == INFINITY) e = 120;  // nothing finite may become infinite beside it
     e = e < -120 ? -120 : e > 120 ? 120 : e;
     down = ldexpf(1.f, -e);
     power = ldexpf(1.f, e);
