@@ -534,7 +534,8 @@ fasq_status fasq_residual_norm(const void* x, const void* y, int64_t M, int64_t 
  * and y[i][m] = base[i][m] where a lies outside [0, L) (a request without an
  * adapter).  base is what the shared projection gave (fasq_pq_gemv, _gemm and
  * their kin).  The low-rank values A x are fp32 and enter the second product
- * with 22 bits or more, sums are fp32, and y is rounded to fp16 once.
+ * with 22 bits (those below 2^-17 of a token's largest in steps of 2^-38 of it),
+ * sums are fp32, and y is rounded to fp16 once.
  * Adapters of a smaller rank than r are padded with zero rows in A.
  *
  *   x         fp16 [M x K]

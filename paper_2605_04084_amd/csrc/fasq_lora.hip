@@ -203,17 +203,19 @@ __global__ __launch_bounds__(256) void k_lora_down(LoraArgs a) {
 }
 
 // A token's low-rank values for the matrix cores: scaled by a power of two so
-// that the largest lies in [1/2, 1), each is the sum of two fp16 values (the
-// value and what its rounding left: 22 bits).  power: the scale undone.
+// that the largest lies in [2^14, 2^15), each is the sum of two fp16 values (the
+// value and what its rounding left): 22 bits down to 2^-17 of the largest,
+// steps of 2^-38 of it below (with the largest in [1/2, 1) the second value
+// would run out of exponent 15 bits earlier).  power: the scale undone.
 struct LowScale {
   float down, power;
   __device__ __forceinline__ explicit LowScale(float top) {
     int e = 0;
     if (top > 0.f && top < INFINITY) frexpf(top, &e);
     if (top == INFINITY) e = 120;  // nothing finite may become infinite beside it
-    e = e < -120 ? -120 : e > 120 ? 120 : e;
-    down = ldexpf(1.f, -e);
-    power = ldexpf(1.f, e);
+    e = e < -100 ? -100 : e > 120 ? 120 : e;
+    down = ldexpf(1.f, 15 - e);
+    power = ldexpf(1.f, e - 15);
   }
   __device__ __forceinline__ void split(float v, half_t& hi, half_t& lo) const {
     const float x = v * down;
