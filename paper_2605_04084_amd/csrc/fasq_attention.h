@@ -65,6 +65,7 @@ struct AttentionArgs {
   // Split over workgroups (part_o != nullptr): workgroup w of `parts` takes
   // the w-th equal share of the batch's keys; see Place.
   int parts;
+  int64_t first;  // without a split: the launch's first workgroup of all
   float* part_o;  // [2 * parts][rows][DP], not divided by the sum
   float* part_ml;  // [2 * parts][rows][2]: maximum (in powers of two), sum
   CutTile* cuts;   // [parts]

@@ -109,6 +109,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
     pos = w * share;
     pos_end = pos + share < head_len * given.Hkv ? pos + share : head_len * given.Hkv;
   } else {
+    w += given.first;
     const int64_t tile = quotient(w, given.Hkv);
     pos = (w - tile * given.Hkv) * head_len + tile;
     pos_end = tile < head_len ? pos + 1 : pos;
@@ -306,6 +307,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     pos = w * share;
     pos_end = pos + share < head_len * given.Hkv ? pos + share : head_len * given.Hkv;
   } else {
+    w += given.first;
     const int64_t tile = quotient(w, given.Hkv);
     pos = (w - tile * given.Hkv) * head_len + tile;
     pos_end = tile < head_len ? pos + 1 : pos;
@@ -636,6 +638,18 @@ AttentionPlan plan_attention(int64_t T, int64_t B, int Hq, int Hkv, int D, const
   return p;
 }
 
+// All workgroups of a call, in as many launches as they need.
+hipError_t launch_blocks(void (*kernel)(AttentionArgs), int64_t blocks, int threads, size_t lds, hipStream_t stream,
+                         AttentionArgs a) {
+  const int64_t most = kMaxGridThreads / threads;
+  for (; a.first < blocks; a.first += most) {
+    const int64_t n = blocks - a.first < most ? blocks - a.first : most;
+    const hipError_t e = launch_kernel(kernel, dim3((unsigned)n), dim3(threads), lds, stream, a);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <int DP, bool FULL>
 hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipStream_t stream) {
   constexpr int NW = DP == 256 ? 2 : 4, JY = 8;
@@ -644,12 +658,12 @@ hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipSt
   hipError_t e;
   if (pl.few) {
     if ((e = prepare_kernel(k_attention_few<DP, NW, FULL>)) != hipSuccess) return e;
-    e = launch_kernel(k_attention_few<DP, NW, FULL>, dim3((unsigned)blocks), dim3(NW * kWave), NW * 256 * DP, stream, a);
+    e = launch_blocks(k_attention_few<DP, NW, FULL>, blocks, NW * kWave, NW * 256 * DP, stream, a);
     if (e != hipSuccess || !shared) return e;
     return launch_kernel(k_attention_join<DP, 32, JY>, dim3((unsigned)blocks - 1, JY), dim3(256), 0, stream, a);
   }
   if ((e = prepare_kernel(k_attention_tile<DP, FULL>)) != hipSuccess) return e;
-  e = launch_kernel(k_attention_tile<DP, FULL>, dim3((unsigned)blocks), dim3(256), 512 * DP + 16, stream, a);
+  e = launch_blocks(k_attention_tile<DP, FULL>, blocks, 256, 512 * DP + 16, stream, a);
   if (e != hipSuccess || !shared) return e;
   return launch_kernel(k_attention_join<DP, 128, 16>, dim3((unsigned)blocks - 1, 16), dim3(256), 0, stream, a);
 }

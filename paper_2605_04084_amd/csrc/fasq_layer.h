@@ -17,6 +17,10 @@ struct HeadsView {
   int64_t ts, hs;
 };
 
+// Threads of a launch in x: a grid holds fewer than 2^32 (beyond, some launches
+// fail and others run only part of their workgroups), so longer calls go in pieces.
+constexpr int64_t kMaxGridThreads = (int64_t(1) << 32) - 1024;
+
 constexpr int kMaxRopeHalf = 128;
 
 struct RopeProblem {

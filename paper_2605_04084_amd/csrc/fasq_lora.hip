@@ -227,9 +227,10 @@ struct LowScale {
 
 // One wave per token and projection (4.8 us for 2048 tokens of 2 x 64 ranks).
 __global__ __launch_bounds__(256) void k_lora_fold(LoraArgs a) {
-  const int64_t row = blockIdx.x * (int64_t)4 + threadIdx.x / kWave;  // of [count][M]
-  if (row >= (int64_t)a.count * a.M) return;
-  const int lane = threadIdx.x % kWave, ad = a.adapters[row % a.M];
+  const int m = blockIdx.x * 4 + threadIdx.x / kWave;
+  if (m >= a.M) return;
+  const int64_t row = (int64_t)blockIdx.y * a.M + m;  // of [count][M]
+  const int lane = threadIdx.x % kWave, ad = a.adapters[m];
   if (ad < 0 || ad >= a.L) return;
   const int rp = (a.r + 31) / 32 * 32;
   const int64_t split = (int64_t)a.count * a.M * a.r;
@@ -563,7 +564,7 @@ hipError_t launch_lora(const LoraProblem& p, const DeviceInfo& dev, hipStream_t 
   if (pl.TU > 16) {
     a.low = reinterpret_cast<half_t*>(a.t + up_to(pl.splits * p.M * p.r * p.count, 4) * 4);
     a.factors = reinterpret_cast<float*>(a.low + p.M * p.count * 2 * (up_to(p.r, 32) * 32));
-    e = launch_kernel(k_lora_fold, dim3((unsigned)up_to(p.M * p.count, 4)), dim3(256), 0, stream, a);
+    e = launch_kernel(k_lora_fold, dim3((unsigned)up_to(p.M, 4), (unsigned)p.count), dim3(256), 0, stream, a);
     if (e != hipSuccess) return e;
   }
   // several slices share what a workgroup makes of the low-rank values, where

@@ -144,9 +144,21 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(NormArgs a) {
 }
 
 template <int THREADS, int CH>
-hipError_t launch_row(const NormArgs& a, int64_t M, bool vec, hipStream_t stream) {
-  return vec ? launch_kernel(k_residual_norm<THREADS, CH, true>, dim3((unsigned)M), dim3(THREADS), 0, stream, a)
-             : launch_kernel(k_residual_norm<THREADS, CH, false>, dim3((unsigned)M), dim3(THREADS), 0, stream, a);
+hipError_t launch_row(const NormArgs& all, int64_t M, bool vec, hipStream_t stream) {
+  constexpr int64_t most = kMaxGridThreads / THREADS;  // rows of a launch
+  for (int64_t m0 = 0; m0 < M; m0 += most) {
+    const dim3 grid((unsigned)(M - m0 < most ? M - m0 : most));
+    NormArgs a = all;
+    a.x += m0 * a.N;
+    if (a.y != nullptr) a.y += m0 * a.N;
+    if (a.gate != nullptr) a.gate += m0 * a.gate_stride;
+    if (a.x_out != nullptr) a.x_out += m0 * a.N;
+    if (a.h != nullptr) a.h += m0 * a.N;
+    const hipError_t e = vec ? launch_kernel(k_residual_norm<THREADS, CH, true>, grid, dim3(THREADS), 0, stream, a)
+                             : launch_kernel(k_residual_norm<THREADS, CH, false>, grid, dim3(THREADS), 0, stream, a);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

@@ -295,8 +295,8 @@ hipError_t launch_rope_append(const RopeProblem& p, hipStream_t stream) {
                    view16(p.k) && view16(p.v) && aligned16(p.q_norm) && aligned16(p.k_norm) && aligned16(p.table) &&
                    (p.k.p == nullptr || (aligned16(a.ck) && aligned16(a.cv) &&
                                          (a.page_stride | a.slot_stride | a.head_stride) % 8 == 0));
-  // rows are numbered in 32 bits: more than 2^31 heads go in several launches
-  const int64_t most = (int64_t(1) << 31) / heads;
+  const int lanes = !vec ? kWave : p.D <= 64 ? 4 : p.D <= 128 ? 8 : 16;  // of a head
+  const int64_t most = kMaxGridThreads / lanes / heads;  // tokens of a launch
   for (int64_t t0 = 0; t0 < p.T; t0 += most) {
     const int64_t n = p.T - t0 < most ? p.T - t0 : most;
     RopeArgs b = a;
