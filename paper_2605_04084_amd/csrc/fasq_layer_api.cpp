@@ -139,12 +139,12 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
                                  int64_t out_ts, int64_t out_hs, float* lse, void* workspace, int64_t workspace_bytes,
                                  hipStream_t stream) {
   if (T < 0 || T > fasq::kMaxTokens) return bad("T must lie in [0, 2^24]");
-  if (B < 1 || B > fasq::kMaxTokens) return bad("B must lie in [1, 2^24]");
+  if (B < (T > 0 ? 1 : 0) || B > fasq::kMaxTokens) return bad("B must lie in [1, 2^24] (0 only with T = 0)");
   if (Hkv < 1 || Hq < 1 || Hq > fasq::kMaxHeads || Hq % Hkv != 0) return bad("Hq must be a multiple of Hkv, both >= 1");
   if (T * (Hq / Hkv) > (int64_t(1) << 30)) return bad("T * Hq / Hkv must be at most 2^30");
   if (D < 1) return bad("D must be >= 1");
   if (D % 8 != 0 || D > 256) return fasq::fail(FASQ_ERR_UNSUPPORTED, "attention needs D a multiple of 8, at most 256");
-  if (max_pages < 1 || max_pages > INT32_MAX || page_row_stride < 0 || page_row_stride > fasq::kMaxStride)
+  if (max_pages < (T > 0 ? 1 : 0) || max_pages > INT32_MAX || page_row_stride < 0 || page_row_stride > fasq::kMaxStride)
     return bad("max_pages must be >= 1 and the page table's stride must not be negative");
   if (window < 0) return bad("window must be >= 0");
   if (std::isnan(scale)) return bad("scale must be a number");
@@ -189,7 +189,7 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
 }
 
 int64_t fasq_paged_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D) {
-  if (T < 0 || T > fasq::kMaxTokens || B < 1 || B > fasq::kMaxTokens) return -1;
+  if (T < 0 || T > fasq::kMaxTokens || B < (T > 0 ? 1 : 0) || B > fasq::kMaxTokens) return -1;
   if (Hkv < 1 || Hq < 1 || Hq > fasq::kMaxHeads || Hq % Hkv != 0 || D < 8 || D > 256 || D % 8 != 0) return -1;
   if (T * (Hq / Hkv) > (int64_t(1) << 30)) return -1;
   if (T == 0) return 0;

@@ -46,3 +46,12 @@ def test_windows_without_causality(reqs, Hq, Hkv, window, D):
 def test_windows_without_causality_and_more_tokens_than_keys():
     b = Batch([(400, 90), (90, 400), (33, 0)], 2, 1, 64, 20)
     b.check(b.run(causal=False, window=25), causal=False, window=25)
+
+
+def test_no_requests():
+    h = lambda *s: torch.zeros(s, dtype=torch.float16, device="cuda:0")  # noqa: E731
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    for pages in (i(0, 3), i(0, 0)):
+        out, lse = fasq.paged_attention(h(0, 4, 64), h(3, 16, 2, 64), h(3, 16, 2, 64), pages, i(1), i(0), return_lse=True)
+        assert tuple(out.shape) == (0, 4, 64) and tuple(lse.shape) == (0, 4)
+    assert tuple(fasq.paged_attention(h(0, 4, 64), h(3, 16, 2, 64), h(3, 16, 2, 64), i(2, 0), i(3), i(2)).shape) == (0, 4, 64)

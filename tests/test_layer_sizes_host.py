@@ -1,0 +1,30 @@
+"""Sizes at the ends of what the entry points between projections take: what is
+refused, and empty batches.  Nothing here touches a GPU.
+"""
+
+import ctypes
+import os
+
+import pytest
+
+import paper_2605_04084_amd as fasq
+from test_layer_abi_host import _attend, _cache, _refused
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(fasq.LIB_PATH):
+        from paper_2605_04084_amd import _build
+
+        _build.build()
+    return fasq.lib()
+
+
+@pytest.mark.parametrize("pages", [dict(), dict(pages=0, max_pages=0), dict(q=0, out=0, q_start=0, kv_len=0)])
+def test_no_requests_launch_nothing(L, pages):
+    """A batch of no requests has no tokens; its tables may be empty."""
+    assert _attend(L, T=0, B=0, **pages) == fasq.FASQ_OK
+    assert L.fasq_paged_attention_workspace_bytes(0, 0, 4, 2, 64) == 0
+    _refused(_attend(L, T=3, B=0), "B must")
+    assert L.fasq_paged_attention_workspace_bytes(3, 0, 4, 2, 64) == -1
+    _refused(_attend(L, T=0, B=-1), "B must")
