@@ -60,7 +60,7 @@ struct AttentionArgs {
   bool causal;
   bool out_vec;  // 8-byte stores of out
   bool whole_units;     // pages hold whole units of 16 keys, within 2^31 bytes
-  int window;  // 0: none
+  int window;  // 0: none, or all that there can be
   float* lse;
   // Split over workgroups (part_o != nullptr): workgroup w of `parts` takes
   // the w-th equal share of the batch's keys; see Place.
@@ -125,7 +125,7 @@ struct Span {
 __device__ __forceinline__ Span token_span(const AttentionArgs& a, const Request& r, int i) {
   const int pos = r.kv - r.n + i;  // may be negative: more new tokens than keys
   int end = a.causal && pos + 1 < r.kv ? pos + 1 : r.kv;
-  int begin = a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
+  int begin = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
   end = end < 0 ? 0 : end;
   return {begin < end ? begin : end, end};
 }
@@ -159,8 +159,8 @@ __device__ __forceinline__ int64_t tile_length(const AttentionArgs& a, const Req
   if (a.window > 0) {
     // of the tile's tokens, from a multiple of 32 on; without causality the
     // request's first token sees the window before it and all that follows
-    const int most = a.window + (a.causal ? token_of(a, ROWS) : r.n) + 32;
-    keys = keys < most ? keys : most;
+    const int besides = (a.causal ? token_of(a, ROWS) : r.n) + 32;
+    keys = keys - besides > a.window ? a.window + besides : keys;
   }
   return keys <= STEP ? STEP : ((int64_t)keys + STEP - 1) / STEP * STEP;
 }

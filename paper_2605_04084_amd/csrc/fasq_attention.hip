@@ -707,7 +707,7 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
   if (a.c < 1e-30f) a.c = 1e-30f;
   a.negate = p.scale < 0.f;
   a.causal = p.causal;
-  a.window = p.window < INT32_MAX / 2 ? (int)p.window : 0;  // wider than any cache: none
+  a.window = p.window < a.capacity ? (int)p.window : 0;
   auto aligned = [](const HeadsView& v, int bytes) {
     return reinterpret_cast<uintptr_t>(v.p) % bytes == 0 && v.ts % (bytes / 2) == 0 && v.hs % (bytes / 2) == 0;
   };
