@@ -469,7 +469,8 @@ fasq_status fasq_rope_append(const void* q, int64_t q_token_stride, int64_t q_he
  *               [0, num_pages) (an entry outside is read as the nearest page)
  *   B           requests; 0 only with T = 0 (as max_pages)
  *   q_start     int32 [B + 1], not decreasing, within [0, T]
- *   kv_len      int32 [B], at most max_pages * page_size (more is cut there)
+ *   kv_len      int32 [B], at most max_pages * page_size (more is cut there),
+ *               which is at most 2^31 - 1024
  *   lse         fp32 [T x Hq], contiguous, or NULL
  *   workspace   device scratch of fasq_paged_attention_workspace_bytes()
  *               bytes (16-byte aligned) for the fp32 partial results, where

@@ -52,7 +52,7 @@ struct AttentionArgs {
   int64_t page_stride, slot_stride, head_stride;
   const int32_t* pages;
   int64_t page_row_stride;
-  int capacity;  // max_pages * page_size
+  int capacity;  // max_pages * page_size: at most 2^31 - 1024, so that no key's number overflows, steps past the end included
   const int32_t* q_start;
   const int32_t* kv_len;
   float c;  // |scale| * log2(e), at least 1e-30 so that -inf stays -inf

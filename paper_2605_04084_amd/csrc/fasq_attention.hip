@@ -129,8 +129,8 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
     const int base = span.begin / 32 * 32;
     int lo = base, hi = span.end;
     if (shared) {
-      lo = base + (int)(pos - t0);
-      const int64_t most = base + (seg_end - t0);
+      const int64_t from = base + (pos - t0), most = base + (seg_end - t0);  // may lie behind the last key
+      lo = from < hi ? (int)from : hi;
       hi = most < hi ? (int)most : hi;
     }
     const int rows = p.r.n * a.G, row0 = p.tile * ROWS, live = rows - row0 < ROWS ? rows - row0 : ROWS;
@@ -333,8 +333,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     const int base = span.begin / 32 * 32;
     int lo = base, hi = span.end;
     if (shared) {
-      lo = base + (int)(pos - t0);
-      const int64_t most = base + (seg_end - t0);
+      const int64_t from = base + (pos - t0), most = base + (seg_end - t0);  // may lie behind the last key
+      lo = from < hi ? (int)from : hi;
       hi = most < hi ? (int)most : hi;
     }
     const int rows = p.r.n * a.G, row0 = p.tile * ROWS + wave * 32;

@@ -156,7 +156,8 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
   if ((why = fasq::check_view(q, q_ts, q_hs)) || (why = fasq::check_view(out, out_ts, out_hs)) ||
       (why = fasq::check_cache(cache)))
     return bad(why);
-  if (cache->page_size > INT32_MAX / max_pages) return bad("max_pages * page_size must fit in 31 bits");
+  if (cache->page_size > (INT32_MAX - 1023) / max_pages)
+    return bad("max_pages * page_size must fit in 31 bits, up to 2^31 - 1024");
   if (fasq::misaligned(cache->k, 16) || fasq::misaligned(cache->v, 16) ||
       (cache->page_stride | cache->slot_stride | cache->head_stride) % 8 != 0)
     return bad("the cache must be 16-byte aligned, its strides multiples of 8");

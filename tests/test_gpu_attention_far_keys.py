@@ -2,6 +2,8 @@
 name the same few pages, so that the keys repeat.
 """
 
+import math
+
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -30,6 +32,34 @@ def _inputs(n, seed):
 
 def _len(kv):
     return torch.tensor([kv], dtype=torch.int32, device="cuda:0")
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n", [1, 20, 200])
+def test_windows_at_the_largest_length(n, causal, split):
+    """The last keys there can be, as a short cache has them."""
+    q, k, v, q_start = _inputs(n, n)
+    kw = dict(window=100, causal=causal, return_lse=True)
+    if not split:
+        kw["workspace"] = torch.empty(0, dtype=torch.uint8, device="cuda:0")
+    kv = 2 ** 31 - 1024
+    pages = torch.zeros((1, kv // SIZE), dtype=torch.int32, device="cuda:0")
+    far = fasq.paged_attention(q, k, v, pages, q_start, _len(kv), **kw)
+    near = fasq.paged_attention(q, k, v, pages[:, :100], q_start, _len(1600), **kw)
+    assert all(torch.equal(a, b) for a, b in zip(far, near))
+
+
+def test_all_keys_of_the_largest_length():
+    q, k, v, q_start = _inputs(1, 5)
+    kv = 2 ** 31 - 1024
+    pages = torch.zeros((1, kv // SIZE), dtype=torch.int32, device="cuda:0")
+    out, lse = fasq.paged_attention(q, k, v, pages, q_start, _len(kv), return_lse=True)
+    near, near_lse = fasq.paged_attention(q, k, v, pages[:, :1], q_start, _len(SIZE), return_lse=True)
+    # weights in fp16 (2^-11 of |v| on each side); 2^31 keys over 2^10 waves, 16 a
+    # product: 2^17 additions in fp32 in turn, 2^-24 each
+    assert float((out - near).abs().max()) <= (2.0 ** -7 + 2.0 ** -9) * float(v.abs().max())
+    assert float((lse - near_lse - math.log(kv // SIZE)).abs().max()) <= 2.0 ** -10
 
 
 @pytest.mark.parametrize("n", [1, 100])

@@ -28,3 +28,10 @@ def test_no_requests_launch_nothing(L, pages):
     _refused(_attend(L, T=3, B=0), "B must")
     assert L.fasq_paged_attention_workspace_bytes(3, 0, 4, 2, 64) == -1
     _refused(_attend(L, T=0, B=-1), "B must")
+
+
+@pytest.mark.parametrize("page_size,max_pages", [(2 ** 31 - 1, 1), (2 ** 31 - 1023, 1), (16, 2 ** 27 - 1), (1, 2 ** 31 - 1023)])
+def test_keys_whose_steps_would_pass_31_bits(L, page_size, max_pages):
+    """The kernels step up to some hundred keys past a request's last one."""
+    args = dict(cache=_cache(num_pages=1, page_size=page_size), max_pages=max_pages)
+    _refused(_attend(L, **args), "2^31 - 1024")
