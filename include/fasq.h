@@ -467,7 +467,7 @@ fasq_status fasq_rope_append(const void* q, int64_t q_token_stride, int64_t q_he
  *   pages       int32 [B x max_pages], row stride page_row_stride; entries
  *               past a request's last page are not used, others lie in
  *               [0, num_pages) (an entry outside is read as the nearest page)
- *   B           requests; 0 only with T = 0 (as max_pages)
+ *   B           requests, at most 2^16; 0 only with T = 0 (as max_pages)
  *   q_start     int32 [B + 1], not decreasing, within [0, T]
  *   kv_len      int32 [B], at most max_pages * page_size (more is cut there),
  *               which is at most 2^31 - 1024

@@ -30,6 +30,7 @@ bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t
 
 constexpr int kMaxHeads = 65536;
 constexpr int64_t kMaxTokens = int64_t(1) << 24;  // tokens of one call
+constexpr int64_t kMaxRequests = int64_t(1) << 16;  // each tile of attention is looked up among them
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
 bool stride_ok(int64_t s) { return s >= 0 && s <= kMaxStride; }
@@ -139,7 +140,7 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
                                  int64_t out_ts, int64_t out_hs, float* lse, void* workspace, int64_t workspace_bytes,
                                  hipStream_t stream) {
   if (T < 0 || T > fasq::kMaxTokens) return bad("T must lie in [0, 2^24]");
-  if (B < (T > 0 ? 1 : 0) || B > fasq::kMaxTokens) return bad("B must lie in [1, 2^24] (0 only with T = 0)");
+  if (B < (T > 0 ? 1 : 0) || B > fasq::kMaxRequests) return bad("B must lie in [1, 2^16] (0 only with T = 0)");
   if (Hkv < 1 || Hq < 1 || Hq > fasq::kMaxHeads || Hq % Hkv != 0) return bad("Hq must be a multiple of Hkv, both >= 1");
   if (T * (Hq / Hkv) > (int64_t(1) << 30)) return bad("T * Hq / Hkv must be at most 2^30");
   if (D < 1) return bad("D must be >= 1");
@@ -190,7 +191,7 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
 }
 
 int64_t fasq_paged_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D) {
-  if (T < 0 || T > fasq::kMaxTokens || B < (T > 0 ? 1 : 0) || B > fasq::kMaxTokens) return -1;
+  if (T < 0 || T > fasq::kMaxTokens || B < (T > 0 ? 1 : 0) || B > fasq::kMaxRequests) return -1;
   if (Hkv < 1 || Hq < 1 || Hq > fasq::kMaxHeads || Hq % Hkv != 0 || D < 8 || D > 256 || D % 8 != 0) return -1;
   if (T * (Hq / Hkv) > (int64_t(1) << 30)) return -1;
   if (T == 0) return 0;

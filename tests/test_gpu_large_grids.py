@@ -84,3 +84,17 @@ def test_attention_of_many_whole_tiles():
     out = run(q)
     for part in out.split(2 ** 16):
         assert bool((part == want).all())
+
+
+@pytest.mark.parametrize("split", [True, False])
+def test_attention_of_the_most_requests(split):
+    """2^16 requests of a token and a key each: the key's value."""
+    B, H, D = 2 ** 16, 2, 8
+    q, k = (torch.randn(s, device="cuda:0").half() for s in ((B, 2 * H, D), (B, 1, H, D)))
+    v = torch.randn((B, 1, H, D), device="cuda:0").half()
+    i32 = dict(dtype=torch.int32, device="cuda:0")
+    pages = torch.randperm(B, **i32)[:, None]
+    kw = {} if split else {"workspace": torch.empty(0, dtype=torch.uint8, device="cuda:0")}
+    out = fasq.paged_attention(q, k, v, pages, torch.arange(B + 1, **i32), torch.ones(B, **i32), **kw)
+    want = v[pages[:, 0].long(), 0].repeat_interleave(2, dim=1)
+    assert torch.equal(out, want)

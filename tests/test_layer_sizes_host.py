@@ -35,3 +35,10 @@ def test_keys_whose_steps_would_pass_31_bits(L, page_size, max_pages):
     """The kernels step up to some hundred keys past a request's last one."""
     args = dict(cache=_cache(num_pages=1, page_size=page_size), max_pages=max_pages)
     _refused(_attend(L, **args), "2^31 - 1024")
+
+
+def test_more_requests_than_a_call_takes(L):
+    """Every tile looks for its request among all of them: 2^24 requests, as
+    were taken before, would keep the GPU busy for hours."""
+    _refused(_attend(L, T=1 << 20, B=65537), "B must")
+    assert L.fasq_paged_attention_workspace_bytes(1 << 20, 65537, 4, 2, 64) == -1
