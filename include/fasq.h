@@ -546,7 +546,7 @@ fasq_status fasq_residual_norm(const void* x, const void* y, int64_t M, int64_t 
  *   scales    fp32 [L]
  *   N, A, B, base, y   HOST arrays of `count` entries: sizes, and device
  *             buffers fp16 [L x r x K], [L x N[i] x r], [M x N[i]], [M x N[i]];
- *             y[i] may be base[i]; base[i] NULL: zero
+ *             N[i] <= 2^31 - 2^17; y[i] may be base[i]; base[i] NULL: zero
  *   workspace device scratch of fasq_lora_workspace_bytes() bytes, 16-byte
  *             aligned; contents are overwritten
  *

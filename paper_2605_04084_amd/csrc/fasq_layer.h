@@ -80,6 +80,7 @@ hipError_t launch_residual_norm(const NormProblem& p, hipStream_t stream);
 
 constexpr int kLoraMaxCount = 8;
 constexpr int kLoraMaxRank = 256;
+constexpr int64_t kLoraMaxN = (int64_t(1) << 31) - (1 << 17);  // a block's features end below 2^31
 struct LoraProblem {
   const uint16_t* x;
   int64_t M, K;

@@ -258,7 +258,7 @@ fasq_status fasq_lora_batched(const void* x, int64_t M, int64_t K, const int32_t
   if (fasq::misaligned(x, 2)) return bad("fp16 tensors must be 2-byte aligned");
   for (int i = 0; i < count; ++i) {
     const char* why = nullptr;
-    if (N[i] < 1 || N[i] > INT32_MAX) why = "N must lie in [1, 2^31)";
+    if (N[i] < 1 || N[i] > fasq::kLoraMaxN) why = "N must lie in [1, 2^31 - 2^17]";
     else if (A[i] == nullptr || B[i] == nullptr || y[i] == nullptr) why = "a buffer pointer is NULL";
     else if (fasq::misaligned(A[i], 2) || fasq::misaligned(B[i], 2) || fasq::misaligned(base[i], 2) ||
              fasq::misaligned(y[i], 2))

@@ -98,3 +98,15 @@ def test_attention_of_the_most_requests(split):
     out = fasq.paged_attention(q, k, v, pages, torch.arange(B + 1, **i32), torch.ones(B, **i32), **kw)
     want = v[pages[:, 0].long(), 0].repeat_interleave(2, dim=1)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("N", [2 ** 28 + 5, 2 ** 31 - 2 ** 17])
+def test_adapters_of_the_widest_projections(N):
+    """As many features as a projection may have: blocks of them beyond 65535 in y."""
+    x = torch.full((1, 1), 2.0, dtype=torch.float16, device="cuda:0")
+    ids = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    A = torch.ones((1, 1, 1), dtype=torch.float16, device="cuda:0")
+    B = torch.empty((1, N, 1), dtype=torch.float16, device="cuda:0")
+    B.view(-1)[:] = torch.arange(257, device="cuda:0").half().repeat(-(-N // 257))[:N]
+    y, = fasq.lora_batched(x, ids, [A], [B], torch.ones(1, device="cuda:0"), [None])
+    assert torch.equal(y[0], B.view(-1) * 2)

@@ -8,7 +8,7 @@ import os
 import pytest
 
 import paper_2605_04084_amd as fasq
-from test_layer_abi_host import _attend, _cache, _refused
+from test_layer_abi_host import _attend, _cache, _lora, _refused
 
 
 @pytest.fixture(scope="module")
@@ -42,3 +42,8 @@ def test_more_requests_than_a_call_takes(L):
     were taken before, would keep the GPU busy for hours."""
     _refused(_attend(L, T=1 << 20, B=65537), "B must")
     assert L.fasq_paged_attention_workspace_bytes(1 << 20, 65537, 4, 2, 64) == -1
+
+
+@pytest.mark.parametrize("N", [2 ** 31 - 1, 2 ** 31 - 2 ** 17 + 1])
+def test_features_whose_blocks_would_pass_31_bits(L, N):
+    _refused(_lora(L, N=(32, N)), "projection 1: N")
