@@ -369,7 +369,8 @@ fasq_status fasq_pq_reconstruct(const void* idx, int64_t N, int64_t K, int idx_b
  * memory when the kernels run, so one recorded step serves every step of the
  * same shape.  Zero tokens (T or M = 0) is a valid call that launches
  * nothing.  Strides are in elements; the last dimension of every tensor is
- * contiguous.
+ * contiguous.  Inputs may be broadcast (strides of 0), what is written may not:
+ * its strides of more than one row are at least D.
  * ---------------------------------------------------------------------------
  */
 

@@ -43,6 +43,10 @@ const char* check_view(const void* p, int64_t ts, int64_t hs) {
   return nullptr;
 }
 
+// Of what is written: neighbouring rows of D values lie apart (a broadcast
+// tensor's do not).
+bool rows_overlap(int64_t D, int64_t count, int64_t stride) { return count > 1 && stride < D; }
+
 const char* check_cache(const fasq_kv_cache* c) {
   if (c == nullptr) return "cache is NULL";
   if (c->k == nullptr || c->v == nullptr) return "a cache pointer is NULL";
@@ -104,11 +108,15 @@ fasq_status fasq_rope_append(const void* q, int64_t q_ts, int64_t q_hs, int Hq, 
   if (q != nullptr) {
     if ((why = fasq::check_view(q, q_ts, q_hs)) || (why = fasq::check_view(q_out, qo_ts, qo_hs))) return bad(why);
     if (q == q_out && (q_ts != qo_ts || q_hs != qo_hs)) return bad("q_out = q needs the strides of q");
+    if (fasq::rows_overlap(D, T, qo_ts) || fasq::rows_overlap(D, Hq, qo_hs)) return bad("rows of q_out overlap");
   }
   if (k != nullptr) {
     if ((why = fasq::check_view(k, k_ts, k_hs)) || (why = fasq::check_view(v, v_ts, v_hs)) ||
         (why = fasq::check_cache(cache)))
       return bad(why);
+    if (fasq::rows_overlap(D, cache->num_pages, cache->page_stride) ||
+        fasq::rows_overlap(D, cache->page_size, cache->slot_stride) || fasq::rows_overlap(D, Hkv, cache->head_stride))
+      return bad("rows of the cache overlap");
     if (slots == nullptr) return bad("a buffer pointer is NULL");
   }
   fasq::RopeProblem p = {};
@@ -157,6 +165,7 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
   if ((why = fasq::check_view(q, q_ts, q_hs)) || (why = fasq::check_view(out, out_ts, out_hs)) ||
       (why = fasq::check_cache(cache)))
     return bad(why);
+  if (fasq::rows_overlap(D, T, out_ts) || fasq::rows_overlap(D, Hq, out_hs)) return bad("rows of out overlap");
   if (cache->page_size > (INT32_MAX - 1023) / max_pages)
     return bad("max_pages * page_size must fit in 31 bits, up to 2^31 - 1024");
   if (fasq::misaligned(cache->k, 16) || fasq::misaligned(cache->v, 16) ||

@@ -8,7 +8,7 @@ import os
 import pytest
 
 import paper_2605_04084_amd as fasq
-from test_layer_abi_host import _attend, _cache, _lora, _refused
+from test_layer_abi_host import DUMMY, _attend, _cache, _lora, _refused, _rope
 
 
 @pytest.fixture(scope="module")
@@ -47,3 +47,15 @@ def test_more_requests_than_a_call_takes(L):
 @pytest.mark.parametrize("N", [2 ** 31 - 1, 2 ** 31 - 2 ** 17 + 1])
 def test_features_whose_blocks_would_pass_31_bits(L, N):
     _refused(_lora(L, N=(32, N)), "projection 1: N")
+
+
+@pytest.mark.parametrize("args", [dict(qos=0), dict(qoh=0), dict(qoh=63), dict(cache=_cache(head_stride=0)),
+                                  dict(cache=_cache(slot_stride=32)), dict(cache=_cache(page_stride=0))])
+def test_rope_outputs_whose_rows_overlap(L, args):
+    """Two rows in one place: what is left there depends on which is written last."""
+    _refused(_rope(L, **dict(dict(qo=DUMMY + 4096), **args)), "overlap")
+
+
+@pytest.mark.parametrize("args", [dict(os=0), dict(oh=0), dict(oh=56), dict(os=8)])
+def test_attention_outputs_whose_rows_overlap(L, args):
+    _refused(_attend(L, **dict(dict(out=DUMMY + 4096), **args)), "overlap")
