@@ -460,8 +460,8 @@ fasq_status fasq_rope_append(const void* q, int64_t q_token_stride, int64_t q_he
  * The weights exp(s_j - lse) are rounded to fp16 (relative 2^-12 down to 2^-21
  * of a token's largest one, in steps of at most 2^-31 of it below).
  *
- *   q, out      fp16 [T x Hq x D] with token and head strides; tokens outside
- *               every request are neither read nor written;
+ *   q, out      fp16 [T x Hq x D] with token and head strides, which do not
+ *               overlap; tokens outside every request are neither read nor written;
  *               T * (Hq / Hkv) <= 2^30
  *   cache       16-byte aligned, strides multiples of 8
  *   D           a multiple of 8, 8 <= D <= 256

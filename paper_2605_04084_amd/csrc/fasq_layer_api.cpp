@@ -172,6 +172,7 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
       (cache->page_stride | cache->slot_stride | cache->head_stride) % 8 != 0)
     return bad("the cache must be 16-byte aligned, its strides multiples of 8");
   if (workspace != nullptr && fasq::misaligned(workspace, 16)) return bad("workspace must be 16-byte aligned");
+  if (out == q) return bad("out must not be q");
   fasq::DeviceInfo dev;
   const hipError_t e = fasq::device_info(&dev);
   if (e != hipSuccess)

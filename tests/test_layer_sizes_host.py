@@ -59,3 +59,8 @@ def test_rope_outputs_whose_rows_overlap(L, args):
 @pytest.mark.parametrize("args", [dict(os=0), dict(oh=0), dict(oh=56), dict(os=8)])
 def test_attention_outputs_whose_rows_overlap(L, args):
     _refused(_attend(L, **dict(dict(out=DUMMY + 4096), **args)), "overlap")
+
+
+def test_attention_over_its_own_queries(L):
+    """Rows that meet values that are not finite read their queries again after the output is written."""
+    _refused(_attend(L, q=DUMMY, out=DUMMY), "out must not be q")
