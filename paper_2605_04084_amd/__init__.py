@@ -653,11 +653,13 @@ def _kv_cache(k_cache, v_cache, device, Hkv=None, D=None):
     if not (isinstance(v_cache, torch.Tensor) and v_cache.dtype is torch.float16 and v_cache.shape == shape
             and v_cache.stride() == strides and v_cache.get_device() == device):
         _require_rows(v_cache, "v_cache", torch.float16, 4)
-        if v_cache.shape != shape or v_cache.stride() != strides:
+        if v_cache.shape != shape or any(n > 1 and a != b for n, a, b in zip(shape, v_cache.stride(), strides)):
             raise ValueError("k_cache and v_cache must have the same shape and strides")
         _same_device(device, v_cache)
     if k_cache.get_device() != device:
         _same_device(device, k_cache)
+    if pages == 1 or page_size == 1 or heads == 1:  # these strides are never taken, and may be anything
+        strides = [s if n > 1 else 0 for n, s in zip(shape, strides)]
     return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size, strides[0], strides[1], strides[2])
 
 

@@ -1,5 +1,5 @@
-"""Strides at their edges in the entry points between projections: broadcast
-inputs, and outputs that may not be.
+"""Strides at their edges in the entry points between projections: caches with
+dimensions of one, whose strides mean nothing, and broadcast inputs.
 """
 
 import pytest
@@ -25,6 +25,34 @@ def _i32(*a):
 
 def _rand(*s):
     return torch.randn(s, device="cuda:0").half()
+
+
+def _restride(t, strides):
+    """The same values with other strides, in a buffer of their own."""
+    room = 1 + sum((n - 1) * s for n, s in zip(t.shape, strides))
+    out = torch.zeros(room, dtype=t.dtype, device=t.device).as_strided(t.shape, strides)
+    return out.copy_(t)
+
+
+@pytest.mark.parametrize("shape", [(3, 1, 2, 64), (1, 16, 2, 64), (3, 16, 1, 64), (1, 1, 1, 64), (1, 20, 1, 64)])
+def test_dimensions_of_one(shape):
+    """Both caches hold the same layout; the strides of their single pages,
+    slots or heads differ, and are no multiples of 8."""
+    pages, size, H, D = shape
+    n = pages * size
+    k, v, q = _rand(*shape), _rand(*shape), _rand(1, 2 * H, D)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda:0")[None]
+    args = (table, _i32(0, 1), _i32(n))
+    new = _rand(1, H, D), _rand(1, H, D), _i32(n - 1)
+    fasq.rope_append(None, *new[:2], None, None, new[2], k, v)
+    want = fasq.paged_attention(q, k, v, *args)
+    for odd_k, odd_v in ((13, 7), (0, 5)):
+        strides = [[s if m > 1 else odd for m, s in zip(shape[:3], k.stride())] + [1] for odd in (odd_k, odd_v)]
+        k2, v2 = _restride(k, strides[0]), _restride(v, strides[1])
+        assert torch.equal(fasq.paged_attention(q, k2, v2, *args), want)
+        fasq.rope_append(None, new[1], new[0], None, None, new[2], k2, v2)
+        assert torch.equal(k2.flatten(0, 1)[n - 1], new[1][0]) and torch.equal(v2.flatten(0, 1)[n - 1], new[0][0])
+        assert torch.equal(k2.flatten(0, 1)[:n - 1], k.flatten(0, 1)[:n - 1])
 
 
 def test_caches_of_different_layout_are_refused():
