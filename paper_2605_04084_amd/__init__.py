@@ -682,7 +682,7 @@ def _workspace(workspace, need, device, like):
 
 
 def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
-                     original: int = 0, low: float = 1.0, high: float = 4.0):
+                     original: int = 0, low: float = 1.0, high: Optional[float] = None):
     """The rotary frequencies ``w_i`` (``rot / 2`` Python floats) and the scale of
     the table, for :func:`rope_table`.
 
@@ -695,9 +695,9 @@ def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = N
     * ``"wavelength"``: pairs that turn more than ``high`` times over the original
       context are left, those that turn less than ``low`` times are slowed by
       ``factor``, between them both are mixed by the number of turns (the
-      scaling of Llama-3's long-context models: low 1, high 4);
+      scaling of Llama-3's long-context models: low 1, high 4, the defaults);
     * ``"yarn"`` (arXiv 2309.00071): the mix is linear in the pair's index between
-      the pairs that turn ``high`` (32 in the paper) and ``low`` times, and the
+      the pairs that turn ``high`` (32, as in the paper, unless given) and ``low`` times, and the
       table's scale is ``0.1 ln(factor) + 1``.
     """
     if rot < 2 or rot % 2 or rot > 256:
@@ -716,6 +716,8 @@ def rope_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = N
         return [v / factor for v in w], scale
     if scaling not in ("wavelength", "yarn"):
         raise ValueError("scaling must be None, 'linear', 'ntk', 'wavelength' or 'yarn'")
+    if high is None:
+        high = 32.0 if scaling == "yarn" else 4.0
     if original < 1 or not 0 < low < high:
         raise ValueError(f"{scaling} needs original >= 1 and 0 < low < high")
     turns = [original * v / (2 * math.pi) for v in w]
