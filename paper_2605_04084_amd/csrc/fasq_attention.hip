@@ -82,8 +82,8 @@ constexpr int kTileShare = 256;
 // Up to 32 rows: NW waves, each 32 keys at a time with its own two stages of
 // LDS, so that no wave waits for another until the end, where their results
 // are joined in wave order.  Bound by the keys and values read: 64 requests of
-// 300 to 8192 keys (8 heads of 128 for 32) take 127 us (633 MB, 5.0 TB/s), two
-// of 65536 to 131072 150 us (5.4 TB/s).  One token on 1531 keys takes 8.5 us, of
+// 300 to 8192 keys (8 heads of 128 for 32) take 126 us (633 MB, 5.0 TB/s), two
+// of 65536 to 131072 149 us (5.4 TB/s).  One token on 1531 keys takes 9.1 us, of
 // which reading lengths, finding its keys and the first copies are the most.
 // ---------------------------------------------------------------------------
 template <int DP, int NW, bool FULL>
@@ -257,11 +257,11 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
 // ---------------------------------------------------------------------------
 // 128 rows: four waves of 32 rows over shared tiles of 64 keys, two stages.
 // Bound by what one wave does in turn (see WaveTile::block): 2048 tokens after
-// 6144, 32 heads of 128 on 8, take 259 us (241 GFLOP, 928 TFLOP/s; the matrix
-// cores are busy about 60 % of the time, at 1.74 GHz).  Of 285 us the copies
-// were 30, the LDS reads 30, the maximum 12, the sum of the weights 10 (each
-// left out, for timing).  64 rows a wave would halve the LDS reads, but leave
-// one wave a SIMD.  A tile costs 10 us besides its keys.
+// 6144, 32 heads of 128 on 8, take 261 to 275 us from card to card (241 GFLOP,
+// 925 to 878 TFLOP/s; the matrix cores are busy half of the time, at 1.78 GHz).
+// Of 285 us at the time the copies were 30, the LDS reads 30, the maximum 12, the
+// sum of the weights 10 (each left out, for timing).  64 rows a wave would halve
+// the LDS reads, but leave one wave a SIMD.  A tile costs 10 us besides its keys.
 // ---------------------------------------------------------------------------
 template <int DP, bool FULL>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(AttentionArgs) {
@@ -528,8 +528,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 // Joins the shares of one cut tile: workgroup x takes the one that starts in
 // share x, y cuts the tile's values.  Shares are added in their order, by groups
 // of threads that take every so-manieth share where there are few rows.  4.6 us
-// for one token on 1531 keys, 6.6 for two on 131072, 7.4 for a ragged batch of
-// 25 requests, mostly the launch.
+// for one token on 1531 keys, 5.4 for two on 131072, 7.5 for a ragged batch of
+// 24 requests, mostly the launch.
 // ---------------------------------------------------------------------------
 template <int DP, int ROWS, int YS>
 __global__ __launch_bounds__(256) void k_attention_join(AttentionArgs a) {

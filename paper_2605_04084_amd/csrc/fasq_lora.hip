@@ -134,9 +134,9 @@ struct BlockIds {
 // share of K, which the four waves split once more and add in wave order.
 // Adapters and activations go from memory to the operands: a wave reads 16
 // rows of 64 bytes at a time.  2048 tokens of 4096 values, two projections of 64
-// ranks take 17.6 us (more splits, or shares of K begun at different places,
+// ranks take 17.5 us (more splits, or shares of K begun at different places,
 // were no faster: not the order of memory's channels), 16 tokens with an
-// adapter each on three projections of 16 ranks 4.9 us.
+// adapter each on three projections of 16 ranks 4.8 us.
 // ---------------------------------------------------------------------------
 template <int TT, int RT, bool VEC>
 __global__ __launch_bounds__(256) void k_lora_down(LoraArgs a) {
@@ -225,7 +225,7 @@ struct LowScale {
   }
 };
 
-// One wave per token and projection (4.8 us for 2048 tokens of 2 x 64 ranks).
+// One wave per token and projection (4.9 us for 2048 tokens of 2 x 64 ranks).
 __global__ __launch_bounds__(256) void k_lora_fold(LoraArgs a) {
   const int m = blockIdx.x * 4 + threadIdx.x / kWave;
   if (m >= a.M) return;
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256) void k_lora_fold(LoraArgs a) {
 // feature 8 q + u of its 128, so that a lane ends with 8 neighbouring features
 // of 4 tokens, and base and y move in runs of 256 bytes, base a tile ahead.
 // Bound by that pass over base and y: 2048 tokens, 2 x 14336 features, 64
-// ranks take 66 us (3.6 TB/s).  Measured slower there: runs of 128 bytes (80
+// ranks take 67 us (3.5 TB/s).  Measured slower there: runs of 128 bytes (80
 // us), blocks of 64 tokens (71 us), base two tiles ahead (70 us, registers
 // spill), low-rank values folded by every workgroup instead of once (97 us).
 // 16 tokens with an adapter each on 4096 + 1024 + 1024 features: 7.4 us.

@@ -5,7 +5,7 @@
 // and h written once: bound by memory.  Each of the two norms is a sum over
 // the row (a wave's lanes by DPP, then the waves by LDS in wave order), in fp32;
 // x_out and h are each rounded once, from fp32 values.  4096 rows of 4096 with
-// both norms and a gate take 24.1 us (134 MB, 5.6 TB/s), one row 2.6 us.
+// both norms and a gate take 24.3 us (134 MB, 5.5 TB/s), one row 2.6 us.
 #include <hip/hip_runtime.h>
 
 #include "fasq_device.h"
