@@ -297,9 +297,10 @@ int64_t fasq_pq_encode_workspace_bytes(int64_t N, int64_t K, int d, int64_t C);
  * fasq_launch_list_end, every fasq_* compute call made on the calling thread
  * (fasq_pq_gemv, _batched, _ex, _ex_noalloc, fasq_pq_gemm, _ex, _lut,
  * fasq_pq_reconstruct, fasq_pq_encode, and the entry points between the
- * projections below) validates its arguments and chooses its kernels as usual, then appends its launches (kernel, grid, block, LDS bytes
- * and a copy of the argument values) to the list instead of queueing them; its
- * `stream` argument is ignored.  fasq_launch_list_run queues every recorded
+ * projections below) validates its arguments and chooses its kernels as usual,
+ * then appends its launches (kernel, grid, block, LDS bytes and a copy of the
+ * argument values) to the list instead of queueing them; its `stream` argument
+ * is ignored.  fasq_launch_list_run queues every recorded
  * launch, in recording order, on `stream`.  A run computes what the recorded
  * calls would have computed at that point of the stream, bit for bit.
  *

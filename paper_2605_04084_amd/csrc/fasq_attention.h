@@ -400,9 +400,9 @@ __device__ __forceinline__ bool cut_to_finite(uint16_t* values) {
 // to the running maximum: then they have 11 bits down to 2^-21 of the row's
 // largest, and vanish (while the fp32 sum still counts them) only below 2^-32 of it
 // rather than 2^-25, which a sum over 131072 keys beside one far larger shows.
-// With kLift 7 and a maximum up to 2^8 behind they stay below fp16's largest value, but
-// for scores of 2^25 powers of two and more, whose rounding alone passes it:
-// such rows end not finite and are computed again (SlowRow).
+// With kLift 7 and a maximum up to 2^8 behind they stay below fp16's largest
+// value, but for scores of 2^24 powers of two and more, whose rounding may pass
+// it: such rows end not finite and are computed again (SlowRow).
 constexpr float kLift = 7.f;
 
 template <int DP, int KB>

@@ -73,3 +73,21 @@ def test_output_of_many_weights_far_below_one(n, kv, Hq, D, at, split, powers):
     tol = np.abs(want) * 2.0 ** -11 * 1.001 + 2.0 ** -25 + mass * (2.0 ** -11 + 2.0 ** -14) + kv * 2.0 ** -32
     err = np.abs(out.astype(np.float64) - want)
     assert (err <= tol).all(), (float((err - tol).max()), float((err / np.maximum(want, 1e-30)).max()))
+
+
+@pytest.mark.parametrize("n,split", [(1, True), (3, False), (100, True), (100, False)])
+@pytest.mark.parametrize("top", [2.0 ** 23, 2.0 ** 25, 2.0 ** 27])
+def test_scores_whose_rounding_passes_the_weights(n, split, top):
+    """Equal scores so large that fp32 rounds them to whole powers of two and
+    more: every key counts alike."""
+    kv, D = 700, 64
+    b = Batch([(n, kv)], 2, 1, D, 16, seed=n)
+    b.q[:], b.k[:] = 1, np.where(np.isnan(b.k), b.k, 1)
+    b.k[..., 1:] = np.where(np.isnan(b.k[..., 1:]), b.k[..., 1:], 0)
+    scale = np.float32(top * math.log(2.0) * 1.1)
+    kw = {} if split else {"workspace": torch.empty(0, dtype=torch.uint8, device="cuda:0")}
+    out, lse = b.run(scale=float(scale), **kw)
+    want, want_lse, mass = lo.paged_attention(b.q, b.k, b.v, b.pages, b.q_start, b.kv_len, float(scale))
+    tol = np.abs(want) * 2.0 ** -11 * 1.001 + 2.0 ** -25 + mass * (2.0 ** -11 + 2.0 ** -14)
+    assert (np.abs(out.astype(np.float64) - want) <= tol).all()
+    assert (np.abs(lse - want_lse) <= 2.0 ** -20 * (scale + np.abs(want_lse) + 1)).all()
