@@ -57,7 +57,7 @@
 extern "C" {
 #endif
 
-#define FASQ_ABI_VERSION 7
+#define FASQ_ABI_VERSION 8
 
 typedef enum {
   FASQ_OK = 0,
@@ -495,10 +495,127 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_token_stride, int64_t 
                                  void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
                                  void* workspace, int64_t workspace_bytes, hipStream_t stream);
 
+/*
+ * What attention may have besides (fasq_paged_attention_ex).  A field that is 0
+ * or NULL is not there; with all of them so the call is fasq_paged_attention.
+ *
+ *   softcap  c > 0: a score s becomes c * tanh(s / c).  2^-10 <= c <= 1024, |scale|
+ *            <= 2^64; a capped score is off by at most 2^-21 c
+ *   slopes   fp32 [Hq], finite: query head h at position p adds -slopes[h] * |p - j|
+ *            to its score with key j (before a cap).  2^-24 <= |scale| <= 2^64
+ *   spans    int32 [T x 2]: token t sees the keys spans[t][0] <= j < spans[t][1]
+ *            (cut to what there is) in place of causal and window (window must
+ *            be 0): documents packed into one request, prefixes that are read in
+ *            both directions, windows over other positions
+ *   tree     int32 [T rows of tree_words words, tree_stride words apart]: of the
+ *            request's n new tokens, which are its last n keys, token t sees the
+ *            i-th exactly if bit i % 32 of its word i / 32 is set (itself among
+ *            them); words past tree_words are zero, bits from n on are not used.
+ *            The keys before the new tokens it sees all, or those of its span;
+ *            causal is not used and window must be 0.  Not with slopes
+ */
+typedef struct {
+  float softcap;
+  const float* slopes;
+  const int32_t* spans;
+  const int32_t* tree;
+  int64_t tree_stride, tree_words;
+} fasq_attention_scores;
+
+/*
+ * fasq_paged_attention with scores and masks of the call's own; `scores` NULL:
+ * none.  Everything else, the workspace too, is as there: a token that sees no
+ * key gets out = 0 and lse = -inf, and what a token does not see does not reach
+ * its output, whatever it holds.
+ *
+ * Returns FASQ_ERR_INVALID_ARG, FASQ_ERR_UNSUPPORTED (as there; softcap above
+ * 1024; slopes with tree) or FASQ_ERR_HIP.
+ */
+fasq_status fasq_paged_attention_ex(const void* q, int64_t q_token_stride, int64_t q_head_stride, int64_t T, int Hq,
+                                    const fasq_kv_cache* cache, int Hkv, int D,
+                                    const int32_t* pages, int64_t page_row_stride, int64_t max_pages,
+                                    const int32_t* q_start, const int32_t* kv_len, int64_t B,
+                                    float scale, int causal, int64_t window, const fasq_attention_scores* scores,
+                                    void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                                    void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
 /* Workspace bytes fasq_paged_attention splits keys with on the current device
  * for T tokens of B requests (0 when it would not split), -1 for invalid
  * sizes. */
 int64_t fasq_paged_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D);
+
+/*
+ * What stands between a model's logits and a token (fasq_process_logits).  Row r
+ * belongs to request s = requests[r].  A field that is NULL is not there.
+ *
+ *   requests      int32 [R]; NULL: row r is request r (S = R).  A row whose request
+ *                 lies outside [0, S) is neither read nor written
+ *   S             requests, at most 2^24
+ *   tokens        int32 [S rows of max_tokens, token_stride apart]: a request's
+ *                 prompt and then its answer so far, token_count[s] of them (int32
+ *                 [S]; cut to max_tokens, at most 2^30), the first prompt_len[s]
+ *                 (int32 [S]; NULL: none) the prompt.  Ids outside [0, V) do not count
+ *   repetition    fp32 [S], positive: a logit x of a token that occurs becomes
+ *                 x * (1 / repetition) if x > 0, else x * repetition
+ *   frequency     fp32 [S]: less frequency * n + presence for a token that occurs n
+ *   presence      > 0 times in the answer
+ *   bias_ids      int32 [S x max_bias] (at most 2^24) and bias_values fp32: added to these tokens'
+ *   bias_values   logits; a token's last entry counts, ids outside [0, V) do not
+ *   temperature   fp32 [S]: times 1 / temperature where that is positive
+ *   allowed       int32 [R rows of ceil(V / 32) words, allowed_stride apart]: a token
+ *                 whose bit v % 32 of word v / 32 is clear becomes -inf, whatever it was
+ *   draft_tokens  int32 [R], q_start int32 [S + 1], tree as in fasq_attention_scores:
+ *   q_start, tree the rows of request s are q_start[s] <= r < q_start[s + 1], row r has
+ *                 drafted draft_tokens[r], and the tokens of the rows that its bits
+ *                 name (itself among them) are counted with its answer
+ */
+typedef struct {
+  const int32_t* requests;
+  int64_t S;
+  const int32_t* tokens;
+  int64_t token_stride, max_tokens;
+  const int32_t* token_count;
+  const int32_t* prompt_len;
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  int64_t max_bias;
+  const float* temperature;
+  const int32_t* allowed;
+  int64_t allowed_stride;
+  const int32_t* draft_tokens;
+  const int32_t* q_start;
+  const int32_t* tree;
+  int64_t tree_stride, tree_words;
+} fasq_token_rules;
+
+/*
+ * R rows of V logits under the rules of `rules`, applied in the order above:
+ * penalties, bias, temperature, mask.  Arithmetic is fp32, an operation at a
+ * time (reciprocals rounded before they are used).
+ *
+ *   logits  fp16, or fp32 with logits_fp32; rows `stride` elements apart.  V <= 2^30
+ *   out     fp16 or fp32 (out_fp32), rows out_stride apart, or NULL; may be logits
+ *           (of the same type and stride)
+ *   choice  int32 [R] or NULL: the token of the largest value (before it is
+ *           rounded to out), the lowest of equal ones; NaN is larger than
+ *           all; -1 where every value is -inf
+ *   lse     fp32 [R] or NULL: the logarithm of the sum of the values' exponentials
+ *   workspace  device scratch of fasq_process_logits_workspace_bytes() bytes, 16-byte
+ *           aligned, overwritten; not used without choice and lse
+ *
+ * Returns FASQ_ERR_INVALID_ARG or FASQ_ERR_HIP.
+ */
+fasq_status fasq_process_logits(const void* logits, int logits_fp32, int64_t stride, int64_t R, int64_t V,
+                                const fasq_token_rules* rules, void* out, int out_fp32, int64_t out_stride,
+                                int32_t* choice, float* lse, void* workspace, int64_t workspace_bytes,
+                                hipStream_t stream);
+
+/* Workspace bytes fasq_process_logits needs for choice or lse on the current
+ * device; -1 for invalid sizes. */
+int64_t fasq_process_logits_workspace_bytes(int64_t R, int64_t V);
 
 /*
  * The residual stream between two blocks: the block's output y is normed (if

@@ -62,6 +62,9 @@ __all__ = [
     "rope_append",
     "paged_attention",
     "paged_attention_workspace_bytes",
+    "draft_tree",
+    "process_logits",
+    "process_logits_workspace_bytes",
     "residual_norm",
     "lora_batched",
     "lora_workspace_bytes",
@@ -71,7 +74,7 @@ __all__ = [
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfasq.so")
 
-ABI_VERSION = 7  # FASQ_ABI_VERSION of include/fasq.h
+ABI_VERSION = 8  # FASQ_ABI_VERSION of include/fasq.h
 
 FASQ_OK = 0
 FASQ_ERR_INVALID_ARG = 1
@@ -107,7 +110,10 @@ EXPORTED_SYMBOLS = (
     "fasq_rope_table",
     "fasq_rope_append",
     "fasq_paged_attention",
+    "fasq_paged_attention_ex",
     "fasq_paged_attention_workspace_bytes",
+    "fasq_process_logits",
+    "fasq_process_logits_workspace_bytes",
     "fasq_residual_norm",
     "fasq_lora_batched",
     "fasq_lora_workspace_bytes",
@@ -137,6 +143,23 @@ class KvCache(ctypes.Structure):
 
     _fields_ = [("k", _c_vp), ("v", _c_vp), ("num_pages", _c_i64), ("page_size", _c_i64), ("page_stride", _c_i64),
                 ("slot_stride", _c_i64), ("head_stride", _c_i64)]
+
+
+class AttentionScores(ctypes.Structure):
+    """``fasq_attention_scores``: caps, biases and masks of an attention call."""
+
+    _fields_ = [("softcap", ctypes.c_float), ("slopes", _c_vp), ("spans", _c_vp), ("tree", _c_vp), ("tree_stride", _c_i64),
+                ("tree_words", _c_i64)]
+
+
+class TokenRules(ctypes.Structure):
+    """``fasq_token_rules``: what stands between logits and tokens."""
+
+    _fields_ = [("requests", _c_vp), ("S", _c_i64), ("tokens", _c_vp), ("token_stride", _c_i64), ("max_tokens", _c_i64),
+                ("token_count", _c_vp), ("prompt_len", _c_vp), ("repetition", _c_vp), ("presence", _c_vp),
+                ("frequency", _c_vp), ("bias_ids", _c_vp), ("bias_values", _c_vp), ("max_bias", _c_i64),
+                ("temperature", _c_vp), ("allowed", _c_vp), ("allowed_stride", _c_i64), ("draft_tokens", _c_vp),
+                ("q_start", _c_vp), ("tree", _c_vp), ("tree_stride", _c_i64), ("tree_words", _c_i64)]
 
 
 def lib() -> ctypes.CDLL:
@@ -210,16 +233,24 @@ def lib() -> ctypes.CDLL:
         L.fasq_paged_attention.argtypes = [_c_vp, _c_i64, _c_i64, _c_i64, _c_int, ctypes.POINTER(KvCache), _c_int,
                                            _c_int, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, ctypes.c_float, _c_int,
                                            _c_i64, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, _c_vp]
+        L.fasq_paged_attention_ex.argtypes = [_c_vp, _c_i64, _c_i64, _c_i64, _c_int, ctypes.POINTER(KvCache), _c_int,
+                                              _c_int, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, ctypes.c_float,
+                                              _c_int, _c_i64, ctypes.POINTER(AttentionScores), _c_vp, _c_i64, _c_i64,
+                                              _c_vp, _c_vp, _c_i64, _c_vp]
+        L.fasq_process_logits.argtypes = [_c_vp, _c_int, _c_i64, _c_i64, _c_i64, ctypes.POINTER(TokenRules), _c_vp, _c_int,
+                                          _c_i64, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]
+        L.fasq_process_logits_workspace_bytes.argtypes = [_c_i64, _c_i64]
         L.fasq_paged_attention_workspace_bytes.argtypes = [_c_i64, _c_i64, _c_int, _c_int, _c_int]
         L.fasq_residual_norm.argtypes = [_c_vp, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, ctypes.c_float, _c_vp,
                                          ctypes.c_float, _c_vp, _c_vp, _c_vp]
         L.fasq_lora_batched.argtypes = [_c_vp, _c_i64, _c_i64, _c_vp, _c_i64, _c_int, _c_vp, _c_int, _c_vp, _c_vp,
                                         _c_vp, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]
         L.fasq_lora_workspace_bytes.argtypes = [_c_i64, _c_i64, _c_int, _c_int]
-        for name in ("fasq_rope_table", "fasq_rope_append", "fasq_paged_attention", "fasq_residual_norm",
-                     "fasq_lora_batched"):
+        for name in ("fasq_rope_table", "fasq_rope_append", "fasq_paged_attention", "fasq_paged_attention_ex",
+                     "fasq_process_logits", "fasq_residual_norm", "fasq_lora_batched"):
             getattr(L, name).restype = _c_int
-        for name in ("fasq_paged_attention_workspace_bytes", "fasq_lora_workspace_bytes"):
+        for name in ("fasq_paged_attention_workspace_bytes", "fasq_process_logits_workspace_bytes",
+                     "fasq_lora_workspace_bytes"):
             getattr(L, name).restype = _c_i64
         _lib = L
         return L
@@ -814,14 +845,21 @@ def paged_attention_workspace_bytes(T: int, B: int, Hq: int, Hkv: int, D: int) -
 
 
 def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional[float] = None, causal: bool = True,
-                    window: int = 0, out=None, return_lse: bool = False, workspace=None):
+                    window: int = 0, out=None, return_lse: bool = False, workspace=None, softcap: float = 0.0,
+                    slopes=None, spans=None, tree=None):
     """Attention of the new tokens ``q`` [T x Hq x D] of B requests over the paged
     caches [pages x page_size x Hkv x D]: request b has the tokens
     ``q_start[b] : q_start[b + 1]`` and the first ``kv_len[b]`` slots of the
     pages ``pages[b]`` (all int32).  Returns the output [T x Hq x D] (tokens of
     no request are not written), and with ``return_lse`` also the fp32 logarithms
     of the softmax sums [T x Hq].  ``scale`` is ``D ** -0.5`` unless given;
-    ``window`` 0 sees everything.  See ``fasq_paged_attention``."""
+    ``window`` 0 sees everything.  See ``fasq_paged_attention``.
+
+    ``softcap`` c > 0 takes ``c * tanh(score / c)`` for a score; ``slopes`` (fp32
+    [Hq]) take ``slopes[h] * |position - key|`` off it before that.  ``spans``
+    (int32 [T x 2]) give each token its run of keys in place of ``causal`` and
+    ``window``; ``tree`` (int32 [T x words]) says bit by bit which of the
+    request's new tokens a token sees (:func:`draft_tree`).  See ``fasq_attention_scores``."""
     torch = _torch()
     i32 = torch.int32
     _require_rows(q, "q", torch.float16, 3)
@@ -846,10 +884,26 @@ def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional
     lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if return_lse else None
     qs, os_ = q.stride(), out.stride()
     L = lib()
+    scores = None
+    if softcap or slopes is not None or spans is not None or tree is not None:
+        scores = AttentionScores(softcap)
+        if slopes is not None:
+            _check_tensor(slopes, "slopes", torch.float32, (Hq,), device)
+            scores.slopes = slopes.data_ptr()
+        if spans is not None:
+            _check_tensor(spans, "spans", i32, (T, 2), device)
+            scores.spans = spans.data_ptr()
+        if tree is not None:
+            scores.tree, scores.tree_stride, scores.tree_words = _tree(tree, T, device)
 
     def call(stream):
         need = L.fasq_paged_attention_workspace_bytes(T, B, Hq, Hkv, D) if workspace is None else 0
         ws, ws_bytes = _workspace(workspace, need, device, q)
+        if scores is not None:
+            return L.fasq_paged_attention_ex(q.data_ptr(), qs[0], qs[1], T, Hq, cache, Hkv, D, pages.data_ptr(),
+                                             pages.stride(0), pages.shape[1], q_start.data_ptr(), kv_len.data_ptr(), B,
+                                             D ** -0.5 if scale is None else scale, causal, window, scores,
+                                             out.data_ptr(), os_[0], os_[1], _ptr(lse), _ptr(ws), ws_bytes, stream)
         return L.fasq_paged_attention(q.data_ptr(), qs[0], qs[1], T, Hq, cache, Hkv, D, pages.data_ptr(),
                                       pages.stride(0), pages.shape[1], q_start.data_ptr(), kv_len.data_ptr(), B,
                                       D ** -0.5 if scale is None else scale, causal, window, out.data_ptr(), os_[0],
@@ -857,6 +911,142 @@ def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional
 
     _check(_on_device(device, call))
     return (out, lse) if return_lse else out
+
+
+def _tree(tree, rows, device):
+    """Address, row stride and words of a tree's rows."""
+    _require_rows(tree, "tree", _torch().int32, 2)
+    if tree.shape[0] != rows or tree.shape[1] < 1:
+        raise ValueError(f"tree must be [{rows} x words], got {list(tree.shape)}")
+    _same_device(device, tree)
+    words = tree.shape[1]
+    return tree.data_ptr(), tree.stride(0) if rows > 1 else words, words
+
+
+def draft_tree(parents, device="cuda"):
+    """What :func:`paged_attention` and :func:`process_logits` take of trees of
+    drafted tokens: ``parents[b][i]`` is the node that request b's i-th new token
+    follows (an earlier one; -1: none, it follows what is cached).  Returns
+    ``(tree, depth)``: int32 [T x words], bit j of a node's row set for itself and
+    the nodes it follows, and int32 [T], how many those are before itself.  Both
+    are on ``device``; made once where all steps draft alike."""
+    torch = _torch()
+    words = max([1] + [-(-len(p) // 32) for p in parents])
+    rows, depth = [], []
+    for nodes in parents:
+        ways = []
+        for i, p in enumerate(nodes):
+            if not -1 <= p < i:
+                raise ValueError("a node follows an earlier one, or -1")
+            ways.append((ways[p] if p >= 0 else 0) | 1 << i)
+            depth.append(bin(ways[i]).count("1") - 1)
+        rows += [[w >> 32 * k & 0xFFFFFFFF for k in range(words)] for w in ways]
+    rows = torch.tensor(rows, dtype=torch.int64).reshape(-1, words)
+    tree = torch.where(rows >= 1 << 31, rows - (1 << 32), rows).to(torch.int32)
+    return tree.to(device), torch.tensor(depth, dtype=torch.int32).to(device)
+
+
+def process_logits_workspace_bytes(R: int, V: int) -> int:
+    return lib().fasq_process_logits_workspace_bytes(R, V)
+
+
+def process_logits(logits, requests=None, *, tokens=None, token_count=None, prompt_len=None, repetition=None, presence=None,
+                   frequency=None, bias_ids=None, bias_values=None, temperature=None, allowed=None, draft_tokens=None,
+                   q_start=None, tree=None, requests_count: Optional[int] = None, out=None, write: bool = True,
+                   choose: bool = False, workspace=None):
+    """Rows of logits [R x V] (fp16 or fp32) under the rules of their requests,
+    row r of request ``requests[r]`` (int32 [R]; None: row r of request r; a row
+    whose request does not exist is left alone).
+
+    ``tokens`` (int32 [S x L], the first ``token_count[s]`` of each row, of them
+    ``prompt_len[s]`` the prompt) take the penalties ``repetition``, ``presence``
+    and ``frequency`` (fp32 [S]); with drafted trees (``draft_tokens`` [R],
+    ``q_start`` [S + 1], ``tree`` [R x words]) a node's own and its ancestors'
+    tokens are counted too.  ``bias_ids`` and ``bias_values`` [S x E] add to single
+    logits, ``temperature`` [S] divides all, and ``allowed`` (int32 [R x
+    ceil(V / 32)]) leaves the tokens whose bit is set.  S is taken from these, or
+    from ``requests_count`` where none is given.
+
+    Returns the rows (``out``, fp16 or fp32, may be ``logits``; None with ``write``
+    False), or with ``choose`` ``(rows, choice, lse)``: the likeliest tokens (int32
+    [R], the lowest of equal ones; -1: none is allowed) and the logarithms of the
+    softmax sums (fp32 [R]).  See ``fasq_process_logits``."""
+    torch = _torch()
+    i32, f32 = torch.int32, torch.float32
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError("logits must be a torch.Tensor")
+    wide = logits.dtype is f32
+    _require_rows(logits, "logits", f32 if wide else torch.float16, 2)
+    R, V = logits.shape
+    device = logits.get_device()
+    S = requests_count if requests_count is not None else R if requests is None else None
+    for t, dims in ((token_count, 1), (prompt_len, 1), (repetition, 1), (presence, 1), (frequency, 1), (temperature, 1),
+                    (tokens, 2), (bias_ids, 2)):
+        if S is None and t is not None:
+            if not isinstance(t, torch.Tensor) or t.dim() != dims:
+                raise ValueError("rules must be tensors [S] or [S x ..]")
+            S = t.shape[0]
+    if S is None:
+        S = (1 << 24) if q_start is None else q_start.shape[0] - 1
+    rules = TokenRules(0, S)
+    if requests is not None:
+        _check_tensor(requests, "requests", i32, (R,), device)
+        rules.requests = requests.data_ptr()
+    for name, t, dtype in (("token_count", token_count, i32), ("prompt_len", prompt_len, i32),
+                           ("repetition", repetition, f32), ("presence", presence, f32), ("frequency", frequency, f32),
+                           ("temperature", temperature, f32)):
+        if t is not None:
+            _check_tensor(t, name, dtype, (S,), device)
+            setattr(rules, name, t.data_ptr())
+    if (tokens is None) != (token_count is None) or (bias_ids is None) != (bias_values is None):
+        raise ValueError("tokens come with token_count, bias_ids with bias_values")
+    if tokens is not None:
+        _require_rows(tokens, "tokens", i32, 2)
+        _check_rows(tokens, "tokens", i32, (S, tokens.shape[1]), device)
+        rules.tokens, rules.token_stride, rules.max_tokens = tokens.data_ptr(), tokens.stride(0), tokens.shape[1]
+    if bias_ids is not None:
+        _require(bias_ids, "bias_ids", i32, 2)
+        _check_tensor(bias_ids, "bias_ids", i32, (S, bias_ids.shape[1]), device)
+        rules.bias_ids, rules.max_bias = bias_ids.data_ptr(), bias_ids.shape[1]
+    if bias_values is not None:
+        _check_tensor(bias_values, "bias_values", f32, bias_ids.shape, device)
+        rules.bias_values = bias_values.data_ptr()
+    if allowed is not None:
+        _check_rows(allowed, "allowed", i32, (R, (V + 31) // 32), device)
+        rules.allowed, rules.allowed_stride = allowed.data_ptr(), allowed.stride(0)
+    if draft_tokens is not None:
+        _check_tensor(draft_tokens, "draft_tokens", i32, (R,), device)
+        rules.draft_tokens = draft_tokens.data_ptr()
+    if q_start is not None:
+        _check_tensor(q_start, "q_start", i32, (S + 1,), device)
+        rules.q_start = q_start.data_ptr()
+    if tree is not None:
+        rules.tree, rules.tree_stride, rules.tree_words = _tree(tree, R, device)
+    out_wide = False
+    if not write:
+        if out is not None:
+            raise ValueError("out is given, but write is False")
+    elif out is None:
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+        out_wide = wide
+    else:
+        out_wide = isinstance(out, torch.Tensor) and out.dtype is f32
+        _check_rows(out, "out", f32 if out_wide else torch.float16, (R, V), device)
+    choice = lse = None
+    if choose:
+        choice = torch.empty((R,), dtype=i32, device=logits.device)
+        lse = torch.empty((R,), dtype=f32, device=logits.device)
+    L = lib()
+
+    def call(stream):
+        need = L.fasq_process_logits_workspace_bytes(R, V) if choose and workspace is None else 0
+        ws, ws_bytes = _workspace(workspace, need, device, logits)
+        return L.fasq_process_logits(logits.data_ptr(), wide, logits.stride(0), R, V, rules, _ptr(out), out_wide,
+                                     out.stride(0) if out is not None else 0, _ptr(choice), _ptr(lse), _ptr(ws), ws_bytes,
+                                     stream)
+
+    _check(_on_device(device, call))
+    return (out, choice, lse) if choose else out
 
 
 def residual_norm(x, y=None, weight=None, eps: float = 1e-5, post_weight=None, gate=None, scale: float = 1.0,

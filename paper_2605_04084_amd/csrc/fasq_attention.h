@@ -26,6 +26,15 @@ namespace fasq {
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef half8_t half8_any __attribute__((aligned(2)));
 
+// What a kernel's variant has besides scaled products, causality and windows.
+// MORE: masks of a call's own (runs of keys, trees of drafted tokens); CAP:
+// scores capped by a tanh; SLOPES: scores with a bias that grows with the distance.
+template <bool MORE, bool CAP, bool SLOPES>
+struct Variant {
+  static constexpr bool kMore = MORE, kCap = CAP, kSlopes = SLOPES;
+};
+using Plain = Variant<false, false, false>;
+
 // A request as the kernels read it: lengths cut to what exists.
 struct Request {
   int q0, n, kv;
@@ -69,6 +78,16 @@ struct AttentionArgs {
   float* part_o;  // [2 * parts][rows][DP], not divided by the sum
   float* part_ml;  // [2 * parts][rows][2]: maximum (in powers of two), sum
   CutTile* cuts;   // [parts]
+  // Of variants besides Plain:
+  const int32_t* spans;  // [T][2]: the keys that each token sees, or NULL (causal, window)
+  const int32_t* tree;   // [T][tree_words]: which new tokens each one sees, or NULL
+  int64_t tree_stride;
+  int tree_words;
+  const float* slopes;  // [Hq]
+  float slope_unit;     // a slope times this is one in units of the raw products
+  // With z = scale q.k in powers of two, capped scores are cap * tanh(z / cap)
+  // = cap - 2 cap / (1 + 2^(s cap_in)) of the raw product s.
+  float cap, cap_in;
 };
 
 // The kernel's arguments (its only parameter), as if read for the first time:
@@ -122,7 +141,17 @@ struct Span {
   int begin, end;
 };
 
+template <class V>
 __device__ __forceinline__ Span token_span(const AttentionArgs& a, const Request& r, int i) {
+  if constexpr (V::kMore) {
+    if (a.spans != nullptr) {
+      int begin = a.spans[2 * ((int64_t)r.q0 + i)], end = a.spans[2 * ((int64_t)r.q0 + i) + 1];
+      end = end < 0 ? 0 : end < r.kv ? end : r.kv;
+      begin = begin < 0 ? 0 : begin < end ? begin : end;
+      return {begin, end};
+    }
+    if (a.tree != nullptr) return {0, r.kv};
+  }
   const int pos = r.kv - r.n + i;  // may be negative: more new tokens than keys
   int end = a.causal && pos + 1 < r.kv ? pos + 1 : r.kv;
   int begin = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
@@ -130,13 +159,114 @@ __device__ __forceinline__ Span token_span(const AttentionArgs& a, const Request
   return {begin < end ? begin : end, end};
 }
 
-// Keys that some token of tile t (ROWS rows) sees.
-template <int ROWS>
-__device__ __forceinline__ Span tile_span(const AttentionArgs& a, const Request& r, int t) {
-  const int rows = r.n * a.G;
-  const int last = (t + 1) * ROWS < rows ? (t + 1) * ROWS : rows;
-  const Span s0 = token_span(a, r, token_of(a, t * ROWS)), s1 = token_span(a, r, token_of(a, last - 1));
-  return {s0.begin < s1.begin ? s0.begin : s1.begin, s1.end > s0.end ? s1.end : s0.end};
+// Keys of a wave's rows, lane by lane: what all of them see, and some.
+struct Spans {
+  Span all, any;
+};
+// LANES lanes hold a row each (and every LANES lanes the same rows); `live`: the lane has one.
+template <int LANES>
+__device__ __forceinline__ Spans join_spans(Span s, bool live) {
+  Spans r = {live ? s : Span{0, INT32_MAX}, live && s.begin < s.end ? s : Span{INT32_MAX, 0}};
+#pragma unroll
+  for (int x = 1; x < LANES; x *= 2) {
+    r.all.begin = max(r.all.begin, __shfl_xor(r.all.begin, x, kWave));
+    r.all.end = min(r.all.end, __shfl_xor(r.all.end, x, kWave));
+    r.any.begin = min(r.any.begin, __shfl_xor(r.any.begin, x, kWave));
+    r.any.end = max(r.any.end, __shfl_xor(r.any.end, x, kWave));
+  }
+  if (r.any.begin >= r.any.end) r.any = {0, 0};
+  return {{__builtin_amdgcn_readfirstlane(r.all.begin), __builtin_amdgcn_readfirstlane(r.all.end)},
+          {__builtin_amdgcn_readfirstlane(r.any.begin), __builtin_amdgcn_readfirstlane(r.any.end)}};
+}
+
+// The same of the rows [row, row + count) of a request, count <= 2 * kWave.
+template <class V>
+__device__ __forceinline__ Spans row_spans(const AttentionArgs& a, const Request& r, int row, int count) {
+  Spans s;
+  if (V::kMore && a.spans != nullptr) {
+    const int lane = threadIdx.x % kWave;
+    const Span first = token_span<V>(a, r, token_of(a, row + (lane < count ? lane : 0)));
+    s = join_spans<kWave>(first, true);
+    if (count > kWave) {
+      const Span second = token_span<V>(a, r, token_of(a, row + (kWave + lane < count ? kWave + lane : 0)));
+      const Spans t = join_spans<kWave>(second, true);
+      s.all = {max(s.all.begin, t.all.begin), min(s.all.end, t.all.end)};
+      if (s.any.begin >= s.any.end) s.any = t.any;
+      else if (t.any.begin < t.any.end) s.any = {min(s.any.begin, t.any.begin), max(s.any.end, t.any.end)};
+    }
+  } else {
+    const Span s0 = token_span<V>(a, r, token_of(a, row)), s1 = token_span<V>(a, r, token_of(a, row + count - 1));
+    s.all = {s0.begin > s1.begin ? s0.begin : s1.begin, s0.end < s1.end ? s0.end : s1.end};
+    s.any = {s0.begin < s1.begin ? s0.begin : s1.begin, s1.end > s0.end ? s1.end : s0.end};
+  }
+  if constexpr (V::kMore) {
+    // of the new tokens, which a tree's words tell about, none is seen by all
+    if (a.tree != nullptr && s.all.end > r.kv - r.n) s.all.end = r.kv - r.n;
+  }
+  return s;
+}
+
+// Which new tokens a row of a tree sees: bit j % 32 of word j / 32 tells about
+// the request's j-th new token, which is key `first` + j.
+struct TreeRow {
+  const int32_t* words;
+  int count, first;
+  // The bits of keys key0 .. key0 + 31; those before `first` are set.
+  __device__ __forceinline__ uint32_t block(int key0) const {
+    const int64_t at = (int64_t)key0 - first;
+    const int w = (int)(at >> 5), shift = (int)(at & 31);
+    const uint32_t lo = word(w), hi = word(w + 1);
+    return shift == 0 ? lo : lo >> shift | hi << (32 - shift);
+  }
+  __device__ __forceinline__ uint32_t word(int w) const {
+    return w < 0 ? 0xFFFFFFFFu : w < count ? (uint32_t)words[w] : 0u;
+  }
+};
+__device__ __forceinline__ TreeRow tree_row(const AttentionArgs& a, const Request& r, int i) {
+  return {a.tree + ((int64_t)r.q0 + i) * a.tree_stride, a.tree_words, r.kv - r.n};
+}
+
+// Whether token i sees any key.  Only rows without a weight need to know.
+template <class V>
+__device__ __forceinline__ bool token_sees(const AttentionArgs& a, const Request& r, int i) {
+  const Span s = token_span<V>(a, r, i);
+  if constexpr (V::kMore) {
+    if (a.tree != nullptr && s.begin < s.end) {
+      const TreeRow row = tree_row(a, r, i);
+      if (s.begin < row.first) return true;
+      for (int k = s.begin; k < s.end; k += 32) {
+        const uint32_t bits = row.block(k);
+        if ((s.end - k < 32 ? bits & ((1u << (s.end - k)) - 1) : bits) != 0) return true;
+      }
+      return false;
+    }
+  }
+  return s.begin < s.end;
+}
+
+// The bias of a row's scores: slope * -|position - key|, in units of the raw
+// products, less that of the nearest key it may see (so that a row far from all
+// its keys loses nothing to it; not where scores are capped).
+struct RowBias {
+  float slope;      // negative for positive slopes
+  int pos, nearest; // the distance of the nearest key
+};
+template <class V>
+__device__ __forceinline__ RowBias row_bias(const AttentionArgs& a, const Request& r, int head, int row) {
+  const int t = token_of(a, row), pos = r.kv - r.n + t;
+  const float slope = -a.slopes[head * a.G + row - t * a.G] * a.slope_unit;
+  int nearest = 0;
+  if constexpr (!V::kCap) {
+    const Span s = token_span<V>(a, r, t);
+    if (s.begin < s.end) nearest = pos >= s.end ? pos - s.end + 1 : pos < s.begin ? s.begin - pos : 0;
+  }
+  return {slope, pos, nearest};
+}
+// What the nearest key's bias adds to a logarithm of a sum.
+template <class V>
+__device__ __forceinline__ float lse_bias(const AttentionArgs& a, const Request& r, int head, int row) {
+  const RowBias b = row_bias<V>(a, r, head, row);
+  return b.nearest == 0 ? 0.f : b.slope * a.c * (float)b.nearest * 0.69314718055994530942f;
 }
 
 // The batch as a line of positions.  With `parts` shares, every cache head
@@ -152,10 +282,21 @@ struct Place {
   int64_t start, end;  // the tile's positions
 };
 
-template <int ROWS, int STEP>
+template <class V, int ROWS, int STEP>
 __device__ __forceinline__ int64_t tile_length(const AttentionArgs& a, const Request& r, bool shared) {
   if (!shared) return 1;
   int keys = r.kv;
+  if constexpr (V::kMore) {
+    // where a few tokens see runs of keys of their own, the keys that some of them sees
+    if (a.spans != nullptr && r.n <= 8) {
+      Span s = {INT32_MAX, 0};
+      for (int i = 0; i < r.n; ++i) {
+        const Span t = token_span<V>(a, r, i);
+        if (t.begin < t.end) s = {min(s.begin, t.begin), max(s.end, t.end)};
+      }
+      keys = s.begin < s.end ? s.end - s.begin / 32 * 32 : 0;
+    }
+  }
   if (a.window > 0) {
     // of the tile's tokens, from a multiple of 32 on; without causality the
     // request's first token sees the window before it and all that follows
@@ -190,19 +331,19 @@ __device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r
 }
 
 // Positions of one cache head.
-template <int ROWS, int STEP>
+template <class V, int ROWS, int STEP>
 __device__ __forceinline__ int64_t head_length(const AttentionArgs& a, const Batch& batch, bool shared) {
   int64_t sum = 0;
   for (int64_t b = threadIdx.x % kWave; b < a.B; b += kWave) {
     const Request r = batch.of(a, b);
-    sum += tiles_of<ROWS>(a, r) * tile_length<ROWS, STEP>(a, r, shared);
+    sum += tiles_of<ROWS>(a, r) * tile_length<V, ROWS, STEP>(a, r, shared);
   }
   return a.B == 1 ? lane_value(sum, 0) : uniform(wave_total(sum));
 }
 
 // The tile at a position within a head's stretch, in every lane of the wave.
 // pos < head_length.
-template <int ROWS, int STEP>
+template <class V, int ROWS, int STEP>
 __device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& batch, int64_t pos, bool shared) {
   Place p = {};
   int64_t base = 0;
@@ -212,7 +353,7 @@ __device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& bat
     int64_t one = 0, own = 0;
     if (b < a.B) {
       r = batch.of(a, b);
-      one = tile_length<ROWS, STEP>(a, r, shared);
+      one = tile_length<V, ROWS, STEP>(a, r, shared);
       own = tiles_of<ROWS>(a, r) * one;
     }
     int64_t upto = own;  // positions up to and with this lane's request
@@ -405,13 +546,97 @@ __device__ __forceinline__ bool cut_to_finite(uint16_t* values) {
 // it: such rows end not finite and are computed again (SlowRow).
 constexpr float kLift = 7.f;
 
-template <int DP, int KB>
+// Capped scores, in powers of two (see AttentionArgs::cap).  1 / (1 + e) and
+// 2^x are off by an ulp each, which makes 2^-22 of the cap.
+__device__ __forceinline__ float capped(const AttentionArgs& a, float s) {
+  return fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * a.cap_in)), a.cap);
+}
+// A key that a row does not see, in a variant with capped scores (where -inf is a
+// score like others), and the least score that counts for a maximum.
+constexpr float kUnseen = -3.3e38f, kLeast = -3e38f;
+
+template <class V, int DP, int KB>
 struct WaveTile {
   half8_t q[DP / 16];
   float16_t o[DP / 32];
   // running maximum of the scores (this row), and m * c - kLift (0 without one)
   float m, mc;
   float l, rest;  // sum of this lane's weights, and what its last addition rounded up
+  RowBias bias;   // with SLOPES
+  TreeRow tree;   // with MORE, in calls with a tree
+  bool has_tree;
+
+  // The weight of a capped score: an operation of its own after the other where they are many (block()).
+  __device__ __forceinline__ float capped_weight(const AttentionArgs& a, float s) const {
+    const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * a.cap_in));
+    return __builtin_amdgcn_exp2f(fmaf(-2.f * a.cap, r, a.cap - mc));
+  }
+
+  // What variants need of row `row`, which exists.
+  __device__ __forceinline__ void load_row(const AttentionArgs& a, const Request& r, int head, int row) {
+    if constexpr (V::kSlopes) bias = row_bias<V>(a, r, head, row);
+    if constexpr (V::kMore) {
+      has_tree = a.tree != nullptr;
+      if (has_tree) tree = tree_row(a, r, token_of(a, row));
+    }
+  }
+
+  // The scores that the products with a block's keys are added to.
+  __device__ __forceinline__ float16_t before(int key0) const {
+    float16_t s = {};
+    if constexpr (V::kSlopes) {
+      const int h4 = threadIdx.x % kWave / 32 * 4;
+      // at most 2^31 - 1024 + 64: keys behind the last one may be named
+      const int back = bias.pos - key0 - h4 - bias.nearest;
+      if (__all(bias.pos - key0 - 31 >= 0)) {
+        const float base = bias.slope * (float)back;
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          // factors that instructions hold themselves: no registers for them
+          s[e] = e == 0 ? base : fmaf(bias.slope, -4.f, fmaf(bias.slope, -4.f, s[e == 0 ? 0 : e - 4]));
+          s[e + 1] = s[e] - bias.slope;
+          s[e + 2] = fmaf(bias.slope, -2.f, s[e]);
+          s[e + 3] = fmaf(bias.slope, -2.f, s[e + 1]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int d = back + bias.nearest - ((e / 4) * 8 + e % 4);
+          s[e] = bias.slope * (float)((d < 0 ? -d : d) - bias.nearest);
+        }
+      }
+    }
+    return s;
+  }
+
+  // A maximum of scores in powers of two.
+  __device__ __forceinline__ float scaled(const AttentionArgs& a, float top) const {
+    return V::kCap ? capped(a, top) : top * a.c;
+  }
+
+  // A block's scores with those that the row does not see taken out; returns the largest of this lane's.
+  __device__ __forceinline__ float mask(float16_t& s, int key0, int begin, int end) const {
+    const int h4 = threadIdx.x % kWave / 32 * 4, first = begin - key0 - h4, last = end - key0 - h4;
+    uint32_t bits = 0xFFFFFFFFu;
+    if constexpr (V::kMore) {
+      if (has_tree && key0 + 32 > tree.first) bits = tree.block(key0) >> h4;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int key = (e / 4) * 8 + e % 4;
+      bool out = key < first || key >= last;
+      if constexpr (V::kMore) out = out || !(bits >> key & 1);
+      if constexpr (V::kCap) {
+        top = fmaxf(top, out ? -INFINITY : fmaxf(s[e], kLeast));
+        s[e] = out ? kUnseen : s[e];
+      } else {
+        s[e] = out ? -INFINITY : s[e];
+        top = fmaxf(top, s[e]);
+      }
+    }
+    return top;
+  }
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -463,7 +688,8 @@ struct WaveTile {
   // sees all of the tile.  Operands are read from LDS a step or two ahead of
   // the products that take them; the scheduling barriers keep them there.
   __device__ __forceinline__ void step(const uint16_t* keys, const uint16_t* values, int key0, int begin, int end,
-                                       bool masked, float c) {
+                                       bool masked, const AttentionArgs& a) {
+    const float c = a.c;
     const int lane = threadIdx.x % kWave, l32 = lane % 32, h = lane / 32;
     constexpr int KT = DP / 16, AHEAD = 2;
     const uint32_t k_at = lds_address(keys) + l32 * (DP * 2) + (h ^ chunk_swap<DP>(l32)) * 16;
@@ -476,13 +702,17 @@ struct WaveTile {
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t) read_k(t);
     float16_t s[KB];
+    if constexpr (V::kSlopes)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb] = before(key0 + kb * 32);
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
       if (t + AHEAD < KT) read_k(t + AHEAD);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t % (AHEAD + 1)][kb], q[t], t == 0 ? float16_t{} : s[kb], 0, 0, 0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t % (AHEAD + 1)][kb], q[t],
+                                                       t == 0 && !V::kSlopes ? float16_t{} : s[kb], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
     // rows of V in the order of the score registers: weight j of slab u is
@@ -508,21 +738,36 @@ struct WaveTile {
     };
     read_v(0);
     __builtin_amdgcn_sched_barrier(0);
-    if (masked) {
-      const int first = begin - key0 - h * 4, last = end - key0 - h * 4;
+    float top;
+    if constexpr (V::kCap || V::kMore) {
+      top = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        if (masked) {
+          top = fmaxf(top, mask(s[kb], key0 + kb * 32, begin, end));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+          if constexpr (V::kCap) top = fmaxf(top, kLeast);
+        }
+      }
+    } else {
+      if (masked) {
+        const int first = begin - key0 - h * 4, last = end - key0 - h * 4;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int key = kb * 32 + (e / 4) * 8 + e % 4;
+            s[kb][e] = key < first || key >= last ? -INFINITY : s[kb][e];
+          }
+      }
+      top = s[0][0];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = kb * 32 + (e / 4) * 8 + e % 4;
-          s[kb][e] = key < first || key >= last ? -INFINITY : s[kb][e];
-        }
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
     }
-    float top = s[0][0];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
     {
       const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       top = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
@@ -533,7 +778,7 @@ struct WaveTile {
     const bool grown = (top - m) * c > 8.f;  // from -inf too; not from -inf to -inf
     if (__any(grown)) {
       // the weights are 2^(s c - mc) with the rounded mc, here too
-      const float next_c = top * c - kLift;
+      const float next_c = scaled(a, top) - kLift;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
       scale_sum(keep);
 #pragma unroll
@@ -549,7 +794,13 @@ struct WaveTile {
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float w = __builtin_amdgcn_exp2f(s[kb][e] * c - mc);
+        float w;
+        if constexpr (V::kCap) {
+          w = capped_weight(a, s[kb][e]);
+          if (masked) w = s[kb][e] == kUnseen ? 0.f : w;
+        } else {
+          w = __builtin_amdgcn_exp2f(s[kb][e] * c - mc);
+        }
         sum += w;
         p[2 * kb + e / 8][e % 8] = static_cast<half_t>(w);
       }
@@ -639,7 +890,8 @@ struct WaveTile {
   }
 
   // Scores of a block alone.
-  __device__ __forceinline__ void scores(uint32_t k_at, float16_t& s) {
+  __device__ __forceinline__ void scores(uint32_t k_at, int key0, float16_t& s) {
+    if constexpr (V::kSlopes) s = before(key0);
     auto read = [&](int t) {
       ops[t % OPS] = __builtin_bit_cast(u32x4, *(lds_half8)(uintptr_t)((k_at ^ (t % 8 * 32)) + t / 8 * 256));
     };
@@ -650,17 +902,19 @@ struct WaveTile {
       if (t + OPS - 1 < N) read(t + OPS - 1);
       __builtin_amdgcn_sched_barrier(0);
       s = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, ops[t % OPS]), q[t],
-                                                 t == 0 ? float16_t{} : s, 0, 0, 0);
+                                                 t == 0 && !V::kSlopes ? float16_t{} : s, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 
   // Weights of scores alone.
-  __device__ __forceinline__ void weights(const float16_t& s, half8_t (&p)[2], float c) {
+  __device__ __forceinline__ void weights(const float16_t& s, half8_t (&p)[2], const AttentionArgs& a) {
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float w = __builtin_amdgcn_exp2f(s[e] * c - mc);
+      float w;
+      if constexpr (V::kCap) w = s[e] == kUnseen ? 0.f : capped_weight(a, s[e]);
+      else w = __builtin_amdgcn_exp2f(s[e] * a.c - mc);
       sum += w;
       p[e / 8][e % 8] = static_cast<half_t>(w);
     }
@@ -678,8 +932,14 @@ struct WaveTile {
   // of two (where nothing is masked).  p: weights that have not met their
   // values yet.
   __device__ __forceinline__ void settle(float16_t& s, float top, float over, half8_t (&p)[2], int key0, int begin,
-                                         int end, bool masked, float c) {
-    if (masked) {
+                                         int end, bool masked, const AttentionArgs& a) {
+    const float c = a.c;
+    if constexpr (V::kCap || V::kMore) {
+      if (masked) {
+        top = row_max(mask(s, key0, begin, end));
+        over = (top - m) * c;
+      }
+    } else if (masked) {
       const int h4 = threadIdx.x % kWave / 32 * 4, first = begin - key0 - h4, last = end - key0 - h4;
       top = -INFINITY;
 #pragma unroll
@@ -693,7 +953,7 @@ struct WaveTile {
     }
     const bool grown = over > 8.f;  // as in step()
     if (__any(grown)) {
-      const float next_c = top * c - kLift;
+      const float next_c = scaled(a, top) - kLift;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
       scale_sum(keep);
 #pragma unroll
@@ -713,13 +973,35 @@ struct WaveTile {
   // of the row (top) and by how much it passes the maximum (over).  The operands
   // of the first three steps are there; those of the block after this one are
   // read if `more` (32 rows further).  at_step(i): what else step i issues.
+  // next_key: the first key of the scores `next`.
   template <typename F>
   __device__ __forceinline__ void block(const float16_t& s, float16_t& next, const half8_t (&p)[2], half8_t (&made)[2],
-                                        const Lanes& at, uint32_t k_off, uint32_t v_off, bool more, float c,
-                                        float& top, float& over, F at_step) {
+                                        const Lanes& at, uint32_t k_off, uint32_t v_off, bool more,
+                                        const AttentionArgs& a, int next_key, float& top, float& over, F at_step) {
+    const float c = a.c;
     constexpr int STEPS = 2 * N;
     float w[16], sum;
     u32x4 packed[2];
+    float ex[16], lift = 0.f, drop = 0.f;
+    if constexpr (V::kCap) {
+      lift = a.cap - mc;
+      drop = -2.f * a.cap;
+    }
+    if constexpr (V::kSlopes) next = before(next_key);
+    // with CAP a weight is three operations in turn, each an element behind the one before it
+    auto first_of = [&](int e) {
+      ex[e] = 1.f + __builtin_amdgcn_exp2f(s[e] * a.cap_in);
+      asm volatile("" : "+v"(ex[e]));
+    };
+    auto second_of = [&](int e) {
+      ex[e] = __builtin_amdgcn_rcpf(ex[e]);
+      asm volatile("" : "+v"(ex[e]));
+    };
+    if constexpr (V::kCap) {
+      first_of(0);
+      first_of(1);
+      second_of(0);
+    }
     auto add = [&](int e) {
       sum = e == 0 ? w[0] : sum + w[e];
       asm volatile("" : "+v"(sum));
@@ -737,7 +1019,7 @@ struct WaveTile {
       else if (more) read_op(at, k_off + 32 * DP * 2, v_off + 32 * DP * 2, j - STEPS);
       __builtin_amdgcn_sched_barrier(0);
       const half8_t op = __builtin_bit_cast(half8_t, ops[i % OPS]);
-      if (is_key(i)) next = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, q[nth(i)], i == 0 ? float16_t{} : next, 0, 0, 0);
+      if (is_key(i)) next = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, q[nth(i)], i == 0 && !V::kSlopes ? float16_t{} : next, 0, 0, 0);
       else {
         const int u = nth(i) / (DP / 32), d = nth(i) % (DP / 32);
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op, p[u], o[d], 0, 0, 0);
@@ -747,7 +1029,14 @@ struct WaveTile {
         // computed here, not where it is used: the compiler would move it
         // there (the empty asm statements); a weight is added up a step later,
         // when the exponential is there
-        w[e] = __builtin_amdgcn_exp2f(s[e] * c - mc);
+        if constexpr (V::kCap) {
+          if (e + 2 < 16) first_of(e + 2);
+          w[e] = __builtin_amdgcn_exp2f(fmaf(drop, ex[e], lift));
+          w[e] = s[e] == kUnseen ? 0.f : w[e];
+          if (e + 1 < 16) second_of(e + 1);
+        } else {
+          w[e] = __builtin_amdgcn_exp2f(s[e] * c - mc);
+        }
         asm volatile("" : "+v"(w[e]));
         if (e >= 1) add(e - 1);
       }
@@ -759,6 +1048,7 @@ struct WaveTile {
       }
       if (i == SCORED + 4) {
         top = row_max(top);
+        if constexpr (V::kCap) top = fmaxf(top, kLeast);
         over = (top - m) * c;
         asm volatile("" : "+v"(top), "+v"(over));
       }
@@ -804,31 +1094,56 @@ __device__ __forceinline__ float row_lse(float mc, float l, bool sees) {
   return (mc + __log2f(l)) * 0.69314718055994530942f;
 }
 
+// The logarithm of a row's sum as it is returned.
+template <class V>
+__device__ __forceinline__ float final_lse(float mc, float l, bool sees, const AttentionArgs& a, const Request& r,
+                                           int head, int row) {
+  const float lse = row_lse(mc, l, sees);
+  if constexpr (V::kSlopes && !V::kCap) return lse + lse_bias<V>(a, r, head, row);
+  return lse;
+}
+
 // One row over the keys [begin, end), key by key, by a whole wave: for rows
 // whose result is not finite, or whose masked tiles held values that are not.
 // Only keys that the row sees are touched.  Lane l holds dimensions l, l + 64, ...
-template <int DP>
+template <class V, int DP>
 struct SlowRow {
   float m = -INFINITY, l = 0.f, o[(DP + kWave - 1) / kWave] = {};
 
+  // r, head, row: as in query_row
   __device__ __forceinline__ void run(const AttentionArgs& a, const uint16_t* q, int64_t head_off,
-                                      const int32_t* pages, int begin, int end) {
+                                      const int32_t* pages, const Request& r, int head, int row, int begin, int end) {
+    RowBias bias = {};
+    if constexpr (V::kSlopes) bias = row_bias<V>(a, r, head, row);
+    const bool has_tree = V::kMore && a.tree != nullptr;
+    TreeRow tree = {};
+    if (has_tree) tree = tree_row(a, r, token_of(a, row));
     const int lane = threadIdx.x % kWave;
     for (int j0 = begin; j0 < end; j0 += kWave) {
       const int j = j0 + lane;
       float s = -INFINITY;
       int64_t off = 0;
-      if (j < end) {
+      const bool seen = j < end && (!has_tree || (tree.block(j) & 1) != 0);
+      if (seen) {
         off = key_offset(a, page_of(a, pages, j), j) + head_off;
         s = 0.f;
         for (int i = 0; i < a.D; ++i) s += half_value(q[i]) * half_value(a.ck[off + i]);
-        s *= a.negate ? -a.c : a.c;
+        if constexpr (V::kSlopes || V::kCap) {
+          s = a.negate ? -s : s;
+          if constexpr (V::kSlopes) {
+            const int d = bias.pos - j;
+            s += bias.slope * (float)((d < 0 ? -d : d) - bias.nearest);
+          }
+          s = V::kCap ? capped(a, s) : s * a.c;
+        } else {
+          s *= a.negate ? -a.c : a.c;
+        }
       }
       float top = s;
 #pragma unroll
       for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kWave));
       const float next = fmaxf(m, top);
-      const float p = j < end ? exp2f(s - (next == -INFINITY ? 0.f : next)) : 0.f;
+      const float p = seen ? exp2f(s - (next == -INFINITY ? 0.f : next)) : 0.f;
       const float keep = l == 0.f ? 0.f : exp2f(m - next);
       l = l * keep + wave_sum(p);
       m = next;
@@ -837,6 +1152,7 @@ struct SlowRow {
       const int count = end - j0 < kWave ? end - j0 : kWave;
       for (int e = 0; e < count; ++e) {
         const float w = __shfl(p, e, kWave);
+        if (V::kMore && !__shfl((int)seen, e, kWave)) continue;
         const int64_t vo = __shfl(off, e, kWave);
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(o) / sizeof(float)); ++i)
@@ -850,7 +1166,7 @@ struct SlowRow {
   // tiles' result stands for rows that see finite values alone.
   template <int ROWS>
   __device__ __forceinline__ void store(const AttentionArgs& a, const Request& r, int head, int row, int at,
-                                        int64_t slot, bool sees, bool broken) const {
+                                        int64_t slot, bool broken) const {
     const int lane = threadIdx.x % kWave;
     constexpr int N = (DP + kWave - 1) / kWave;
     float z = l - l;
@@ -868,14 +1184,15 @@ struct SlowRow {
       }
       return;
     }
-    const float f = row_factor(l, sees);
     const int t = token_of(a, row);
+    const bool sees = l != 0.f || token_sees<V>(a, r, t);
+    const float f = row_factor(l, sees);
     uint16_t* dst = a.out.p + (r.q0 + t) * a.out.ts + (head * a.G + row - t * a.G) * a.out.hs;
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (lane + i * kWave < a.D) dst[lane + i * kWave] = f32_to_f16_bits(o[i] * f);
     if (lane == 0 && a.lse != nullptr)
-      a.lse[(int64_t)(r.q0 + t) * a.Hq + head * a.G + row - t * a.G] = row_lse(m, l, sees);
+      a.lse[(int64_t)(r.q0 + t) * a.Hq + head * a.G + row - t * a.G] = final_lse<V>(m, l, sees, a, r, head, row);
   }
 };
 

@@ -1,0 +1,6 @@
+// Attention of new tokens over a paged cache with scores with a bias.
+#include "fasq_attention_kernels.h"
+
+namespace fasq {
+template hipError_t launch_variant<Variant<true, false, true>>(const AttentionPlan&, const AttentionArgs&, hipStream_t);
+}

@@ -42,6 +42,15 @@ hipError_t launch_rope_table(const double* inv_freq, int half, int64_t positions
                              hipStream_t stream);
 hipError_t launch_rope_append(const RopeProblem& p, hipStream_t stream);
 
+// What an attention call may have besides scaled products, causality and windows.
+struct AttentionMore {
+  float softcap;         // 0: none
+  const float* slopes;   // NULL: none
+  const int32_t* spans;  // NULL: none
+  const int32_t* tree;   // NULL: none
+  int64_t tree_stride, tree_words;
+};
+
 struct AttentionProblem {
   HeadsView q, out;
   int64_t T;
@@ -58,6 +67,7 @@ struct AttentionProblem {
   float* lse;
   void* workspace;
   int64_t workspace_bytes;
+  AttentionMore more;
 };
 int64_t attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D, const DeviceInfo& dev);
 hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hipStream_t stream);
@@ -98,6 +108,22 @@ struct LoraProblem {
 };
 int64_t lora_workspace_bytes(int64_t M, int64_t K, int r, int count, const DeviceInfo& dev);
 hipError_t launch_lora(const LoraProblem& p, const DeviceInfo& dev, hipStream_t stream);
+
+constexpr int64_t kMaxVocabulary = (int64_t(1) << 30);
+struct LogitsProblem {
+  const void* logits;
+  bool wide;  // fp32
+  int64_t stride, R, V;
+  fasq_token_rules rules;
+  void* out;  // NULL: not written
+  bool out_wide;
+  int64_t out_stride;
+  int32_t* choice;  // NULL: not asked for
+  float* lse;
+  void* workspace;
+};
+int64_t logits_workspace_bytes(int64_t R, int64_t V, const DeviceInfo& dev);
+hipError_t launch_logits(const LogitsProblem& p, const DeviceInfo& dev, hipStream_t stream);
 
 // The status of a launch, with fasq_last_error() set.
 fasq_status launch_status(hipError_t e);

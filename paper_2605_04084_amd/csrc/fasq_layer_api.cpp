@@ -33,6 +33,11 @@ constexpr int64_t kMaxTokens = int64_t(1) << 24;  // tokens of one call
 constexpr int64_t kMaxRequests = int64_t(1) << 16;  // each tile of attention is looked up among them
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
+constexpr float kMaxSoftcap = 1024.f;  // a capped score is off by 2^-22 of its cap
+constexpr float kMinSoftcap = 0.0009765625f;
+constexpr float kMaxScoresScale = 1.8446744e19f;
+constexpr float kMinSlopesScale = 5.9604645e-8f;  // slopes are taken in units of the unscaled products
+
 bool stride_ok(int64_t s) { return s >= 0 && s <= kMaxStride; }
 
 // A heads view of the caller: sizes, alignment of fp16, strides that do not
@@ -141,12 +146,12 @@ fasq_status fasq_rope_append(const void* q, int64_t q_ts, int64_t q_hs, int Hq, 
   return fasq::launch_status(fasq::launch_rope_append(p, stream));
 }
 
-fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int64_t T, int Hq,
-                                 const fasq_kv_cache* cache, int Hkv, int D, const int32_t* pages,
-                                 int64_t page_row_stride, int64_t max_pages, const int32_t* q_start,
-                                 const int32_t* kv_len, int64_t B, float scale, int causal, int64_t window, void* out,
-                                 int64_t out_ts, int64_t out_hs, float* lse, void* workspace, int64_t workspace_bytes,
-                                 hipStream_t stream) {
+fasq_status fasq_paged_attention_ex(const void* q, int64_t q_ts, int64_t q_hs, int64_t T, int Hq,
+                                    const fasq_kv_cache* cache, int Hkv, int D, const int32_t* pages,
+                                    int64_t page_row_stride, int64_t max_pages, const int32_t* q_start,
+                                    const int32_t* kv_len, int64_t B, float scale, int causal, int64_t window,
+                                    const fasq_attention_scores* scores, void* out, int64_t out_ts, int64_t out_hs,
+                                    float* lse, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
   if (T < 0 || T > fasq::kMaxTokens) return bad("T must lie in [0, 2^24]");
   if (B < (T > 0 ? 1 : 0) || B > fasq::kMaxRequests) return bad("B must lie in [1, 2^16] (0 only with T = 0)");
   if (Hkv < 1 || Hq < 1 || Hq > fasq::kMaxHeads || Hq % Hkv != 0) return bad("Hq must be a multiple of Hkv, both >= 1");
@@ -157,6 +162,26 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
     return bad("max_pages must be >= 1 and the page table's stride must not be negative");
   if (window < 0) return bad("window must be >= 0");
   if (std::isnan(scale)) return bad("scale must be a number");
+  fasq::AttentionMore more = {};
+  if (scores != nullptr) {
+    const fasq_attention_scores& m = *scores;
+    const bool sane = std::fabs(scale) <= fasq::kMaxScoresScale;
+    if (!(m.softcap >= 0.f)) return bad("softcap must be >= 0");
+    if (m.softcap > fasq::kMaxSoftcap) return fasq::fail(FASQ_ERR_UNSUPPORTED, "a softcap above 1024");
+    if (m.softcap > 0.f && m.softcap < fasq::kMinSoftcap) return bad("softcap must be 0 or at least 2^-10");
+    if (m.softcap > 0.f && !sane) return bad("softcap needs a scale of at most 2^64");
+    if (m.slopes != nullptr && !(sane && std::fabs(scale) >= fasq::kMinSlopesScale))
+      return bad("slopes need a scale of 2^-24 to 2^64");
+    if ((m.spans != nullptr || m.tree != nullptr) && window > 0) return bad("window must be 0 with spans or tree");
+    if (m.tree != nullptr && m.slopes != nullptr) return fasq::fail(FASQ_ERR_UNSUPPORTED, "slopes with tree");
+    if (m.tree != nullptr && (m.tree_words < 1 || m.tree_words > fasq::kMaxTokens || m.tree_stride < m.tree_words ||
+                              m.tree_stride > fasq::kMaxStride))
+      return bad("tree_words must be >= 1, tree_stride at least that");
+    if (fasq::misaligned(m.slopes, 4) || fasq::misaligned(m.spans, 4) || fasq::misaligned(m.tree, 4))
+      return bad("slopes, spans and tree must be 4-byte aligned");
+    more = {m.softcap, m.slopes, m.spans, m.tree, m.tree != nullptr ? m.tree_stride : 0,
+            m.tree != nullptr ? m.tree_words : 0};
+  }
   if (workspace_bytes < 0) return bad("workspace_bytes must be >= 0");
   if (T == 0) return fasq::launch_status(hipSuccess);  // buffers of no tokens may be NULL
   if (q == nullptr || out == nullptr || pages == nullptr || q_start == nullptr || kv_len == nullptr)
@@ -197,7 +222,19 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int6
   p.lse = lse;
   p.workspace = workspace;
   p.workspace_bytes = workspace_bytes;
+  p.more = more;
   return fasq::launch_status(fasq::launch_attention(p, dev, stream));
+}
+
+fasq_status fasq_paged_attention(const void* q, int64_t q_ts, int64_t q_hs, int64_t T, int Hq,
+                                 const fasq_kv_cache* cache, int Hkv, int D, const int32_t* pages,
+                                 int64_t page_row_stride, int64_t max_pages, const int32_t* q_start,
+                                 const int32_t* kv_len, int64_t B, float scale, int causal, int64_t window, void* out,
+                                 int64_t out_ts, int64_t out_hs, float* lse, void* workspace, int64_t workspace_bytes,
+                                 hipStream_t stream) {
+  return fasq_paged_attention_ex(q, q_ts, q_hs, T, Hq, cache, Hkv, D, pages, page_row_stride, max_pages, q_start,
+                                 kv_len, B, scale, causal, window, nullptr, out, out_ts, out_hs, lse, workspace,
+                                 workspace_bytes, stream);
 }
 
 int64_t fasq_paged_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int D) {
@@ -303,6 +340,88 @@ fasq_status fasq_lora_batched(const void* x, int64_t M, int64_t K, const int32_t
   p.y = y;
   p.workspace = workspace;
   return fasq::launch_status(fasq::launch_lora(p, dev, stream));
+}
+
+int64_t fasq_process_logits_workspace_bytes(int64_t R, int64_t V) {
+  if (R < 0 || R > fasq::kMaxTokens || V < 1 || V > fasq::kMaxVocabulary) return -1;
+  fasq::DeviceInfo dev;
+  if (fasq::device_info(&dev) != hipSuccess) return -1;
+  return fasq::logits_workspace_bytes(R, V, dev);
+}
+
+fasq_status fasq_process_logits(const void* logits, int logits_fp32, int64_t stride, int64_t R, int64_t V,
+                                const fasq_token_rules* rules, void* out, int out_fp32, int64_t out_stride,
+                                int32_t* choice, float* lse, void* workspace, int64_t workspace_bytes,
+                                hipStream_t stream) {
+  if (R < 0 || R > fasq::kMaxTokens) return bad("R must lie in [0, 2^24]");
+  if (V < 1 || V > fasq::kMaxVocabulary) return bad("V must lie in [1, 2^30]");
+  if (rules == nullptr) return bad("rules is NULL");
+  const fasq_token_rules& r = *rules;
+  if (r.S < 0 || r.S > fasq::kMaxTokens) return bad("S must lie in [0, 2^24]");
+  if (r.requests == nullptr && r.S != R) return bad("without requests every row is a request: S must be R");
+  if (R == 0) return fasq::launch_status(hipSuccess);  // buffers of no rows may be NULL
+  if (logits == nullptr) return bad("a buffer pointer is NULL");
+  if (out == nullptr && choice == nullptr && lse == nullptr)
+    return bad("there is nothing to write: out, choice and lse are NULL");
+  const int in_bytes = logits_fp32 ? 4 : 2, out_bytes = out_fp32 ? 4 : 2;
+  if (fasq::misaligned(logits, in_bytes) || (out != nullptr && fasq::misaligned(out, out_bytes)))
+    return bad("tensors must be aligned to their values");
+  if (!fasq::stride_ok(stride) || !fasq::stride_ok(out_stride)) return bad("strides must lie in [0, 2^40]");
+  if (out != nullptr && fasq::rows_overlap(V, R, out_stride)) return bad("rows of out overlap");
+  if (out == logits && (in_bytes != out_bytes || (R > 1 && stride != out_stride)))
+    return bad("out = logits needs the type and the stride of logits");
+  if (r.token_count != nullptr ? r.tokens == nullptr && r.max_tokens != 0 : r.tokens != nullptr)
+    return bad("tokens and token_count are given together or not at all");
+  if (r.prompt_len != nullptr && r.token_count == nullptr) return bad("prompt_len needs tokens");
+  if (r.token_count != nullptr &&
+      (r.max_tokens < 0 || r.max_tokens > (int64_t(1) << 30) || r.token_stride < 0 || r.token_stride > fasq::kMaxStride))
+    return bad("max_tokens must lie in [0, 2^30] and the tokens' stride must not be negative");
+  if ((r.bias_ids == nullptr) != (r.bias_values == nullptr))
+    return bad("bias_ids and bias_values are given together or not at all");
+  if (r.bias_ids != nullptr && (r.max_bias < 0 || r.max_bias > (int64_t(1) << 24)))
+    return bad("max_bias must lie in [0, 2^24]");
+  if (r.allowed != nullptr && (r.allowed_stride < 0 || r.allowed_stride > fasq::kMaxStride))
+    return bad("strides must lie in [0, 2^40]");
+  if ((r.draft_tokens == nullptr) != (r.tree == nullptr) || (r.q_start == nullptr) != (r.tree == nullptr))
+    return bad("draft_tokens, q_start and tree are given together or not at all");
+  if (r.tree != nullptr && (r.tree_words < 1 || r.tree_words > fasq::kMaxTokens || r.tree_stride < r.tree_words ||
+                            r.tree_stride > fasq::kMaxStride))
+    return bad("tree_words must be >= 1, tree_stride at least that");
+  if ((r.repetition != nullptr || r.presence != nullptr || r.frequency != nullptr) && r.token_count == nullptr &&
+      r.tree == nullptr)
+    return bad("repetition, presence and frequency need tokens or a tree");
+  const void* words[] = {r.requests,   r.tokens,      r.prompt_len, r.token_count, r.repetition,   r.presence, r.frequency,
+                         r.bias_ids,   r.bias_values, r.allowed,    r.temperature, r.draft_tokens, r.q_start,  r.tree,
+                         choice,       lse};
+  for (const void* w : words)
+    if (fasq::misaligned(w, 4)) return bad("int32 and fp32 arrays must be 4-byte aligned");
+  fasq::DeviceInfo dev;
+  const hipError_t e = fasq::device_info(&dev);
+  if (e != hipSuccess)
+    return fasq::fail(FASQ_ERR_HIP, "querying the current device: ", hipGetErrorString(e));
+  const int64_t need = choice != nullptr || lse != nullptr ? fasq::logits_workspace_bytes(R, V, dev) : 0;
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need))
+    return bad("workspace smaller than fasq_process_logits_workspace_bytes()");
+  if (fasq::misaligned(workspace, 16)) return bad("workspace must be 16-byte aligned");
+  fasq::LogitsProblem p = {};
+  p.logits = logits;
+  p.wide = logits_fp32 != 0;
+  p.stride = stride;
+  p.R = R;
+  p.V = V;
+  p.rules = r;
+  if (r.bias_ids == nullptr) p.rules.max_bias = 0;
+  if (r.repetition == nullptr && r.presence == nullptr && r.frequency == nullptr) {  // occurrences change nothing
+    p.rules.token_count = nullptr;
+    p.rules.tree = nullptr;
+  }
+  p.out = out;
+  p.out_wide = out_fp32 != 0;
+  p.out_stride = out_stride;
+  p.choice = choice;
+  p.lse = lse;
+  p.workspace = workspace;
+  return fasq::launch_status(fasq::launch_logits(p, dev, stream));
 }
 
 }  // extern "C"
