@@ -21,13 +21,15 @@ typedef float8_t float8_any __attribute__((aligned(4)));
 typedef int int4_t __attribute__((ext_vector_type(4)));
 typedef int4_t int4_any __attribute__((aligned(4)));
 
-constexpr int kThreads = 256, kEach = 8;  // threads of a workgroup, neighbouring logits of a thread
+constexpr int kEach = 8;  // neighbouring logits of a thread
 constexpr uint32_t kInPrompt = 0x80000000u;
 
-// What a slice of a row found.
+constexpr float kLog2e = 1.44269504088896341f;
+
+// What some of a row's logits come to.
 struct Found {
-  uint64_t best;  // order_of() of the largest logit, then its index's complement
-  float m, sum;   // the largest logit that is a number, the sum of exp(x - m)
+  uint64_t best;  // order_of() of the largest, then its index's complement
+  float m, sum;   // the largest that is a number, the sum of exp(x - m)
 };
 
 struct LogitsArgs {
@@ -37,6 +39,7 @@ struct LogitsArgs {
   int64_t stride, out_stride;  // elements between rows
   int64_t R, first;            // the launch's first workgroup of all
   int V, slices;
+  int rows;  // of a workgroup
   int S;
   const int32_t* requests;
   const int32_t* tokens;
@@ -55,11 +58,20 @@ struct LogitsArgs {
   const int32_t* tree;
   int64_t tree_stride;
   int tree_words;
-  bool counted, finds;  // tokens are counted; choice or lse is asked for
-  Found* found;         // [R][slices], with more than one
+  bool counted;  // tokens are
+  Found* found;  // [R][parts]: of each wave that holds some of a row; nullptr: not asked for
+  int parts;
   int32_t* choice;
   float* lse;
 };
+
+// The kernel's arguments, as if read for the first time: held from the start on they
+// would fill the scalar registers, and what does not fit goes through the vector ones.
+__device__ __forceinline__ const LogitsArgs& fresh_args() {
+  auto p = (__attribute__((address_space(4))) const LogitsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const LogitsArgs*)p;
+}
 
 // Larger for larger logits; NaN above all, the two zeros alike.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -69,32 +81,10 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 constexpr uint32_t kOrderOfNone = ~0xFF800000u;  // of -inf
 
-// exp(x - m) for a finite m or x <= m = +inf.
-__device__ __forceinline__ float weight_of(float x, float m) {
-  return x == m ? 1.f : __builtin_amdgcn_exp2f((x - m) * 1.4426950408889634f);
-}
-
-__device__ __forceinline__ void join(Found& a, const Found& b) {
-  const float m = fmaxf(a.m, b.m);
-  if (m == -INFINITY) {
-    a.sum += b.sum;  // 0, or NaN
-  } else {
-    a.sum = (a.m == -INFINITY ? a.sum : a.sum * weight_of(a.m, m)) + (b.m == -INFINITY ? b.sum : b.sum * weight_of(b.m, m));
-  }
-  a.m = m;
-  a.best = a.best > b.best ? a.best : b.best;
-}
-
-__device__ __forceinline__ void join_wave(Found& f) {
-#pragma unroll
-  for (int x = 1; x < kWave; x *= 2) {
-    Found g;
-    const uint32_t lo = __shfl_xor((uint32_t)f.best, x, kWave), hi = __shfl_xor((uint32_t)(f.best >> 32), x, kWave);
-    g.best = (uint64_t)hi << 32 | lo;
-    g.m = __shfl_xor(f.m, x, kWave);
-    g.sum = __shfl_xor(f.sum, x, kWave);
-    join(f, g);
-  }
+// A value that no kernel writes while this one runs, at an address that a whole wave shares: a scalar load.
+template <typename T>
+__device__ __forceinline__ T fixed(const T* p) {
+  return *(__attribute__((address_space(4))) const T*)(uintptr_t)p;
 }
 
 __device__ __forceinline__ int request_of(const LogitsArgs& a, int64_t row) {
@@ -102,202 +92,487 @@ __device__ __forceinline__ int request_of(const LogitsArgs& a, int64_t row) {
   return s >= 0 && s < a.S ? (int)s : -1;
 }
 
-__device__ __forceinline__ void store_row(const LogitsArgs& a, int64_t row, const Found& f) {
-  if (a.choice != nullptr) a.choice[row] = (uint32_t)(f.best >> 32) == kOrderOfNone ? -1 : (int)~(uint32_t)f.best;
-  if (a.lse != nullptr) {
-    // an infinite logit's sum is infinite; without any logit above -inf it is 0 (or NaN)
-    a.lse[row] = f.m == -INFINITY ? (f.sum == f.sum ? f.m : f.sum) : f.m + __logf(f.sum);
-  }
-}
-
+// Eight of them, or the `count` that there are.
 template <typename V8, typename T>
-__device__ __forceinline__ void store_logits(T* to, int v, int V, const float (&x)[kEach]) {
-  if (v + kEach <= V) {
+__device__ __forceinline__ void store_logits(T* to, uint32_t at, int count, const float (&x)[kEach]) {
+  if (count >= kEach) {
     V8 h;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) h[e] = static_cast<T>(x[e]);
-    *reinterpret_cast<V8*>(to + v) = h;
+    *reinterpret_cast<V8*>(to + at) = h;
   } else {
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
-      if (v + e < V) to[v + e] = static_cast<T>(x[e]);
+      if (e < count) to[at + e] = static_cast<T>(x[e]);
   }
 }
 
-// One slice of 2048 GROUPS logits of a row.
-template <typename T, int GROUPS>
-__global__ __launch_bounds__(kThreads) void k_logits(LogitsArgs a) {
-#pragma clang fp contract(off)
-  constexpr int SLICE = kThreads * kEach * GROUPS;
-  extern __shared__ __align__(16) uint32_t counts[];  // [SLICE], then the biases' [SLICE]
-  int* slots = reinterpret_cast<int*>(counts + SLICE);
-  __shared__ Found part[kThreads / kWave];
-  const int64_t block = a.first + blockIdx.x, row = block / a.slices;
-  const int slice = (int)(block - row * a.slices), v0 = slice * SLICE, tid = threadIdx.x;
-  const int req = request_of(a, row);
-  if (req < 0) return;
+// Over a wave, as a scalar.
+template <typename T, typename F>
+__device__ __forceinline__ T wave_join(T own, F f) {
+  static_assert(sizeof(T) == 4);
+  auto step = [&](uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, f(__builtin_bit_cast(T, a), __builtin_bit_cast(T, b)));
+  };
+  uint32_t v = __builtin_bit_cast(uint32_t, own);
+  // lanes 1, 2, 4 and 8 apart, or as far within eight and sixteen mirrored
+  v = step(v, __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true));
+  v = step(v, __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true));
+  v = step(v, __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true));
+  v = step(v, __builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, true));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = step(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(step(b[0], b[1])));
+}
+// The larger one that is a number.  As an instruction, because the compiler would
+// first make each operand a value that no signalling NaN is.
+__device__ __forceinline__ float larger(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ float larger(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-  // the logits, on their way while the tokens are counted
-  const T* from = static_cast<const T*>(a.logits) + row * a.stride;
-  float x[GROUPS][kEach];
+// What a wave's logits come to, in its first lane.  first: the index of x[0][0] in lane
+// 0; lanes lie side by side, groups `apart`.
+template <int GROUPS>
+__device__ __forceinline__ Found find(const float (&x)[GROUPS][kEach], int first, int apart) {
+  float own[GROUPS], top = -INFINITY;
 #pragma unroll
   for (int g = 0; g < GROUPS; ++g) {
-    const int v = v0 + (g * kThreads + tid) * kEach;
-    if (v + kEach <= a.V) {
-      if constexpr (sizeof(T) == 2) {
-        const half8_t h = *reinterpret_cast<const half8_any*>(from + v);
+    own[g] = larger(x[g][0], x[g][1]);
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) x[g][e] = (float)h[e];
-      } else {
-        const float8_t h = *reinterpret_cast<const float8_any*>(from + v);
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) x[g][e] = h[e];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) x[g][e] = v + e < a.V ? (float)from[v + e] : -INFINITY;
-    }
+    for (int e = 2; e < kEach; e += 2) own[g] = larger(own[g], x[g][e], x[g][e + 1]);
+    top = larger(top, own[g]);
   }
-
-  const bool counted = a.counted, biased = a.max_bias > 0;
-  if (counted)
-    for (int i = tid * 4; i < SLICE; i += kThreads * 4) *reinterpret_cast<int4_t*>(counts + i) = int4_t{0, 0, 0, 0};
-  if (biased)
-    for (int i = tid * 4; i < SLICE; i += kThreads * 4) *reinterpret_cast<int4_t*>(slots + i) = int4_t{-1, -1, -1, -1};
-  __syncthreads();
-  if (counted) {
-    auto count = [&](int token, bool prompt) {
-      const uint32_t u = (uint32_t)token - (uint32_t)v0;
-      if (token < 0 || token >= a.V || u >= (uint32_t)SLICE) return;
-      if (prompt) atomicOr(&counts[u], kInPrompt);
-      else atomicAdd(&counts[u], 1u);
-    };
-    const int32_t* tokens = a.tokens + req * a.token_stride;
-    int n = a.token_count != nullptr ? a.token_count[req] : 0, prompt = a.prompt_len != nullptr ? a.prompt_len[req] : 0;
-    n = n < 0 ? 0 : n > a.max_tokens ? a.max_tokens : n;
-    prompt = prompt < 0 ? 0 : prompt > n ? n : prompt;
-    // a prompt matters to the repetition penalty alone
-    for (int i = (a.repetition != nullptr ? 0 : prompt) + tid * 4; i < n; i += kThreads * 4) {
-      if (i + 4 <= n) {
-        const int4_t t = *reinterpret_cast<const int4_any*>(tokens + i);
+  top = wave_join(top, [](float a, float b) { return larger(a, b); });
+  Found f = {0, top, 0.f};
+  const float c = top * kLog2e;
+  if (fabsf(top) < 1e38f) {
+    // one operation fewer than (x - top) * kLog2e; what the product rounds is made good below
 #pragma unroll
-        for (int e = 0; e < 4; ++e) count(t[e], i + e < prompt);
-      } else {
-        for (int e = i; e < n; ++e) count(tokens[e], e < prompt);
-      }
+    for (int g = 0; g < GROUPS; ++g) {
+      float w[kEach];
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(x[g][e], kLog2e, -c));
+#pragma unroll
+      for (int e = 0; e < kEach; e += 2) w[e] += w[e + 1];
+      f.sum += (w[0] + w[2]) + (w[4] + w[6]);
     }
-    if (a.tree != nullptr) {
-      int first = a.q_start[req], nodes = a.q_start[req + 1];
-      first = first < 0 ? 0 : first > a.R ? (int)a.R : first;
-      nodes = nodes < first ? 0 : (nodes > a.R ? (int)a.R : nodes) - first;
-      const int32_t* words = a.tree + row * a.tree_stride;
-      for (int j = tid; j < nodes && j / 32 < a.tree_words; j += kThreads)
-        if (words[j / 32] >> (j % 32) & 1) count(a.draft_tokens[first + j], false);
-    }
-  }
-  if (biased) {
-    const int32_t* ids = a.bias_ids + (int64_t)req * a.max_bias;
-    for (int i = tid; i < a.max_bias; i += kThreads) {
-      const int token = ids[i];
-      const uint32_t u = (uint32_t)token - (uint32_t)v0;
-      if (token >= 0 && token < a.V && u < (uint32_t)SLICE) atomicMax(&slots[u], i);  // a token's last entry counts
-    }
-  }
-  __syncthreads();
-
-  const float rho = a.repetition != nullptr ? a.repetition[req] : 1.f, one_over = 1.f / rho;
-  const float frequency = a.frequency != nullptr ? a.frequency[req] : 0.f;
-  const float presence = a.presence != nullptr ? a.presence[req] : 0.f;
-  const float tau = a.temperature != nullptr ? a.temperature[req] : 0.f, cool = tau > 0.f ? 1.f / tau : 1.f;
-  const float* values = a.bias_values + (int64_t)req * a.max_bias;
-  Found f = {0, -INFINITY, 0.f};
-#pragma unroll
-  for (int g = 0; g < GROUPS; ++g) {
-    const int at = (g * kThreads + tid) * kEach, v = v0 + at;
-    if (counted) {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const uint32_t c = counts[at + e];
-        if (c == 0) continue;
-        float& y = x[g][e];
-        const float times = (float)(c & ~kInPrompt);
-        y = y > 0.f ? y * one_over : y * rho;
-        y = y - (frequency * times + (times > 0.f ? presence : 0.f));
-      }
-    }
-    if (biased) {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int s = slots[at + e];
-        if (s >= 0) x[g][e] = x[g][e] + values[s];
-      }
-    }
-    const uint32_t bits = a.allowed != nullptr && v < a.V ? a.allowed[row * a.allowed_stride + v / 8] : 0xFFu;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      x[g][e] = x[g][e] * cool;
-      if (!(bits >> e & 1)) x[g][e] = -INFINITY;
-    }
-  }
-  if (a.finds) {
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int v = v0 + (g * kThreads + tid) * kEach + e;
-        const uint64_t key = (uint64_t)order_of(x[g][e]) << 32 | (uint32_t)~v;
-        if (v < a.V && key > f.best) f.best = key;
-        f.m = fmaxf(f.m, x[g][e]);
-      }
+  } else {  // infinite ones, and masks of the type's lowest value
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
       for (int e = 0; e < kEach; ++e)
-        f.sum += f.m == -INFINITY ? (x[g][e] == x[g][e] ? 0.f : x[g][e]) : weight_of(x[g][e], f.m);
+        f.sum += x[g][e] == top ? (top == -INFINITY ? 0.f : 1.f)
+                                : __builtin_amdgcn_exp2f((x[g][e] - top) * kLog2e);
   }
-  if (a.out != nullptr) {
+  f.sum = wave_join(f.sum, sum_of);
+  if (fabsf(top) < 1e38f) f.sum *= __builtin_amdgcn_exp2f(-fmaf(top, kLog2e, -c));
+  const bool nan = f.sum != f.sum;  // then some logit is
+  uint32_t at = 0;
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      const int v = v0 + (g * kThreads + tid) * kEach;
-      if (a.out_wide) store_logits<float8_any>(static_cast<float*>(a.out) + row * a.out_stride, v, a.V, x[g]);
-      else store_logits<half8_any>(static_cast<half_t*>(a.out) + row * a.out_stride, v, a.V, x[g]);
+  for (int g = GROUPS - 1; g >= 0; --g) {
+    // the first lane with one, and the first of its eight
+    int e0 = kEach;
+    if (nan) {
+#pragma unroll
+      for (int e = kEach - 1; e >= 0; --e) e0 = x[g][e] != x[g][e] ? e : e0;
+    } else if (__ballot(own[g] == top) != 0) {
+#pragma unroll
+      for (int e = kEach - 1; e >= 0; --e) e0 = x[g][e] == top ? e : e0;
+    }
+    const uint64_t with = __ballot(e0 < kEach);
+    if (with != 0) {
+      const int l = __ffsll((unsigned long long)with) - 1;
+      at = first + g * apart + l * kEach + __builtin_amdgcn_readlane(e0, l);
     }
   }
-  if (a.finds) {
-    join_wave(f);
-    if (tid % kWave == 0) part[tid / kWave] = f;
-    __syncthreads();
-    if (tid == 0) {
+  f.best = (uint64_t)order_of(nan ? f.sum : top) << 32 | (uint32_t)~at;
+  return f;
+}
+
+// A value as if it was new: what follows from it is not kept over a loop (a row's
+// end is compared with every index, which filled the scalar registers).
+__device__ __forceinline__ int again(int v) {
+  v = __builtin_amdgcn_readfirstlane(v);
+  asm volatile("" : "+s"(v));
+  return v;
+}
+
+// Eight logits as they are loaded.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<half_t> {
+  typedef half8_t Held;
+  typedef half8_any InMemory;
+};
+template <>
+struct Eight<float> {
+  typedef float8_t Held;
+  typedef float8_any InMemory;
+};
+
+// One slice of 8 TH GROUPS logits of a.rows rows, one after the other.  Rows of
+// one request that follow each other share its counts.
+template <typename T, int TH, int GROUPS>
+__global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) {
+#pragma clang fp contract(off)
+  const LogitsArgs& a = fresh_args();
+  constexpr int SLICE = TH * kEach * GROUPS, WAVES = TH / kWave;
+  // counts [SLICE]: occurrences in the answer, kInPrompt.  The biases' entries (-1: none) take
+  // their place for a single row, else the place behind them.
+  extern __shared__ __align__(16) uint32_t counts[];
+  __shared__ int hits;                    // 1: biases fall into the slice, 2: drafted tokens do
+  __shared__ int drafts[WAVES * GROUPS];  // the columns in which they do
+  const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave);
+  int64_t chunk;
+  int slice;
+  {
+    const uint64_t block = a.first + blockIdx.x;
+    if (block >> 32 == 0) {
+      chunk = (uint32_t)block / (uint32_t)a.slices;
+      slice = (int)((uint32_t)block - (uint32_t)chunk * (uint32_t)a.slices);
+    } else {
+      chunk = block / a.slices;
+      slice = (int)(block - chunk * a.slices);
+    }
+  }
+  const int v0 = slice * SLICE, left = a.V - v0;  // of the row, from the slice on
+  const int64_t row0 = chunk * a.rows, row1 = row0 + a.rows < a.R ? row0 + a.rows : a.R;
+  const bool counted = a.counted, biased = a.max_bias > 0, apart = a.rows > 1 && counted;
+  int* const slots = reinterpret_cast<int*>(counts) + (apart ? SLICE : 0);
+  // A token's place in the slice; SLICE and more: not there.
+  auto place = [&](int token) {
+    const uint32_t u = (uint32_t)token - (uint32_t)v0;
+    return (uint32_t)token < (uint32_t)a.V ? u : (uint32_t)SLICE;
+  };
+  // Where it is counted: the k-th logits of a wave's lanes lie side by side.
+  auto column = [](uint32_t u) { return (u & ~511u) | (u & 7) << 6 | (u >> 3 & 63); };
+  auto fill = [&](int* to, int value) {
 #pragma unroll
-      for (int i = 1; i < kThreads / kWave; ++i) join(f, part[i]);
-      if (a.slices == 1) store_row(a, row, f);
-      else a.found[row * a.slices + slice] = f;
+    for (int i = 0; i < 2 * GROUPS; ++i) *reinterpret_cast<int4_t*>(to + (i * TH + tid) * 4) = int4_t{value, value, value, value};
+  };
+  // the logits, on their way while the tokens are counted
+  typename Eight<T>::Held next[GROUPS];
+  int next_bits[GROUPS], next_req;
+  auto load = [&](int64_t row) {
+    next_req = a.requests != nullptr ? fixed(a.requests + row) : (int)row;
+    const T* from = static_cast<const T*>(a.logits) + row * a.stride + v0;
+    const uint8_t* allowed = a.allowed + row * a.allowed_stride + v0 / 8;
+    if (left >= SLICE) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const uint32_t at = (g * TH + tid) * kEach;
+        next[g] = *reinterpret_cast<const typename Eight<T>::InMemory*>(from + at);
+        if (a.allowed != nullptr) next_bits[g] = allowed[at / 8];
+      }
+    } else {
+      const int there = again(left);
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const int at = (g * TH + tid) * kEach;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const T x = from[at + e < there ? at + e : there - 1];
+          next[g][e] = at + e < there ? x : static_cast<T>(-INFINITY);
+        }
+        if (a.allowed != nullptr) next_bits[g] = allowed[(at < there ? at : 0) / 8];
+      }
+    }
+  };
+  load(row0);
+
+  int held = -1;           // the request whose tokens are counted
+  int nodes = 0, node0 = 0;  // its drafted tokens
+  uint32_t own = SLICE;    // this thread's of them
+  bool some_bias = false, some_draft = false;
+  int met[GROUPS] = {};  // the columns of this wave in which some token has occurred
+  float rho = 1.f, one_over = 1.f, frequency = 0.f, presence = 0.f, cool = 1.f;
+  for (int64_t row = row0; row < row1; ++row) {
+    const int req = next_req;
+    if ((uint32_t)req >= (uint32_t)a.S) {
+      if (row + 1 < row1) load(row + 1);
+      continue;
+    }
+
+    const int32_t* ids = a.bias_ids + (int64_t)req * a.max_bias;
+    const int32_t* words = a.tree + row * a.tree_stride;
+    // the tokens of this row's nodes, once more or once less
+    auto drafted = [&](uint32_t change) {
+      for (int j = tid; j < nodes && j / 32 < a.tree_words; j += TH)
+        if (words[j / 32] >> (j % 32) & 1) {
+          const uint32_t u = j == tid ? own : place(a.draft_tokens[node0 + j]);
+          if (u < (uint32_t)SLICE) atomicAdd(&counts[column(u)], change);
+        }
+    };
+    if (req != held) {
+      held = req;
+      if (counted) {
+        if (a.repetition != nullptr) rho = fixed(a.repetition + req);
+        if (a.frequency != nullptr) frequency = fixed(a.frequency + req);
+        if (a.presence != nullptr) presence = fixed(a.presence + req);
+      }
+      float tau = 0.f;
+      if (a.temperature != nullptr) tau = fixed(a.temperature + req);
+      if (counted || biased) {
+        if (row > row0) __syncthreads();  // nobody reads the last request's
+        int n = 0, prompt = 0;
+        if (counted && a.token_count != nullptr) {
+          n = fixed(a.token_count + req);
+          prompt = a.prompt_len != nullptr ? fixed(a.prompt_len + req) : 0;
+          n = n < 0 ? 0 : n > a.max_tokens ? a.max_tokens : n;
+          prompt = prompt < 0 ? 0 : prompt > n ? n : prompt;
+        }
+        const int32_t* tokens = a.tokens + req * a.token_stride;
+        int drafted_one = -1, bias_one = -1;  // of this thread
+        if (a.tree != nullptr) {
+          node0 = fixed(a.q_start + req);
+          nodes = fixed(a.q_start + req + 1);
+          node0 = node0 < 0 ? 0 : node0 > a.R ? (int)a.R : node0;
+          nodes = nodes < node0 ? 0 : (nodes > a.R ? (int)a.R : nodes) - node0;
+          if (tid < nodes) drafted_one = a.draft_tokens[node0 + tid];
+        }
+        if (tid < a.max_bias) bias_one = ids[tid];
+        if (counted) fill(reinterpret_cast<int*>(counts), 0);
+        if (biased && (apart || !counted)) fill(slots, -1);
+        if (tid == 0) hits = 0;
+        if (tid < WAVES * GROUPS) drafts[tid] = 0;
+        __syncthreads();
+        auto scan = [&](int i, int end, auto count) __attribute__((always_inline)) {
+          constexpr int AHEAD = 4;
+          auto one = [&](int token) __attribute__((always_inline)) {
+            const uint32_t u = place(token);
+            if (u < (uint32_t)SLICE) count(&counts[column(u)]);
+          };
+#pragma unroll 1
+          for (; i + AHEAD * TH * 4 <= end; i += AHEAD * TH * 4) {
+            int4_t t[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) t[k] = *reinterpret_cast<const int4_any*>(tokens + i + (k * TH + tid) * 4);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) one(t[k][e]);
+          }
+#pragma unroll 1
+          for (i += tid * 4; i < end; i += TH * 4) {
+            if (i + 4 <= end) {
+              const int4_t t = *reinterpret_cast<const int4_any*>(tokens + i);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) one(t[e]);
+            } else {
+#pragma unroll 1
+              for (int k = i; k < end; ++k) one(tokens[k]);
+            }
+          }
+        };
+        // a prompt matters to the repetition penalty alone
+        if (a.repetition != nullptr) scan(0, prompt, [](uint32_t* c) { atomicOr(c, kInPrompt); });
+        scan(prompt, n, [](uint32_t* c) { atomicAdd(c, 1u); });
+        own = place(drafted_one);
+        int hit = 0;
+        for (int i = tid; i < a.max_bias; i += TH) {
+          const uint32_t u = place(i == tid ? bias_one : ids[i]);
+          if (u >= (uint32_t)SLICE) continue;
+          hit = 1;
+          if (apart || !counted) atomicMax(&slots[u], i);  // a token's last entry counts
+        }
+        for (int j = tid; j < nodes; j += TH) {
+          const uint32_t u = j == tid ? own : place(a.draft_tokens[node0 + j]);
+          if (u >= (uint32_t)SLICE) continue;
+          hit |= 2;
+          atomicOr(&drafts[u >> 9], 1 << (u & 7));
+        }
+        if (hit != 0) atomicOr(&hits, hit);
+        __syncthreads();
+        some_bias = (uniform(hits) & 1) != 0;
+        some_draft = (uniform(hits) & 2) != 0;
+        if (counted) {
+#pragma unroll
+          for (int g = 0; g < GROUPS; ++g) {
+            met[g] = uniform(drafts[g * WAVES + wave]);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) met[g] |= __any(counts[(g * WAVES + wave) * 512 + e * kWave + lane] != 0) ? 1 << e : 0;
+          }
+        }
+      }
+      one_over = 1.f / rho;
+      cool = tau > 0.f ? 1.f / tau : 1.f;
+    }
+
+    int bits[GROUPS];
+    float x[GROUPS][kEach];
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) x[g][e] = (float)next[g][e];
+      bits[g] = next_bits[g];
+    }
+    if (row + 1 < row1) load(row + 1);
+    if (counted) {
+      if (some_draft) {
+        drafted(1u);
+        __syncthreads();
+      }
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        if (met[g] == 0) continue;  // few columns have any
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          if (!(met[g] >> e & 1)) continue;
+          const uint32_t k = counts[(g * WAVES + wave) * 512 + e * kWave + lane];
+          const float y = x[g][e], times = (float)(k & ~kInPrompt);
+          const float z = y * (y > 0.f ? one_over : rho) - (frequency * times + (times > 0.f ? presence : 0.f));
+          x[g][e] = k != 0 ? z : y;
+        }
+      }
+      if (some_draft) {
+        __syncthreads();
+        drafted(0xFFFFFFFFu);
+      }
+    }
+    if (some_bias) {
+      if (counted && !apart) {
+        __syncthreads();
+        fill(slots, -1);
+        __syncthreads();
+        for (int i = tid; i < a.max_bias; i += TH) {
+          const uint32_t u = place(ids[i]);
+          if (u < (uint32_t)SLICE) atomicMax(&slots[u], i);
+        }
+        __syncthreads();
+      }
+      const float* values = a.bias_values + (int64_t)req * a.max_bias;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const int4_t* at = reinterpret_cast<const int4_t*>(slots + (g * TH + tid) * kEach);
+        const int4_t c[2] = {at[0], at[1]};
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+          if (c[e / 4][e % 4] >= 0) x[g][e] = x[g][e] + values[c[e / 4][e % 4]];
+      }
+    }
+    if (a.temperature != nullptr) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) x[g][e] = x[g][e] * cool;
+    }
+    if (a.allowed != nullptr) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          // all ones or none, then x or -inf bit by bit (which the compiler makes four operations of)
+          const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(bits[g], e, 1);
+          asm("v_bfi_b32 %0, %1, %0, %2" : "+v"(x[g][e]) : "v"(keep), "s"(0xFF800000u));
+        }
+      }
+    }
+    if (a.out != nullptr) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const int at = (g * TH + tid) * kEach, count = left >= SLICE ? kEach : again(left) - at;
+        if (a.out_wide) store_logits<float8_any>(static_cast<float*>(a.out) + row * a.out_stride + v0, at, count, x[g]);
+        else store_logits<half8_any>(static_cast<half_t*>(a.out) + row * a.out_stride + v0, at, count, x[g]);
+      }
+    }
+    if (a.found != nullptr) {
+      // what lies past the vocabulary is -inf, and no choice where all is
+      const Found f = find<GROUPS>(x, v0 + wave * kWave * kEach, TH * kEach);
+      if (lane == 0) a.found[(row * a.slices + slice) * WAVES + wave] = f;
     }
   }
 }
 
 // One wave a row.
-__global__ __launch_bounds__(kThreads) void k_logits_join(LogitsArgs a) {
-  const int64_t row = a.first + (int64_t)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void k_logits_join(LogitsArgs a) {
+  const int64_t row = a.first + (int64_t)blockIdx.x * (kJoinThreads / kWave) + threadIdx.x / kWave;
   if (row >= a.R || request_of(a, row) < 0) return;
-  Found f = {0, -INFINITY, 0.f};
-  for (int i = threadIdx.x % kWave; i < a.slices; i += kWave) join(f, a.found[row * a.slices + i]);
-  join_wave(f);
-  if (threadIdx.x % kWave == 0) store_row(a, row, f);
+  const int lane = threadIdx.x % kWave;
+  const Found* parts = a.found + row * a.parts;
+  constexpr int HELD = 4;
+  Found f[HELD];
+  uint32_t order = 0, index = 0xFFFFFFFFu;
+  float m = -INFINITY, sum = 0.f;
+  for (int i0 = 0; i0 < a.parts; i0 += HELD * kWave) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) f[k] = i0 + k * kWave + lane < a.parts ? parts[i0 + k * kWave + lane] : Found{0, -INFINITY, 0.f};
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) top = fmaxf(top, f[k].m);
+    top = wave_join(top, [](float a, float b) { return larger(a, b); });
+    sum *= m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * kLog2e);
+    m = top;
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+      sum += f[k].sum * (f[k].m == m ? 1.f : __builtin_amdgcn_exp2f((f[k].m - m) * kLog2e));
+      const uint32_t o = (uint32_t)(f[k].best >> 32), at = ~(uint32_t)f[k].best;
+      index = o > order ? at : o == order && at < index ? at : index;
+      order = o > order ? o : order;
+    }
+  }
+  sum = wave_join(sum, sum_of);
+  const uint32_t best = wave_join(order, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  index = wave_join(order == best ? index : 0xFFFFFFFFu, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+  if (lane != 0) return;
+  if (a.choice != nullptr) a.choice[row] = best == kOrderOfNone ? -1 : (int)index;
+  if (a.lse != nullptr) a.lse[row] = sum == 0.f ? -INFINITY : m + __log2f(sum) * 0.693147180559945309f;
 }
 
-constexpr int kGroups = 2;
+// How a call's rows are cut.
+struct LogitsPlan {
+  int threads, groups;
+  int slices, rows;
+};
 
-int slices_of(int64_t V) { return (int)((V + kThreads * kEach * kGroups - 1) / (kThreads * kEach * kGroups)); }
+LogitsPlan plan_logits(int64_t R, int64_t V, int64_t rows_of_request, const DeviceInfo& dev) {
+  LogitsPlan p;
+  p.rows = (int)(rows_of_request > 8 ? 8 : rows_of_request);
+  p.threads = 512;
+  p.groups = R * V > (int64_t)dev.num_cus * 4096 ? 2 : 1;
+  p.slices = (int)((V + p.threads * p.groups * kEach - 1) / (p.threads * p.groups * kEach));
+  return p;
+}
+
+template <typename T, int TH, int GROUPS>
+hipError_t launch_slices(LogitsArgs a, hipStream_t stream) {
+  const int64_t blocks = (a.R + a.rows - 1) / a.rows * a.slices, most = kMaxGridThreads / TH;
+  const int arrays = a.counted && a.max_bias > 0 && a.rows > 1 ? 2 : a.counted || a.max_bias > 0 ? 1 : 0;
+  const size_t lds = arrays * TH * GROUPS * kEach * sizeof(uint32_t);
+  for (a.first = 0; a.first < blocks; a.first += most) {
+    const int64_t n = blocks - a.first < most ? blocks - a.first : most;
+    const hipError_t e = launch_kernel(k_logits<T, TH, GROUPS>, dim3((unsigned)n), dim3(TH), lds, stream, a);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename T>
+hipError_t launch_planned(const LogitsPlan& pl, const LogitsArgs& a, hipStream_t stream) {
+  return pl.groups == 1 ? launch_slices<T, 512, 1>(a, stream) : launch_slices<T, 512, 2>(a, stream);
+}
 
 }  // namespace
 
-int64_t logits_workspace_bytes(int64_t R, int64_t V, const DeviceInfo&) {
-  return slices_of(V) > 1 ? R * slices_of(V) * (int64_t)sizeof(Found) : 0;
+int64_t logits_workspace_bytes(int64_t R, int64_t V, const DeviceInfo& dev) {
+  const LogitsPlan p = plan_logits(R, V, 1, dev);
+  return R * p.slices * (p.threads / kWave) * (int64_t)sizeof(Found);
 }
 
-hipError_t launch_logits(const LogitsProblem& p, const DeviceInfo&, hipStream_t stream) {
+hipError_t launch_logits(const LogitsProblem& p, const DeviceInfo& dev, hipStream_t stream) {
   const fasq_token_rules& r = p.rules;
+  const LogitsPlan pl = plan_logits(p.R, p.V, r.S > 0 ? (p.R + r.S - 1) / r.S : 1, dev);
   LogitsArgs a = {};
   a.logits = p.logits;
   a.out = p.out;
@@ -306,7 +581,8 @@ hipError_t launch_logits(const LogitsProblem& p, const DeviceInfo&, hipStream_t 
   a.out_stride = p.out_stride;
   a.R = p.R;
   a.V = (int)p.V;
-  a.slices = slices_of(p.V);
+  a.slices = pl.slices;
+  a.rows = pl.rows;
   a.S = (int)r.S;
   a.requests = r.requests;
   a.tokens = r.tokens;
@@ -331,21 +607,14 @@ hipError_t launch_logits(const LogitsProblem& p, const DeviceInfo&, hipStream_t 
   a.choice = p.choice;
   a.lse = p.lse;
   a.counted = r.token_count != nullptr || r.tree != nullptr;
-  a.finds = p.choice != nullptr || p.lse != nullptr;
-  if (a.finds && a.slices > 1) a.found = static_cast<Found*>(p.workspace);
-  constexpr int SLICE = kThreads * kEach * kGroups;
-  const size_t lds = SLICE * 4 * (a.max_bias > 0 ? 2 : a.counted ? 1 : 0);
-  const int64_t blocks = p.R * a.slices, most = kMaxGridThreads / kThreads;
-  for (a.first = 0; a.first < blocks; a.first += most) {
-    const int64_t n = blocks - a.first < most ? blocks - a.first : most;
-    const hipError_t e = launch_kernel(p.wide ? k_logits<float, kGroups> : k_logits<half_t, kGroups>, dim3((unsigned)n),
-                                       dim3(kThreads), lds, stream, a);
-    if (e != hipSuccess) return e;
-  }
-  if (!a.finds || a.slices == 1) return hipSuccess;
-  constexpr int ROWS = kThreads / kWave;
+  a.parts = pl.slices * (pl.threads / kWave);
+  if (p.choice != nullptr || p.lse != nullptr) a.found = static_cast<Found*>(p.workspace);
+  const hipError_t e = p.wide ? launch_planned<float>(pl, a, stream) : launch_planned<half_t>(pl, a, stream);
+  if (e != hipSuccess) return e;
+  if (a.found == nullptr) return hipSuccess;
+  constexpr int ROWS = kJoinThreads / kWave;
   a.first = 0;
-  return launch_kernel(k_logits_join, dim3((unsigned)((p.R + ROWS - 1) / ROWS)), dim3(kThreads), 0, stream, a);
+  return launch_kernel(k_logits_join, dim3((unsigned)((p.R + ROWS - 1) / ROWS)), dim3(kJoinThreads), 0, stream, a);
 }
 
 }  // namespace fasq

@@ -205,6 +205,18 @@ def test_masked_infinities_and_rows_without_tokens():
     assert np.isneginf(got[2][[2, 4]]).all() and np.isposinf(got[2][3]) and np.isnan(got[2][1])
 
 
+def test_masks_of_the_lowest_value():
+    """fp32 and fp16 logits whose masked tokens hold their type's lowest value, and rows of nothing else."""
+    for wide, low in ((True, np.finfo(np.float32).min), (False, np.finfo(np.float16).min)):
+        b = Rows(3, 1, 5000, wide=wide, seed=13)
+        b.logits[0, 40:] = low
+        b.logits[1] = low
+        b.logits[2, ::3] = low
+        got = b.both(())
+        assert got[1][1] == 0 and got[1][0] == b.logits[0, :40].argmax()
+        assert abs(float(got[2][1]) - float(low)) <= 2.0 ** -22 * abs(float(low)) + 9
+
+
 def test_counts_of_any_length():
     """Lengths of nothing, of all there is, beyond it and below zero; a token thousands of times."""
     b = Rows(5, 1, 3000, L=5000, seed=7)
