@@ -237,7 +237,7 @@ def lib() -> ctypes.CDLL:
                                               _c_int, _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, ctypes.c_float,
                                               _c_int, _c_i64, ctypes.POINTER(AttentionScores), _c_vp, _c_i64, _c_i64,
                                               _c_vp, _c_vp, _c_i64, _c_vp]
-        L.fasq_process_logits.argtypes = [_c_vp, _c_int, _c_i64, _c_i64, _c_i64, ctypes.POINTER(TokenRules), _c_vp, _c_int,
+        L.fasq_process_logits.argtypes = [_c_vp, _c_int, _c_i64, _c_i64, _c_i64, _c_vp, _c_vp, _c_int,
                                           _c_i64, _c_vp, _c_vp, _c_vp, _c_i64, _c_vp]
         L.fasq_process_logits_workspace_bytes.argtypes = [_c_i64, _c_i64]
         L.fasq_paged_attention_workspace_bytes.argtypes = [_c_i64, _c_i64, _c_int, _c_int, _c_int]
@@ -979,71 +979,74 @@ def process_logits(logits, requests=None, *, tokens=None, token_count=None, prom
     _require_rows(logits, "logits", f32 if wide else torch.float16, 2)
     R, V = logits.shape
     device = logits.get_device()
-    S = requests_count if requests_count is not None else R if requests is None else None
-    for t, dims in ((token_count, 1), (prompt_len, 1), (repetition, 1), (presence, 1), (frequency, 1), (temperature, 1),
-                    (tokens, 2), (bias_ids, 2)):
-        if S is None and t is not None:
-            if not isinstance(t, torch.Tensor) or t.dim() != dims:
-                raise ValueError("rules must be tensors [S] or [S x ..]")
-            S = t.shape[0]
-    if S is None:
-        S = (1 << 24) if q_start is None else q_start.shape[0] - 1
-    rules = TokenRules(0, S)
-    if requests is not None:
-        _check_tensor(requests, "requests", i32, (R,), device)
-        rules.requests = requests.data_ptr()
-    for name, t, dtype in (("token_count", token_count, i32), ("prompt_len", prompt_len, i32),
-                           ("repetition", repetition, f32), ("presence", presence, f32), ("frequency", frequency, f32),
-                           ("temperature", temperature, f32)):
-        if t is not None:
-            _check_tensor(t, name, dtype, (S,), device)
-            setattr(rules, name, t.data_ptr())
     if (tokens is None) != (token_count is None) or (bias_ids is None) != (bias_values is None):
         raise ValueError("tokens come with token_count, bias_ids with bias_values")
+    S = requests_count if requests_count is not None else R if requests is None else None
+    if S is None:
+        for t in (token_count, temperature, repetition, presence, frequency, prompt_len, bias_ids):
+            if isinstance(t, torch.Tensor) and t.dim() > 0:
+                S = t.shape[0]
+                break
+        else:
+            S = (1 << 24) if q_start is None else q_start.shape[0] - 1
+    of_request, of_row = (S,), (R,)
+
+    def vector(t, name, dtype, shape):
+        if t is None:
+            return 0
+        # what _check_tensor asks: this is most of what a small call costs
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == device
+                and t.is_contiguous()):
+            _check_tensor(t, name, dtype, shape, device)
+        return t.data_ptr()
+
+    token_at = token_stride = max_tokens = bias_at = max_bias = value_at = allowed_at = allowed_stride = 0
+    tree_at = tree_stride = words = 0
     if tokens is not None:
         _require_rows(tokens, "tokens", i32, 2)
-        _check_rows(tokens, "tokens", i32, (S, tokens.shape[1]), device)
-        rules.tokens, rules.token_stride, rules.max_tokens = tokens.data_ptr(), tokens.stride(0), tokens.shape[1]
+        max_tokens = tokens.shape[1]
+        _check_rows(tokens, "tokens", i32, (S, max_tokens), device)
+        token_at, token_stride = tokens.data_ptr(), tokens.stride(0)
     if bias_ids is not None:
         _require(bias_ids, "bias_ids", i32, 2)
-        _check_tensor(bias_ids, "bias_ids", i32, (S, bias_ids.shape[1]), device)
-        rules.bias_ids, rules.max_bias = bias_ids.data_ptr(), bias_ids.shape[1]
-    if bias_values is not None:
-        _check_tensor(bias_values, "bias_values", f32, bias_ids.shape, device)
-        rules.bias_values = bias_values.data_ptr()
+        max_bias = bias_ids.shape[1]
+        bias_at = vector(bias_ids, "bias_ids", i32, (S, max_bias))
+        value_at = vector(bias_values, "bias_values", f32, (S, max_bias))
     if allowed is not None:
         _check_rows(allowed, "allowed", i32, (R, (V + 31) // 32), device)
-        rules.allowed, rules.allowed_stride = allowed.data_ptr(), allowed.stride(0)
-    if draft_tokens is not None:
-        _check_tensor(draft_tokens, "draft_tokens", i32, (R,), device)
-        rules.draft_tokens = draft_tokens.data_ptr()
-    if q_start is not None:
-        _check_tensor(q_start, "q_start", i32, (S + 1,), device)
-        rules.q_start = q_start.data_ptr()
+        allowed_at, allowed_stride = allowed.data_ptr(), allowed.stride(0)
     if tree is not None:
-        rules.tree, rules.tree_stride, rules.tree_words = _tree(tree, R, device)
-    out_wide = False
-    if not write:
-        if out is not None:
-            raise ValueError("out is given, but write is False")
-    elif out is None:
-        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
-        out_wide = wide
-    else:
-        out_wide = isinstance(out, torch.Tensor) and out.dtype is f32
-        _check_rows(out, "out", f32 if out_wide else torch.float16, (R, V), device)
+        tree_at, tree_stride, words = _tree(tree, R, device)
+    # the fields of fasq_token_rules, eight bytes each
+    rules = array.array("q", (
+        vector(requests, "requests", i32, of_row), S, token_at, token_stride, max_tokens,
+        vector(token_count, "token_count", i32, of_request), vector(prompt_len, "prompt_len", i32, of_request),
+        vector(repetition, "repetition", f32, of_request), vector(presence, "presence", f32, of_request),
+        vector(frequency, "frequency", f32, of_request), bias_at, value_at, max_bias,
+        vector(temperature, "temperature", f32, of_request), allowed_at, allowed_stride,
+        vector(draft_tokens, "draft_tokens", i32, of_row), vector(q_start, "q_start", i32, (S + 1,)), tree_at, tree_stride,
+        words))
+    out_wide, out_at, out_stride = False, 0, 0
+    if write:
+        if out is None:
+            out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+            out_wide = wide
+        else:
+            out_wide = isinstance(out, torch.Tensor) and out.dtype is f32
+            _check_rows(out, "out", f32 if out_wide else torch.float16, logits.shape, device)
+        out_at, out_stride = out.data_ptr(), out.stride(0)
+    elif out is not None:
+        raise ValueError("out is given, but write is False")
     choice = lse = None
     if choose:
-        choice = torch.empty((R,), dtype=i32, device=logits.device)
-        lse = torch.empty((R,), dtype=f32, device=logits.device)
+        choice, lse = logits.new_empty(of_row, dtype=i32), logits.new_empty(of_row, dtype=f32)
     L = lib()
 
     def call(stream):
         need = L.fasq_process_logits_workspace_bytes(R, V) if choose and workspace is None else 0
         ws, ws_bytes = _workspace(workspace, need, device, logits)
-        return L.fasq_process_logits(logits.data_ptr(), wide, logits.stride(0), R, V, rules, _ptr(out), out_wide,
-                                     out.stride(0) if out is not None else 0, _ptr(choice), _ptr(lse), _ptr(ws), ws_bytes,
-                                     stream)
+        return L.fasq_process_logits(logits.data_ptr(), wide, logits.stride(0), R, V, rules.buffer_info()[0], out_at, out_wide,
+                                     out_stride, _ptr(choice), _ptr(lse), _ptr(ws), ws_bytes, stream)
 
     _check(_on_device(device, call))
     return (out, choice, lse) if choose else out

@@ -2,6 +2,7 @@
 without a GPU: refusals before anything touches one, pins of the fp64
 definitions against closed forms, and the trees of the binding."""
 
+import ctypes
 import math
 
 import numpy as np
@@ -47,6 +48,9 @@ def _logits(L, fields=None, **kw):
     a = dict(logits=DUMMY, wide=0, stride=100, R=3, V=100, rules=fasq.TokenRules(**{**dict(S=3), **(fields or {})}), out=DUMMY + 4096, out_wide=0,
              out_stride=100, choice=0, lse=0, ws=0, wb=0)
     a.update(kw)
+    held = a["rules"]
+    if held is not None:
+        a["rules"] = ctypes.addressof(held)
     return L.fasq_process_logits(*a.values(), 0)
 
 
