@@ -68,6 +68,7 @@ struct AttentionArgs {
   bool negate;  // scale < 0: the queries change sign instead
   bool causal;
   bool out_vec;  // 8-byte stores of out
+  bool out_rows;  // 16-byte ones
   bool whole_units;     // pages hold whole units of 16 keys, within 2^31 bytes
   int window;  // 0: none, or all that there can be
   float* lse;
@@ -88,6 +89,7 @@ struct AttentionArgs {
   // With z = scale q.k in powers of two, capped scores are cap * tanh(z / cap)
   // = cap - 2 cap / (1 + 2^(s cap_in)) of the raw product s.
   float cap, cap_in;
+  int classes;  // 1, or 2: see k_attention_tile
 };
 
 // The kernel's arguments (its only parameter), as if read for the first time:
@@ -104,11 +106,14 @@ __device__ __forceinline__ const AttentionArgs& fresh_args() {
 // Where work lies
 // ---------------------------------------------------------------------------
 
-// Quotients without the long way round that a 64-bit division, or one by a
-// value that is no constant, takes (about a microsecond of a short call).
+// Quotients without the long way round that a 64-bit division takes (about a
+// microsecond of a short call): through fp64, for 0 <= a < 2^53, b > 0.  Positions are
+// at most the keys that all tiles of all heads can need, which no call could read
+// if they were more.
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
-  return a / b;
+  const int64_t q = (int64_t)((double)a / (double)b);  // or its neighbour
+  const int64_t rest = a - q * b;
+  return rest < 0 ? q - 1 : rest >= b ? q + 1 : q;
 }
 __device__ __forceinline__ int token_of(const AttentionArgs& a, int row) {
   return a.g_shift >= 0 ? row >> a.g_shift : (int)((uint32_t)row / (uint32_t)a.G);
@@ -163,37 +168,23 @@ __device__ __forceinline__ Span token_span(const AttentionArgs& a, const Request
 struct Spans {
   Span all, any;
 };
-// LANES lanes hold a row each (and every LANES lanes the same rows); `live`: the lane has one.
-template <int LANES>
+// `live`: the lane has a row.  Without any key, `any` ends before it begins.
 __device__ __forceinline__ Spans join_spans(Span s, bool live) {
-  Spans r = {live ? s : Span{0, INT32_MAX}, live && s.begin < s.end ? s : Span{INT32_MAX, 0}};
-#pragma unroll
-  for (int x = 1; x < LANES; x *= 2) {
-    r.all.begin = max(r.all.begin, __shfl_xor(r.all.begin, x, kWave));
-    r.all.end = min(r.all.end, __shfl_xor(r.all.end, x, kWave));
-    r.any.begin = min(r.any.begin, __shfl_xor(r.any.begin, x, kWave));
-    r.any.end = max(r.any.end, __shfl_xor(r.any.end, x, kWave));
-  }
-  if (r.any.begin >= r.any.end) r.any = {0, 0};
-  return {{__builtin_amdgcn_readfirstlane(r.all.begin), __builtin_amdgcn_readfirstlane(r.all.end)},
-          {__builtin_amdgcn_readfirstlane(r.any.begin), __builtin_amdgcn_readfirstlane(r.any.end)}};
+  auto most = [](int a, int b) { return a > b ? a : b; };
+  auto least = [](int a, int b) { return a < b ? a : b; };
+  const Span some = live && s.begin < s.end ? s : Span{INT32_MAX, 0};
+  if (!live) s = {0, INT32_MAX};
+  return {{wave_join(s.begin, most), wave_join(s.end, least)}, {wave_join(some.begin, least), wave_join(some.end, most)}};
 }
 
-// The same of the rows [row, row + count) of a request, count <= 2 * kWave.
+// The same of the rows [row, row + count) of a request, of which lane l holds the
+// one that sees `mine`, if `live` (which counts where a call has spans).
 template <class V>
-__device__ __forceinline__ Spans row_spans(const AttentionArgs& a, const Request& r, int row, int count) {
+__device__ __forceinline__ Spans row_spans(const AttentionArgs& a, const Request& r, int row, int count, Span mine,
+                                           bool live) {
   Spans s;
   if (V::kMore && a.spans != nullptr) {
-    const int lane = threadIdx.x % kWave;
-    const Span first = token_span<V>(a, r, token_of(a, row + (lane < count ? lane : 0)));
-    s = join_spans<kWave>(first, true);
-    if (count > kWave) {
-      const Span second = token_span<V>(a, r, token_of(a, row + (kWave + lane < count ? kWave + lane : 0)));
-      const Spans t = join_spans<kWave>(second, true);
-      s.all = {max(s.all.begin, t.all.begin), min(s.all.end, t.all.end)};
-      if (s.any.begin >= s.any.end) s.any = t.any;
-      else if (t.any.begin < t.any.end) s.any = {min(s.any.begin, t.any.begin), max(s.any.end, t.any.end)};
-    }
+    s = join_spans(mine, live);
   } else {
     const Span s0 = token_span<V>(a, r, token_of(a, row)), s1 = token_span<V>(a, r, token_of(a, row + count - 1));
     s.all = {s0.begin > s1.begin ? s0.begin : s1.begin, s0.end < s1.end ? s0.end : s1.end};
@@ -326,17 +317,18 @@ __device__ __forceinline__ int64_t wave_total(int64_t v) {
 }
 
 template <int ROWS>
-__device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r) {
-  return (r.n * a.G + ROWS - 1) / ROWS;
+__device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r, int classes = 1) {
+  const int tiles = (r.n * a.G + ROWS - 1) / ROWS;
+  return classes == 2 ? (tiles + 1) / 2 : tiles;
 }
 
-// Positions of one cache head.
+// Positions of one cache head; of every classes-th tile.
 template <class V, int ROWS, int STEP>
-__device__ __forceinline__ int64_t head_length(const AttentionArgs& a, const Batch& batch, bool shared) {
+__device__ __forceinline__ int64_t head_length(const AttentionArgs& a, const Batch& batch, bool shared, int classes = 1) {
   int64_t sum = 0;
   for (int64_t b = threadIdx.x % kWave; b < a.B; b += kWave) {
     const Request r = batch.of(a, b);
-    sum += tiles_of<ROWS>(a, r) * tile_length<V, ROWS, STEP>(a, r, shared);
+    sum += tiles_of<ROWS>(a, r, classes) * tile_length<V, ROWS, STEP>(a, r, shared);
   }
   return a.B == 1 ? lane_value(sum, 0) : uniform(wave_total(sum));
 }
@@ -344,9 +336,19 @@ __device__ __forceinline__ int64_t head_length(const AttentionArgs& a, const Bat
 // The tile at a position within a head's stretch, in every lane of the wave.
 // pos < head_length.
 template <class V, int ROWS, int STEP>
-__device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& batch, int64_t pos, bool shared) {
+__device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& batch, int64_t pos, bool shared,
+                                         int classes = 1) {
   Place p = {};
   int64_t base = 0;
+  if (a.B == 1) {
+    p.b = 0;
+    p.r = {uniform(batch.first.q0), uniform(batch.first.n), uniform(batch.first.kv)};  // of lane 0
+    const int64_t one = tile_length<V, ROWS, STEP>(a, p.r, shared);
+    p.tile = (int)(shared ? quotient(pos, one) : pos);
+    p.start = p.tile * one;
+    p.end = p.start + one;
+    return p;
+  }
   for (int64_t b0 = 0; b0 < a.B; b0 += kWave) {
     const int64_t b = b0 + threadIdx.x % kWave;
     Request r = {};
@@ -354,7 +356,7 @@ __device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& bat
     if (b < a.B) {
       r = batch.of(a, b);
       one = tile_length<V, ROWS, STEP>(a, r, shared);
-      own = tiles_of<ROWS>(a, r) * one;
+      own = tiles_of<ROWS>(a, r, classes) * one;
     }
     int64_t upto = own;  // positions up to and with this lane's request
     if (a.B > 1) {
@@ -382,6 +384,35 @@ __device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& bat
   }
   p.b = -1;
   return p;
+}
+
+// The tile behind `p`, of the next request or the next head where that was the
+// last; there is one.  false: not among the next few requests, use locate().
+template <class V, int ROWS, int STEP>
+__device__ __forceinline__ bool advance(const AttentionArgs& a, const Batch& batch, Place& p, int& head,
+                                        int classes = 1) {
+  const int64_t one = p.end - p.start;
+  if (++p.tile < tiles_of<ROWS>(a, p.r, classes)) {
+    p.start = p.end;
+    p.end += one;
+    return true;
+  }
+  p.tile = 0;
+  p.start = p.end;
+  for (int tries = 0; tries < 4; ++tries) {
+    if (++p.b == a.B) {
+      p.b = 0;
+      p.start = 0;
+      ++head;
+    }
+    if (p.b < kWave) p.r = {lane_value(batch.first.q0, p.b), lane_value(batch.first.n, p.b), lane_value(batch.first.kv, p.b)};
+    else p.r = read_request(a, p.b);
+    if (p.r.n > 0) {
+      p.end = p.start + tile_length<V, ROWS, STEP>(a, p.r, true);
+      return true;
+    }
+  }
+  return false;
 }
 
 // Element offset of key j's row in a cache head (page table row `pages`).
@@ -621,19 +652,22 @@ struct WaveTile {
     if constexpr (V::kMore) {
       if (has_tree && key0 + 32 > tree.first) bits = tree.block(key0) >> h4;
     }
-    float top = -INFINITY;
+    bits &= last >= 32 ? ~0u : last <= 0 ? 0u : ~(~0u << last);
+    bits &= first <= 0 ? ~0u : first >= 32 ? 0u : ~0u << first;
+    const float unseen = V::kCap ? kUnseen : -INFINITY;
+    float top = unseen;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int key = (e / 4) * 8 + e % 4;
-      bool out = key < first || key >= last;
-      if constexpr (V::kMore) out = out || !(bits >> key & 1);
-      if constexpr (V::kCap) {
-        top = fmaxf(top, out ? -INFINITY : fmaxf(s[e], kLeast));
-        s[e] = out ? kUnseen : s[e];
-      } else {
-        s[e] = out ? -INFINITY : s[e];
-        top = fmaxf(top, s[e]);
-      }
+      // all ones or none, then the score or `unseen` bit by bit: half the operations of comparisons
+      const uint32_t seen = (uint32_t)__builtin_amdgcn_sbfe((int)bits, (e / 4) * 8 + e % 4, 1);
+      float v = s[e];
+      asm("v_bfi_b32 %0, %1, %0, %2" : "+v"(v) : "v"(seen), "s"(unseen));
+      s[e] = v;
+      top = fmaxf(top, v);
+    }
+    if constexpr (V::kCap) {
+      constexpr uint32_t mine = 0x0F0F0F0Fu;  // the keys of this lane
+      top = (bits & mine) != 0 ? fmaxf(top, kLeast) : -INFINITY;
     }
     return top;
   }
@@ -661,18 +695,21 @@ struct WaveTile {
     rest *= keep;
   }
 
-  // Row `row` of the request, which exists (lane l and l ^ 32 hold one row;
-  // zeros unless `live`, and past D).
-  __device__ __forceinline__ void load_q(const AttentionArgs& a, const Request& r, int head, int row, bool live) {
+  // Row `row` of the request, which exists (lane l and l ^ 32 hold one row): the loads
+  // (wherever rows start), and later what waits for them.
+  __device__ __forceinline__ void fetch_q(const AttentionArgs& a, const Request& r, int head, int row) {
     const int h = (threadIdx.x % kWave) / 32;
     const int t = token_of(a, row);
     const uint16_t* src = a.q.p + (r.q0 + t) * a.q.ts + (head * a.G + row - t * a.G) * a.q.hs;
-    // all loads first (wherever rows start), then what they have to wait for
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {
       const int d = s * 16 + h * 8;
       q[s] = *reinterpret_cast<const half8_any*>(src + (d < a.D ? d : 0));
     }
+  }
+  // Zeros unless `live`, and past D.
+  __device__ __forceinline__ void finish_q(const AttentionArgs& a, bool live) {
+    const int h = (threadIdx.x % kWave) / 32;
     const uint32_t flip = a.negate ? 0x80008000u : 0u;
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {

@@ -35,6 +35,7 @@ AttentionPlan plan_attention(int64_t T, int64_t B, int Hq, int Hkv, int D, const
   const int64_t whole = rows / p.rows * Hkv;
   const bool once = B == 1 && p.tiles * Hkv <= p.parts && 16 * whole >= 15 * p.parts;
   p.split = p.few || !(once || whole >= 2 * p.parts);
+  p.classes = !p.few && p.split && p.parts % 16 == 0 && rows > p.rows * B && rows <= 4 * p.rows * B ? 2 : 1;
   const int64_t of_share = int64_t(2) * p.rows * (p.DP + 2) * (int64_t)sizeof(float) + (int64_t)sizeof(CutTile);
   p.bytes = p.split ? p.parts * of_share : 0;
   return p;
@@ -84,6 +85,7 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
     return reinterpret_cast<uintptr_t>(v.p) % bytes == 0 && v.ts % (bytes / 2) == 0 && v.hs % (bytes / 2) == 0;
   };
   a.out_vec = aligned(p.out, 8);
+  a.out_rows = aligned(p.out, 16);
   a.whole_units = p.cache.page_size % 16 == 0 && p.cache.slot_stride < int64_t(1) << 25;
   a.lse = p.lse;
   if (pl.split && p.workspace != nullptr && p.workspace_bytes >= pl.bytes) {
@@ -102,6 +104,7 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
   a.slopes = more.slopes;
   a.slope_unit = (float)(1.4426950408889634074 / a.c);
   a.cap = (float)(more.softcap * 1.4426950408889634074);
+  a.classes = pl.classes;
   a.cap_in = cap ? (float)(2.0 * a.c / more.softcap) : 0.f;
   if (cap) return slopes ? launch_variant<Variant<true, true, true>>(pl, a, stream) : launch_variant<Variant<true, true, false>>(pl, a, stream);
   return slopes ? launch_variant<Variant<true, false, true>>(pl, a, stream) : launch_variant<Variant<true, false, false>>(pl, a, stream);

@@ -20,6 +20,7 @@ struct AttentionPlan {
   int64_t tiles;  // at most, of one cache head
   int parts;      // shares of a split call
   bool split;     // worth splitting
+  int classes;    // of tiles in a split call with masks or scores of its own
   int64_t bytes;  // of the workspace
 };
 
@@ -71,9 +72,9 @@ __device__ __forceinline__ int64_t slot_of(int64_t w, int64_t share, int64_t til
 
 // Leaves the tile that starts in share w and goes on past it for the join (or
 // that there is none).  One thread.
-__device__ __forceinline__ void leave_cut(const AttentionArgs& a, int64_t w, int64_t share, const Place& p, int head,
-                                          int64_t t0, int64_t t1, bool cut) {
-  a.cuts[w] = CutTile{t0, t1, share, p.r, p.tile, head, cut ? 1 : 0};
+__device__ __forceinline__ void leave_cut(const AttentionArgs& a, int64_t w, int64_t share, const Place& p, int tile,
+                                          int head, int64_t t0, int64_t t1, bool cut) {
+  a.cuts[w] = CutTile{t0, t1, share, p.r, tile, head, cut ? 1 : 0};
 }
 
 template <int STEP>
@@ -115,31 +116,39 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
   const Batch batch(given);
   const int64_t head_len = head_length<V, ROWS, STEP>(given, batch, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
+  int head;
   if (shared) {
     share = share_of<STEP>(head_len * given.Hkv, given.parts, kFewShare);
     pos = w * share;
     pos_end = pos + share < head_len * given.Hkv ? pos + share : head_len * given.Hkv;
+    head = pos < pos_end ? (int)quotient(pos, head_len) : 0;
   } else {
     w += given.first;
     const int64_t tile = quotient(w, given.Hkv);
-    pos = (w - tile * given.Hkv) * head_len + tile;
+    head = (int)(w - tile * given.Hkv);
+    pos = head * head_len + tile;
     pos_end = tile < head_len ? pos + 1 : pos;
   }
-  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(given, w, share, Place{}, 0, 0, 0, false);
+  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(given, w, share, Place{}, 0, 0, 0, 0, false);
+  Place p = {};
+  bool placed = false;
   while (pos < pos_end) {
     const AttentionArgs a = fresh_args();
-    const int head = (int)quotient(pos, head_len);
-    const Place p = locate<V, ROWS, STEP>(a, batch, pos - head * head_len, shared);
-    if (p.b < 0) {
-      if (shared && threadIdx.x == 0) leave_cut(a, w, share, p, 0, 0, 0, false);
-      return;
+    if (!placed) {
+      p = locate<V, ROWS, STEP>(a, batch, pos - head * head_len, shared);
+      if (p.b < 0) {
+        if (shared && threadIdx.x == 0) leave_cut(a, w, share, p, 0, 0, 0, 0, false);
+        return;
+      }
     }
     const int64_t t0 = head * head_len + p.start, t1 = head * head_len + p.end;
     const int64_t seg_end = t1 < pos_end ? t1 : pos_end;
     const int rows = p.r.n * a.G, row0 = p.tile * ROWS, live = rows - row0 < ROWS ? rows - row0 : ROWS;
+    const bool alive = l32 < live;
+    Span mine = token_span<V>(a, p.r, token_of(a, row0 + (alive ? l32 : live - 1)));
     // keys that some live row sees, and every one
-    const Spans spans = row_spans<V>(a, p.r, row0, live);
-    const Span span = spans.any;
+    const Spans spans = row_spans<V>(a, p.r, row0, live, mine, alive);
+    const Span span = spans.any.begin < spans.any.end ? spans.any : Span{0, 0};
     const int base = span.begin / 32 * 32;
     int lo = base, hi = span.end;
     if (shared) {
@@ -147,8 +156,6 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
       lo = from < hi ? (int)from : hi;
       hi = most < hi ? (int)most : hi;
     }
-    const bool alive = l32 < live;
-    Span mine = token_span<V>(a, p.r, token_of(a, row0 + (alive ? l32 : live - 1)));
     const int all_begin = spans.all.begin;
     int all_end = spans.all.end;
     const bool mixed = spans.all.begin != span.begin || spans.all.end != span.end;  // rows see different keys
@@ -174,11 +181,12 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
       copy.run(a, a.cv, head_off, page1, k + 16, span.begin, hi - 1, to + 48 * DP * 2);
     };
     int page = page_at(k0), stage = 0;
-    t.load_q(a, p.r, head, row0 + (alive ? l32 : live - 1), alive);
-    t.load_row(a, p.r, head, row0 + (alive ? l32 : live - 1));
-    t.clear();
+    t.fetch_q(a, p.r, head, row0 + (alive ? l32 : live - 1));
     if (k0 < hi) issue(k0, page, 0);
     page = page_at(k0 + STEP);
+    t.finish_q(a, alive);
+    t.load_row(a, p.r, head, row0 + (alive ? l32 : live - 1));
+    t.clear();
     for (; k0 < hi; k0 += STEP, stage ^= 1) {
       const int next = k0 + STEP;
       if (next < hi) {
@@ -217,7 +225,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
     const bool cut = shared && (t0 < pos || seg_end < t1);
     const int64_t slot = cut ? slot_of(w, share, t0) : 0;
     if (shared && seg_end == pos_end && threadIdx.x == 0)
-      leave_cut(a, w, share, p, head, t0, t1, t0 >= w * share && t1 > seg_end);
+      leave_cut(a, w, share, p, p.tile, head, t0, t1, t0 >= w * share && t1 > seg_end);
     for (int u = threadIdx.x; u < live * (DP / 4); u += NW * kWave) {
       const int row = u / (DP / 4), d = u % (DP / 4) * 4;
       float top = jm[row];
@@ -264,6 +272,10 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
     }
     __syncthreads();
     pos = seg_end;
+    if (pos < pos_end) {
+      placed = advance<V, ROWS, STEP>(a, batch, p, head);
+      if (!placed) head = (int)quotient(pos, head_len);
+    }
   }
 }
 
@@ -289,8 +301,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
   const RowCopy<DP, FULL> copy(given);
   const bool shared = given.part_o != nullptr;
   const Batch batch(given);
-  const int64_t head_len = head_length<V, ROWS, STEP>(given, batch, shared);
-  int64_t pos, pos_end, share = 0, w = blockIdx.x;
+  // With two classes every request's even tiles lie in the first half of the line,
+  // its odd ones at the same places of the second: workgroups of one compute unit
+  // then read the same keys at the same time, once from memory (see plan_attention).
+  const int classes = V::kMore && shared ? given.classes : 1;
+  const int64_t head_len = head_length<V, ROWS, STEP>(given, batch, shared, classes);
+  int64_t pos, pos_end, share = 0, base = 0, w = blockIdx.x;
+  int head, cls = 0;
   if (shared) {
     // Workgroups go to the XCDs in turn, and each XCD has its own L2: its
     // shares lie side by side, so that they read the keys of few heads (2048
@@ -301,8 +318,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     if (given.parts % kXcds == 0) {
       const int per = given.parts / kXcds;
       int v = (int)w / kXcds;
-      if (DP <= 128 && v >= per / 2) v = per / 2 + (per - 1 - v);
-      w = w % kXcds * per + v;
+      if (classes == 2) {
+        w = v < per / 2 ? w % kXcds * (per / 2) + v : given.parts / 2 + w % kXcds * (per / 2) + v - per / 2;
+      } else {
+        if (DP <= 128 && v >= per / 2) v = per / 2 + (per - 1 - v);
+        w = w % kXcds * per + v;
+      }
     }
     // Short tiles are left whole where all have one length (300 tokens: 28 us, 38
     // with each cut; 1207 tokens in a window of 107 27.5 and 42.6; but 224 rows
@@ -315,51 +336,84 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       length = tile_length<V, ROWS, STEP>(given, Request{0, 0, INT32_MAX}, true);
     }
     const bool whole = length > 0 && length * DP <= 384 * 128;
-    share = share_of<STEP>(head_len * given.Hkv, given.parts, whole ? (int)length : kTileShare);
+    const int parts = classes == 2 ? given.parts / 2 : given.parts;  // of a class
+    share = share_of<STEP>(head_len * given.Hkv, parts, whole ? (int)length : kTileShare);
     if (whole) share = quotient(share - 1, length) * length + length;
+    if (classes == 2 && w >= parts) cls = 1;
+    base = cls * parts * share;
     pos = w * share;
-    pos_end = pos + share < head_len * given.Hkv ? pos + share : head_len * given.Hkv;
+    pos_end = base + head_len * given.Hkv;
+    if (pos + share < pos_end) pos_end = pos + share;
+    head = pos < pos_end ? (int)quotient(pos - base, head_len) : 0;
   } else {
     w += given.first;
     const int64_t tile = quotient(w, given.Hkv);
-    pos = (w - tile * given.Hkv) * head_len + tile;
+    head = (int)(w - tile * given.Hkv);
+    pos = head * head_len + tile;
     pos_end = tile < head_len ? pos + 1 : pos;
   }
-  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(given, w, share, Place{}, 0, 0, 0, false);
+  if (shared && pos >= pos_end && threadIdx.x == 0) leave_cut(given, w, share, Place{}, 0, 0, 0, 0, false);
   if constexpr (!FULL) {
     clear_lds<DP>(ring + wave * (64 * DP), 64);
     __syncthreads();
   }
+  Place p = {};
+  bool placed = false;
   while (pos < pos_end) {
     const AttentionArgs a = fresh_args();
-    const int head = (int)quotient(pos, head_len);
-    Place p = locate<V, ROWS, STEP>(a, batch, pos - head * head_len, shared);
-    if (p.b < 0) {
-      if (shared && threadIdx.x == 0) leave_cut(a, w, share, p, 0, 0, 0, false);
-      return;
+    if (!placed) {
+      p = locate<V, ROWS, STEP>(a, batch, pos - base - head * head_len, shared, classes);
+      if (p.b < 0) {
+        if (shared && threadIdx.x == 0) leave_cut(a, w, share, p, 0, 0, 0, 0, false);
+        return;
+      }
     }
     // the tiles with the most keys first
-    if (!shared) p.tile = tiles_of<ROWS>(a, p.r) - 1 - p.tile;
-    const int64_t t0 = head * head_len + p.start, t1 = head * head_len + p.end;
+    const int tile = !shared ? tiles_of<ROWS>(a, p.r) - 1 - p.tile : p.tile * classes + cls;
+    const int64_t t0 = base + head * head_len + p.start, t1 = base + head * head_len + p.end;
     const int64_t seg_end = t1 < pos_end ? t1 : pos_end;
-    const int rows = p.r.n * a.G, tile_rows = rows - p.tile * ROWS < ROWS ? rows - p.tile * ROWS : ROWS;
-    // over the four waves: the keys that some row sees, and that all see
-    const Spans of_tile = row_spans<V>(a, p.r, p.tile * ROWS, tile_rows);
-    const Span span = of_tile.any;
-    const int base = span.begin / 32 * 32;
-    int lo = base, hi = span.end;
-    if (shared) {
-      const int64_t from = base + (pos - t0), most = base + (seg_end - t0);  // may lie behind the last key
-      lo = from < hi ? (int)from : hi;
-      hi = most < hi ? (int)most : hi;
+    if (V::kMore && classes == 2 && tile >= tiles_of<ROWS>(a, p.r)) {  // a request of an odd number
+      if (seg_end == pos_end && threadIdx.x == 0) leave_cut(a, w, share, p, tile, head, t0, t1, false);
+      pos = seg_end;
+      if (pos < pos_end) {
+        placed = advance<V, ROWS, STEP>(a, batch, p, head, classes);
+        if (!placed) head = (int)quotient(pos - base, head_len);
+      }
+      continue;
     }
-    const int row0 = p.tile * ROWS + wave * 32;
+    const int rows = p.r.n * a.G, tile_rows = rows - tile * ROWS < ROWS ? rows - tile * ROWS : ROWS;
+    const int row0 = tile * ROWS + wave * 32;
     const int live = rows - row0 < 32 ? rows - row0 : 32;  // may be <= 0
     const bool alive = l32 < live;
     Span mine = {0, 0}, all = {0, 0};
-    if (live > 0) {
-      if (alive) mine = token_span<V>(a, p.r, token_of(a, row0 + l32));
-      all = row_spans<V>(a, p.r, row0, live).all;
+    if (alive) mine = token_span<V>(a, p.r, token_of(a, row0 + l32));
+    // over the four waves: the keys that some row sees, and that all see
+    Spans of_tile;
+    if (V::kMore && a.spans != nullptr) {
+      Spans* const of_waves = reinterpret_cast<Spans*>(flag + 4);
+      of_tile = row_spans<V>(a, p.r, row0, live, mine, alive);
+      all = of_tile.all;
+      if (lane == 0) of_waves[wave] = of_tile;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const Spans s = of_waves[i];
+        of_tile.all = {max(of_tile.all.begin, s.all.begin), min(of_tile.all.end, s.all.end)};
+        of_tile.any = {min(of_tile.any.begin, s.any.begin), max(of_tile.any.end, s.any.end)};
+      }
+      of_tile = {{uniform(of_tile.all.begin), uniform(of_tile.all.end)}, {uniform(of_tile.any.begin), uniform(of_tile.any.end)}};
+      if (of_tile.any.begin >= of_tile.any.end) of_tile.any = {0, 0};
+    } else {
+      of_tile = row_spans<V>(a, p.r, tile * ROWS, tile_rows, mine, alive);
+      if (live > 0) all = row_spans<V>(a, p.r, row0, live, mine, alive).all;
+    }
+    const Span span = of_tile.any;
+    const int key0 = span.begin / 32 * 32;
+    int lo = key0, hi = span.end;
+    if (shared) {
+      const int64_t from = key0 + (pos - t0), most = key0 + (seg_end - t0);  // may lie behind the last key
+      lo = from < hi ? (int)from : hi;
+      hi = most < hi ? (int)most : hi;
     }
     const bool mixed = of_tile.all.begin != span.begin || of_tile.all.end != span.end;  // rows see different keys
     const int most_begin = of_tile.all.begin, least_end = of_tile.all.end;
@@ -393,11 +447,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     };
     auto masked = [&](int k) { return k < all.begin || k + 32 > all.end; };
     int page[3] = {page_at(lo), page_at(lo + STEP), 0};
-    t.load_q(a, p.r, head, alive ? row0 + l32 : p.tile * ROWS, alive);
-    t.load_row(a, p.r, head, alive ? row0 + l32 : p.tile * ROWS);
+    int ahead[2] = {page_at(lo + 2 * STEP), page_at(lo + 3 * STEP)};  // with them: one wait less
+    t.fetch_q(a, p.r, head, alive ? row0 + l32 : tile * ROWS);
+    t.load_row(a, p.r, head, alive ? row0 + l32 : tile * ROWS);
     t.clear();
     if (lo < hi) {
-      asm volatile("" : "+v"(page[0]), "+v"(page[1]));  // one wait for both, and not for copies
+      asm volatile("" : "+v"(page[0]), "+v"(page[1]), "+v"(ahead[0]), "+v"(ahead[1]));  // one wait, and not for copies
       copy_keys(lo, page[0], 0);
       copy_keys(lo + STEP, page[1], 1);  // behind the end: any key, masked
       copy_values(lo, page[0], 0);
@@ -405,9 +460,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       // 1, keys of tile 2; pages of this one and the next two
       int page_v = page[1];
       int64_t off_v = copy.whole_offset(a, head_off, page_v, lo + STEP + wave * 16);
-      page[0] = page_at(lo + 2 * STEP);
-      page[1] = page_at(lo + 3 * STEP);
+      page[0] = ahead[0];
+      page[1] = ahead[1];
       int64_t off_k = copy.whole_offset(a, head_off, page[0], lo + 2 * STEP + wave * 16);
+      t.finish_q(a, alive);
       wait_loads<0>();
       barrier_only();
       float16_t s0, s1;
@@ -489,16 +545,28 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     const bool cut = shared && (t0 < pos || seg_end < t1);
     const int64_t slot = cut ? slot_of(w, share, t0) : 0;
     if (shared && seg_end == pos_end && threadIdx.x == 0)
-      leave_cut(end, w, share, p, head, t0, t1, t0 >= w * share && t1 > seg_end);
+      leave_cut(end, w, share, p, tile, head, t0, t1, t0 >= w * share && t1 > seg_end);
+    uint64_t broken = __ballot(alive && t.broken());
+    broken = (broken | broken >> 32) & 0xFFFFFFFFu;
+    __syncthreads();  // the stages are free
+    // Whole rows go through the wave's own part of the stages, where neighbouring
+    // lanes find neighbouring values (a lane holds four of every eight of its row):
+    // 400 documents of 10 tokens 45 -> XX us.
+    const bool aside = FULL && (cut || end.out_rows);
+    uint8_t* const own = smem + wave * (32 * DP * 4);
+    int row_of = l32, half = h;
+    asm volatile("" : "+v"(row_of), "+v"(half));  // no address of this is kept over the keys
     if (alive) {
       if (cut) {
         const int64_t at = slot * ROWS + wave * 32 + l32;
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<float4_t*>(end.part_o + at * DP + i * 32 + e * 8 + h * 4) =
-                float4_t{t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
+          for (int e = 0; e < 4; ++e) {
+            const float4_t v = {t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
+            if (FULL) *reinterpret_cast<float4_t*>(own + row_of * (DP * 4) + ((i * 8 + e * 2 + half) ^ (row_of & 7)) * 16) = v;
+            else *reinterpret_cast<float4_t*>(end.part_o + at * DP + i * 32 + e * 8 + h * 4) = v;
+          }
         if (h == 0) {
           end.part_ml[at * 2] = t.top();
           end.part_ml[at * 2 + 1] = l;
@@ -512,16 +580,41 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float v[4] = {t.o[i][4 * e] * f, t.o[i][4 * e + 1] * f, t.o[i][4 * e + 2] * f, t.o[i][4 * e + 3] * f};
-            store4(end, dst, i * 32 + e * 8 + h * 4, v);
+            if (aside) {
+              half4_t r;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) r[k] = static_cast<half_t>(v[k]);
+              *reinterpret_cast<half4_t*>(own + row_of * (DP * 2) + ((i * 4 + e) ^ (row_of & 7)) * 16 + half * 8) = r;
+            } else {
+              store4(end, dst, i * 32 + e * 8 + h * 4, v);
+            }
           }
         if (h == 0 && end.lse != nullptr)
           end.lse[lse_at(end, p.r, head, row0 + l32)] =
               final_lse<V>(t.top(), l, sees, end, p.r, head, row0 + l32);
       }
     }
-    uint64_t broken = __ballot(alive && t.broken());
-    broken = (broken | broken >> 32) & 0xFFFFFFFFu;
-    __syncthreads();
+    if (aside) {
+      wait_lds();
+      const int first = half * 32 + row_of;
+      if (cut) {
+        constexpr int CHUNKS = DP / 4;  // of 16 bytes a row
+        float* to = end.part_o + (slot * ROWS + wave * 32) * DP;
+#pragma unroll 4
+        for (int u = first; u < live * CHUNKS; u += kWave) {
+          const int row = u / CHUNKS, c = u % CHUNKS;
+          *reinterpret_cast<u32x4*>(to + u * 4) = *reinterpret_cast<const u32x4*>(own + row * (CHUNKS * 16) + (c ^ (row & 7)) * 16);
+        }
+      } else {
+        constexpr int CHUNKS = DP / 8;
+#pragma unroll 2
+        for (int u = first; u < live * CHUNKS; u += kWave) {
+          const int row = u / CHUNKS, c = u % CHUNKS;
+          *reinterpret_cast<u32x4*>(out_row(end, p.r, head, row0 + row) + c * 8) =
+              *reinterpret_cast<const u32x4*>(own + row * (CHUNKS * 16) + (c ^ (row & 7)) * 16);
+        }
+      }
+    }
     uint64_t again = *flag != 0 && live > 0 ? (uint64_t(1) << live) - 1 : broken;
     if (again != 0) {
       wait_loads<0>();  // the stores above come first
@@ -536,7 +629,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       }
     }
     pos = seg_end;
-    if (pos < pos_end) __syncthreads();  // the stages are free
+    if (pos < pos_end) {
+      __syncthreads();  // the stages are free
+      placed = advance<V, ROWS, STEP>(end, batch, p, head, classes);
+      if (!placed) head = (int)quotient(pos - base, head_len);
+    }
   }
 }
 
@@ -644,7 +741,7 @@ hipError_t launch_planned(const AttentionPlan& pl, const AttentionArgs& a, hipSt
     return launch_kernel(k_attention_join<V, DP, 32, JY>, dim3((unsigned)blocks - 1, JY), dim3(256), 0, stream, a);
   }
   if ((e = prepare_kernel(k_attention_tile<V, DP, FULL>)) != hipSuccess) return e;
-  e = launch_blocks(k_attention_tile<V, DP, FULL>, blocks, 256, 512 * DP + 16, stream, a);
+  e = launch_blocks(k_attention_tile<V, DP, FULL>, blocks, 256, 512 * DP + (V::kMore ? 16 + 4 * (int)sizeof(Spans) : 16), stream, a);
   if (e != hipSuccess || !shared) return e;
   return launch_kernel(k_attention_join<V, DP, 128, 16>, dim3((unsigned)blocks - 1, 16), dim3(256), 0, stream, a);
 }

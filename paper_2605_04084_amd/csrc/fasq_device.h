@@ -73,6 +73,24 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
+// Over a wave, as a scalar.
+template <typename T, typename F>
+__device__ __forceinline__ T wave_join(T own, F f) {
+  static_assert(sizeof(T) == 4);
+  auto step = [&](uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, f(__builtin_bit_cast(T, a), __builtin_bit_cast(T, b)));
+  };
+  uint32_t v = __builtin_bit_cast(uint32_t, own);
+  // lanes 1, 2, 4 and 8 apart, or as far within eight and sixteen mirrored
+  v = step(v, __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true));
+  v = step(v, __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true));
+  v = step(v, __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true));
+  v = step(v, __builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, true));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = step(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(step(b[0], b[1])));
+}
 // Full 64-lane sum, result valid in every lane.
 __device__ __forceinline__ float wave_sum(float v) {
   v = group_sum<16>(v);

@@ -265,3 +265,12 @@ def test_tensors_are_checked():
                dict(tree=torch.zeros((2, 1), **i32), window=3), dict(slopes=torch.zeros(4, **f32), scale=0.0)):
         with pytest.raises(fasq.FasqError):
             b.run(**kw)
+
+
+@pytest.mark.parametrize("reqs", [[(64, 5000), (64, 3333)], [(40, 7000), (70, 2000), (33, 6001), (0, 50)], [(100, 9000)], [(50, 64), (200, 4100), (3, 20)]])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (4, 1, 64), (3, 1, 80)])
+def test_trees_of_several_tiles_over_long_caches(reqs, Hq, Hkv, D):
+    """One to seven tiles a request, their keys split over workgroups, even and odd numbers of them."""
+    b = Scored(reqs, Hq, Hkv, D, 64, seed=9)
+    b.both(tree=trees_of(np.random.default_rng(9), reqs))
+    b.both(softcap=20.0)
