@@ -107,10 +107,11 @@ __device__ __forceinline__ const AttentionArgs& fresh_args() {
 // ---------------------------------------------------------------------------
 
 // Quotients without the long way round that a 64-bit division takes (about a
-// microsecond of a short call): through fp64, for 0 <= a < 2^53, b > 0.  Positions are
-// at most the keys that all tiles of all heads can need, which no call could read
-// if they were more.
+// microsecond of a short call): in 32 bits, or through fp64, for 0 <= a < 2^53,
+// b > 0.  Positions are at most the keys that all tiles of all heads can need, which
+// no call could read if they were more.
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
   const int64_t q = (int64_t)((double)a / (double)b);  // or its neighbour
   const int64_t rest = a - q * b;
   return rest < 0 ? q - 1 : rest >= b ? q + 1 : q;

@@ -226,6 +226,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
     const int64_t slot = cut ? slot_of(w, share, t0) : 0;
     if (shared && seg_end == pos_end && threadIdx.x == 0)
       leave_cut(a, w, share, p, p.tile, head, t0, t1, t0 >= w * share && t1 > seg_end);
+#pragma unroll 2
     for (int u = threadIdx.x; u < live * (DP / 4); u += NW * kWave) {
       const int row = u / (DP / 4), d = u % (DP / 4) * 4;
       float top = jm[row];
@@ -258,11 +259,15 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
           a.lse[lse_at(a, p.r, head, row0 + row)] = final_lse<V>(top, sum, sees, a, p.r, head, row0 + row);
       }
     }
-    __syncthreads();
+    // nobody waits for the stores above, but for rows that are stored again
+    wait_lds();
+    barrier_only();
+    const bool again = __any(lane < 32 + NW && flag[lane < 32 + NW ? lane : 0] != 0);
+    if (again) __syncthreads();
     int any_suspect = 0;
 #pragma unroll
     for (int i = 0; i < NW; ++i) any_suspect |= flag[32 + i];
-    for (int row = wave; row < live; row += NW) {
+    for (int row = wave; row < live && again; row += NW) {
       if ((flag[row] | any_suspect) == 0) continue;
       const Span s = token_span<V>(a, p.r, token_of(a, row0 + row));
       SlowRow<V, DP> slow;
@@ -270,9 +275,9 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
                s.begin > lo ? s.begin : lo, s.end < hi ? s.end : hi);
       slow.template store<ROWS>(a, p.r, head, row0 + row, row, cut ? slot : -1, flag[row] != 0);
     }
-    __syncthreads();
     pos = seg_end;
     if (pos < pos_end) {
+      __syncthreads();  // the stages are free
       placed = advance<V, ROWS, STEP>(a, batch, p, head);
       if (!placed) head = (int)quotient(pos, head_len);
     }
