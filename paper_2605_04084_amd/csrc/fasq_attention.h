@@ -68,7 +68,6 @@ struct AttentionArgs {
   bool negate;  // scale < 0: the queries change sign instead
   bool causal;
   bool out_vec;  // 8-byte stores of out
-  bool out_rows;  // 16-byte ones
   bool whole_units;     // pages hold whole units of 16 keys, within 2^31 bytes
   int window;  // 0: none, or all that there can be
   float* lse;

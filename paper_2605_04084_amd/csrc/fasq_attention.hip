@@ -85,7 +85,6 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
     return reinterpret_cast<uintptr_t>(v.p) % bytes == 0 && v.ts % (bytes / 2) == 0 && v.hs % (bytes / 2) == 0;
   };
   a.out_vec = aligned(p.out, 8);
-  a.out_rows = aligned(p.out, 16);
   a.whole_units = p.cache.page_size % 16 == 0 && p.cache.slot_stride < int64_t(1) << 25;
   a.lse = p.lse;
   if (pl.split && p.workspace != nullptr && p.workspace_bytes >= pl.bytes) {

@@ -551,27 +551,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     const int64_t slot = cut ? slot_of(w, share, t0) : 0;
     if (shared && seg_end == pos_end && threadIdx.x == 0)
       leave_cut(end, w, share, p, tile, head, t0, t1, t0 >= w * share && t1 > seg_end);
-    uint64_t broken = __ballot(alive && t.broken());
-    broken = (broken | broken >> 32) & 0xFFFFFFFFu;
-    __syncthreads();  // the stages are free
-    // Whole rows go through the wave's own part of the stages, where neighbouring
-    // lanes find neighbouring values (a lane holds four of every eight of its row):
-    // 400 documents of 10 tokens 45 -> XX us.
-    const bool aside = FULL && (cut || end.out_rows);
-    uint8_t* const own = smem + wave * (32 * DP * 4);
-    int row_of = l32, half = h;
-    asm volatile("" : "+v"(row_of), "+v"(half));  // no address of this is kept over the keys
     if (alive) {
       if (cut) {
         const int64_t at = slot * ROWS + wave * 32 + l32;
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float4_t v = {t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
-            if (FULL) *reinterpret_cast<float4_t*>(own + row_of * (DP * 4) + ((i * 8 + e * 2 + half) ^ (row_of & 7)) * 16) = v;
-            else *reinterpret_cast<float4_t*>(end.part_o + at * DP + i * 32 + e * 8 + h * 4) = v;
-          }
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<float4_t*>(end.part_o + at * DP + i * 32 + e * 8 + h * 4) =
+                float4_t{t.o[i][4 * e], t.o[i][4 * e + 1], t.o[i][4 * e + 2], t.o[i][4 * e + 3]};
         if (h == 0) {
           end.part_ml[at * 2] = t.top();
           end.part_ml[at * 2 + 1] = l;
@@ -585,41 +573,16 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float v[4] = {t.o[i][4 * e] * f, t.o[i][4 * e + 1] * f, t.o[i][4 * e + 2] * f, t.o[i][4 * e + 3] * f};
-            if (aside) {
-              half4_t r;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) r[k] = static_cast<half_t>(v[k]);
-              *reinterpret_cast<half4_t*>(own + row_of * (DP * 2) + ((i * 4 + e) ^ (row_of & 7)) * 16 + half * 8) = r;
-            } else {
-              store4(end, dst, i * 32 + e * 8 + h * 4, v);
-            }
+            store4(end, dst, i * 32 + e * 8 + h * 4, v);
           }
         if (h == 0 && end.lse != nullptr)
           end.lse[lse_at(end, p.r, head, row0 + l32)] =
               final_lse<V>(t.top(), l, sees, end, p.r, head, row0 + l32);
       }
     }
-    if (aside) {
-      wait_lds();
-      const int first = half * 32 + row_of;
-      if (cut) {
-        constexpr int CHUNKS = DP / 4;  // of 16 bytes a row
-        float* to = end.part_o + (slot * ROWS + wave * 32) * DP;
-#pragma unroll 4
-        for (int u = first; u < live * CHUNKS; u += kWave) {
-          const int row = u / CHUNKS, c = u % CHUNKS;
-          *reinterpret_cast<u32x4*>(to + u * 4) = *reinterpret_cast<const u32x4*>(own + row * (CHUNKS * 16) + (c ^ (row & 7)) * 16);
-        }
-      } else {
-        constexpr int CHUNKS = DP / 8;
-#pragma unroll 2
-        for (int u = first; u < live * CHUNKS; u += kWave) {
-          const int row = u / CHUNKS, c = u % CHUNKS;
-          *reinterpret_cast<u32x4*>(out_row(end, p.r, head, row0 + row) + c * 8) =
-              *reinterpret_cast<const u32x4*>(own + row * (CHUNKS * 16) + (c ^ (row & 7)) * 16);
-        }
-      }
-    }
+    uint64_t broken = __ballot(alive && t.broken());
+    broken = (broken | broken >> 32) & 0xFFFFFFFFu;
+    __syncthreads();
     uint64_t again = *flag != 0 && live > 0 ? (uint64_t(1) << live) - 1 : broken;
     if (again != 0) {
       wait_loads<0>();  // the stores above come first
