@@ -232,11 +232,9 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
   const int64_t row0 = chunk * a.rows, row1 = row0 + a.rows < a.R ? row0 + a.rows : a.R;
   const bool counted = a.counted, biased = a.max_bias > 0, apart = a.rows > 1 && counted;
   int* const slots = reinterpret_cast<int*>(counts) + (apart ? SLICE : 0);
-  // A token's place in the slice; SLICE and more: not there.
-  auto place = [&](int token) {
-    const uint32_t u = (uint32_t)token - (uint32_t)v0;
-    return (uint32_t)token < (uint32_t)a.V ? u : (uint32_t)SLICE;
-  };
+  // A token's place in the slice, if it is below `limit`.
+  const uint32_t limit = left < SLICE ? left : SLICE;
+  auto place = [&](int token) { return (uint32_t)token - (uint32_t)v0; };
   // Where it is counted: the k-th logits of a wave's lanes lie side by side.
   auto column = [](uint32_t u) { return (u & ~511u) | (u & 7) << 6 | (u >> 3 & 63); };
   auto fill = [&](int* to, int value) {
@@ -275,7 +273,7 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
 
   int held = -1;           // the request whose tokens are counted
   int nodes = 0, node0 = 0;  // its drafted tokens
-  uint32_t own = SLICE;    // this thread's of them
+  uint32_t own = ~0u;    // this thread's of them
   bool some_bias = false, some_draft = false;
   int met[GROUPS] = {};  // the columns of this wave in which some token has occurred
   float rho = 1.f, one_over = 1.f, frequency = 0.f, presence = 0.f, cool = 1.f;
@@ -293,7 +291,7 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
       for (int j = tid; j < nodes && j / 32 < a.tree_words; j += TH)
         if (words[j / 32] >> (j % 32) & 1) {
           const uint32_t u = j == tid ? own : place(a.draft_tokens[node0 + j]);
-          if (u < (uint32_t)SLICE) atomicAdd(&counts[column(u)], change);
+          if (u < limit) atomicAdd(&counts[column(u)], change);
         }
     };
     if (req != held) {
@@ -331,9 +329,19 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
         __syncthreads();
         auto scan = [&](int i, int end, auto count) __attribute__((always_inline)) {
           constexpr int AHEAD = 4;
-          auto one = [&](int token) __attribute__((always_inline)) {
-            const uint32_t u = place(token);
-            if (u < (uint32_t)SLICE) count(&counts[column(u)]);
+          // most slices hold few of a text's tokens: four are looked at together
+          auto four = [&](int4_t t) __attribute__((always_inline)) {
+            uint32_t u[4];
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              u[e] = place(t[e]);
+              any |= u[e] < limit;
+            }
+            if (!__any(any)) return;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (u[e] < limit) count(&counts[column(u[e])]);
           };
 #pragma unroll 1
           for (; i + AHEAD * TH * 4 <= end; i += AHEAD * TH * 4) {
@@ -341,20 +349,20 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) t[k] = *reinterpret_cast<const int4_any*>(tokens + i + (k * TH + tid) * 4);
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) one(t[k][e]);
+            for (int k = 0; k < AHEAD; ++k) four(t[k]);
           }
 #pragma unroll 1
-          for (i += tid * 4; i < end; i += TH * 4) {
-            if (i + 4 <= end) {
-              const int4_t t = *reinterpret_cast<const int4_any*>(tokens + i);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) one(t[e]);
+          for (i += wave * kWave * 4; i < end; i += TH * 4) {
+            const int at = i + lane * 4;
+            int4_t t = {-1, -1, -1, -1};
+            if (at + 4 <= end) {
+              t = *reinterpret_cast<const int4_any*>(tokens + at);
             } else {
-#pragma unroll 1
-              for (int k = i; k < end; ++k) one(tokens[k]);
+#pragma unroll
+              for (int e = 0; e < 3; ++e)
+                if (at + e < end) t[e] = tokens[at + e];
             }
+            four(t);
           }
         };
         // a prompt matters to the repetition penalty alone
@@ -364,13 +372,13 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
         int hit = 0;
         for (int i = tid; i < a.max_bias; i += TH) {
           const uint32_t u = place(i == tid ? bias_one : ids[i]);
-          if (u >= (uint32_t)SLICE) continue;
+          if (u >= limit) continue;
           hit = 1;
           if (apart || !counted) atomicMax(&slots[u], i);  // a token's last entry counts
         }
         for (int j = tid; j < nodes; j += TH) {
           const uint32_t u = j == tid ? own : place(a.draft_tokens[node0 + j]);
-          if (u >= (uint32_t)SLICE) continue;
+          if (u >= limit) continue;
           hit |= 2;
           atomicOr(&drafts[u >> 9], 1 << (u & 7));
         }
@@ -429,7 +437,7 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
         __syncthreads();
         for (int i = tid; i < a.max_bias; i += TH) {
           const uint32_t u = place(ids[i]);
-          if (u < (uint32_t)SLICE) atomicMax(&slots[u], i);
+          if (u < limit) atomicMax(&slots[u], i);
         }
         __syncthreads();
       }
