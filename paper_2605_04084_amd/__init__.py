@@ -953,7 +953,7 @@ def process_logits_workspace_bytes(R: int, V: int) -> int:
 def process_logits(logits, requests=None, *, tokens=None, token_count=None, prompt_len=None, repetition=None, presence=None,
                    frequency=None, bias_ids=None, bias_values=None, temperature=None, allowed=None, draft_tokens=None,
                    q_start=None, tree=None, requests_count: Optional[int] = None, out=None, write: bool = True,
-                   choose: bool = False, workspace=None):
+                   choose: bool = False, choice=None, lse=None, workspace=None):
     """Rows of logits [R x V] (fp16 or fp32) under the rules of their requests,
     row r of request ``requests[r]`` (int32 [R]; None: row r of request r; a row
     whose request does not exist is left alone).
@@ -970,7 +970,8 @@ def process_logits(logits, requests=None, *, tokens=None, token_count=None, prom
     Returns the rows (``out``, fp16 or fp32, may be ``logits``; None with ``write``
     False), or with ``choose`` ``(rows, choice, lse)``: the likeliest tokens (int32
     [R], the lowest of equal ones; -1: none is allowed) and the logarithms of the
-    softmax sums (fp32 [R]).  See ``fasq_process_logits``."""
+    softmax sums (fp32 [R]), in ``choice`` and ``lse`` where they are given.  See
+    ``fasq_process_logits``."""
     torch = _torch()
     i32, f32 = torch.int32, torch.float32
     if not isinstance(logits, torch.Tensor):
@@ -1037,9 +1038,17 @@ def process_logits(logits, requests=None, *, tokens=None, token_count=None, prom
         out_at, out_stride = out.data_ptr(), out.stride(0)
     elif out is not None:
         raise ValueError("out is given, but write is False")
-    choice = lse = None
     if choose:
-        choice, lse = logits.new_empty(of_row, dtype=i32), logits.new_empty(of_row, dtype=f32)
+        if choice is None:
+            choice = logits.new_empty(of_row, dtype=i32)
+        else:
+            vector(choice, "choice", i32, of_row)
+        if lse is None:
+            lse = logits.new_empty(of_row, dtype=f32)
+        else:
+            vector(lse, "lse", f32, of_row)
+    elif choice is not None or lse is not None:
+        raise ValueError("choice and lse need choose")
     L = lib()
 
     def call(stream):

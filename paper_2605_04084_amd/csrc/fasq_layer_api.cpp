@@ -174,9 +174,8 @@ fasq_status fasq_paged_attention_ex(const void* q, int64_t q_ts, int64_t q_hs, i
       return bad("slopes need a scale of 2^-24 to 2^64");
     if ((m.spans != nullptr || m.tree != nullptr) && window > 0) return bad("window must be 0 with spans or tree");
     if (m.tree != nullptr && m.slopes != nullptr) return fasq::fail(FASQ_ERR_UNSUPPORTED, "slopes with tree");
-    if (m.tree != nullptr && (m.tree_words < 1 || m.tree_words > fasq::kMaxTokens || m.tree_stride < m.tree_words ||
-                              m.tree_stride > fasq::kMaxStride))
-      return bad("tree_words must be >= 1, tree_stride at least that");
+    if (m.tree != nullptr && (m.tree_words < 1 || m.tree_words > fasq::kMaxTokens || !fasq::stride_ok(m.tree_stride)))
+      return bad("tree_words must lie in [1, 2^24], tree_stride in [0, 2^40]");
     if (fasq::misaligned(m.slopes, 4) || fasq::misaligned(m.spans, 4) || fasq::misaligned(m.tree, 4))
       return bad("slopes, spans and tree must be 4-byte aligned");
     more = {m.softcap, m.slopes, m.spans, m.tree, m.tree != nullptr ? m.tree_stride : 0,
@@ -384,9 +383,8 @@ fasq_status fasq_process_logits(const void* logits, int logits_fp32, int64_t str
     return bad("strides must lie in [0, 2^40]");
   if ((r.draft_tokens == nullptr) != (r.tree == nullptr) || (r.q_start == nullptr) != (r.tree == nullptr))
     return bad("draft_tokens, q_start and tree are given together or not at all");
-  if (r.tree != nullptr && (r.tree_words < 1 || r.tree_words > fasq::kMaxTokens || r.tree_stride < r.tree_words ||
-                            r.tree_stride > fasq::kMaxStride))
-    return bad("tree_words must be >= 1, tree_stride at least that");
+  if (r.tree != nullptr && (r.tree_words < 1 || r.tree_words > fasq::kMaxTokens || !fasq::stride_ok(r.tree_stride)))
+    return bad("tree_words must lie in [1, 2^24], tree_stride in [0, 2^40]");
   if ((r.repetition != nullptr || r.presence != nullptr || r.frequency != nullptr) && r.token_count == nullptr &&
       r.tree == nullptr)
     return bad("repetition, presence and frequency need tokens or a tree");

@@ -261,6 +261,31 @@ def test_same_bits_again_and_other_rows_do_not_matter():
         assert np.array_equal(x[:3], y[:3])
 
 
+@pytest.mark.parametrize("names", [Rows.ALL[:10], ("bias_ids", "bias_values"), ("tokens", "token_count", "presence", "repetition"), ("temperature",)])
+def test_requests_in_any_order(names):
+    """Rows of many requests mixed, several to a request, and rows of none between them."""
+    b = Rows(3, 11, 9001, seed=14)
+    rng = np.random.default_rng(14)
+    b.requests = rng.integers(-1, 4, 33).astype(np.int32)
+    b.requests[7:15] = 1
+    out = torch.full((33, 9001), 9.0, dtype=torch.float16, device="cuda:0")
+    choice = torch.full((33,), -7, dtype=torch.int32, device="cuda:0")
+    lse = torch.full((33,), 7.0, dtype=torch.float32, device="cuda:0")
+    got = b.both(names, out=out, choice=choice, lse=lse)
+    none = (b.requests < 0) | (b.requests > 2)
+    assert none.any() and (got[0][none] == 9).all() and (got[1][none] == -7).all() and (got[2][none] == 7).all()
+
+
+def test_broadcast_rules():
+    """One text, one grammar and one tree for all, as expanded tensors."""
+    b = Rows(4, 1, 3003, seed=15)
+    b.tokens[:], b.allowed[:], b.bits[:], b.tree[:], b.logits[:] = b.tokens[0], b.allowed[0], b.bits[0], b.tree[0], b.logits[0]
+    want = b.both()
+    wide = {k: to_dev(getattr(b, k)[:1]).expand(4, -1) for k in ("tokens", "allowed", "tree", "logits")}
+    for x, y in zip(b.run(**wide), want):
+        assert np.array_equal(x, y)
+
+
 def test_large_vocabulary_of_few_rows():
     b = Rows(2, 1, 128256, L=3000, E=300, seed=11)
     b.both()
@@ -285,8 +310,11 @@ def test_tensors_are_checked():
                dict(token_count=torch.zeros(2, dtype=torch.int64, device="cuda:0"))):
         with pytest.raises((TypeError, ValueError)):
             b.run(**kw)
+    for kw in (dict(tokens=None), dict(choice=torch.zeros(5, **i32)), dict(lse=torch.zeros(6, **i32))):
+        with pytest.raises((TypeError, ValueError)):
+            b.run(**kw)
     with pytest.raises(ValueError):
-        b.run(tokens=None)
+        fasq.process_logits(to_dev(b.logits), lse=torch.zeros(6, **f32))
     for kw in (dict(tokens=None, token_count=None), dict(q_start=None), dict(bias_ids=None, bias_values=torch.zeros((2, 0), **f32)),
                dict(workspace=torch.empty(16, dtype=torch.uint8, device="cuda:0"), logits=torch.zeros((6, 9000), **f32), allowed=None)):
         with pytest.raises((fasq.FasqError, ValueError)):

@@ -25,7 +25,7 @@ def _attention(L, scores, **kw):
     (dict(softcap=5.0), dict(scale=float("inf")), "softcap needs"), (dict(softcap=5.0), dict(scale=-1e20), "softcap needs"),
     (dict(slopes=DUMMY), dict(scale=0.0), "slopes need"), (dict(slopes=DUMMY), dict(scale=1e20), "slopes need"),
     (dict(spans=DUMMY), dict(window=5), "window"), (dict(tree=DUMMY, tree_words=1, tree_stride=1), dict(window=5), "window"),
-    (dict(tree=DUMMY), {}, "tree_words"), (dict(tree=DUMMY, tree_words=2, tree_stride=1), {}, "tree_stride"),
+    (dict(tree=DUMMY), {}, "tree_words"), (dict(tree=DUMMY, tree_words=2 ** 25, tree_stride=1), {}, "tree_words"),
     (dict(tree=DUMMY, tree_words=2, tree_stride=-1), {}, "tree_stride"), (dict(tree=DUMMY + 2, tree_words=1, tree_stride=1), {}, "4-byte"),
     (dict(slopes=DUMMY + 1), {}, "4-byte"), (dict(spans=DUMMY + 2), {}, "4-byte"), (dict(), dict(T=-1), "T must"),
     (dict(softcap=5.0), dict(out=DUMMY), "out must not be q"),
@@ -67,7 +67,7 @@ TREE = dict(draft_tokens=DUMMY, q_start=DUMMY, tree=DUMMY, tree_words=1, tree_st
     (dict(bias_ids=DUMMY), {}, "together"), (dict(bias_values=DUMMY), {}, "together"),
     (dict(bias_ids=DUMMY, bias_values=DUMMY, max_bias=-1), {}, "max_bias"), (dict(allowed=DUMMY, allowed_stride=-4), {}, "strides"),
     (dict(draft_tokens=DUMMY), {}, "together"), ({**TREE, "q_start": 0}, {}, "together"), ({**TREE, "tree_words": 0}, {}, "tree_words"),
-    ({**TREE, "tree_stride": 0}, {}, "tree_stride"), (dict(repetition=DUMMY), {}, "need tokens"), (dict(frequency=DUMMY), {}, "need tokens"),
+    ({**TREE, "tree_stride": -1}, {}, "tree_stride"), (dict(repetition=DUMMY), {}, "need tokens"), (dict(frequency=DUMMY), {}, "need tokens"),
     (dict(temperature=DUMMY + 2), {}, "4-byte"), ({}, dict(lse=DUMMY + 2), "4-byte"),
 ])
 def test_logits_refuse(L, rules, kw, why):  # noqa: F811
