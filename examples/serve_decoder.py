@@ -17,6 +17,9 @@ Prompts are read in steps of at most ``chunk`` tokens that may end inside a
 prompt and hold several requests.  The answers' tokens are then taken one a
 step: the layers are captured into a HIP graph whose inputs (the tokens' rows,
 positions, cache slots and lengths) stay on the device and are updated there.
+Or several a step (--draft): a tree of guesses follows the last token, attention
+lets each see its own branch, process_logits chooses a token after every one of
+them, and the guesses that are what was chosen stand.
 Weights are random, so the answers mean nothing.
 """
 
@@ -49,6 +52,7 @@ class Config:
     page_size: int = 16
     max_len: int = 512
     window: int = 0
+    repetition: float = 1.0
     eps: float = 1e-5
     d: int = 2
     codewords: int = 256
@@ -97,6 +101,8 @@ class Batch:
     adapters: torch.Tensor   # int32 [T], -1: none
     q_start: torch.Tensor    # int32 [B + 1]
     kv_len: torch.Tensor     # int32 [B], with this step's tokens
+    tree: torch.Tensor = None   # of drafted tokens: which of them each one sees,
+    spans: torch.Tensor = None  # and its window
 
 
 class Decoder:
@@ -150,16 +156,17 @@ class Decoder:
             fasq.rope_append(q, k, v, self.table, batch.positions, batch.slots, self.k[i], self.v[i],
                              q_norm=w["q_norm"], k_norm=w["k_norm"], eps=cfg.eps, out=q)
             a = fasq.paged_attention(q, self.k[i], self.v[i], self.device_pages, batch.q_start, batch.kv_len,
-                                     window=cfg.window)
+                                     window=cfg.window if batch.tree is None else 0, spans=batch.spans, tree=batch.tree)
             y, = self.project(a.view(T, -1), w["o"])
             x, h = fasq.residual_norm(x, y, w["mlp_norm"], cfg.eps)
             gate, up = self.project(h, w["gate_up"])
             y, = self.project(torch.nn.functional.silu(gate).mul_(up), w["down"])
         return fasq.residual_norm(x, y, self.w["norm"], cfg.eps)[1]
 
-    def next_tokens(self, rows):
-        """The likeliest tokens after these output rows."""
-        return self.project(rows, self.w["head"])[0].argmax(dim=1)
+    def next_tokens(self, rows, requests=None, **rules):
+        """The likeliest tokens after these output rows, under these rules (see process_logits)."""
+        logits, = self.project(rows, self.w["head"])
+        return fasq.process_logits(logits, requests, write=False, choose=True, **rules)[1].long()
 
     def embed(self, tokens):
         return self.w["embed"].index_select(0, tokens)
@@ -234,6 +241,87 @@ def answer(dec: Decoder, lengths, first, adapters, count: int):
     return torch.stack(tokens, 1), torch.stack(rows, 1)
 
 
+def guess(text, branches: int = 2, depth: int = 4):
+    """A tree that may follow a text: what followed its last token before, the
+    latest places first.  Tokens and the node that each follows; node 0 is the last token."""
+    tokens, parents = [text[-1]], [-1]
+    for at in [i for i in range(len(text) - 2, -1, -1) if text[i] == text[-1]][:branches]:
+        node = 0
+        for t in text[at + 1:at + 1 + depth]:
+            tokens.append(t)
+            parents.append(node)
+            node = len(tokens) - 1
+    return tokens, parents
+
+
+def answer_drafted(dec: Decoder, prompts, first, adapters, count: int, draft=guess):
+    """At least ``count`` tokens of every request after its prompt, from the
+    tokens ``first`` on, several a step where ``draft`` guesses them.  Returns the
+    tokens, the output row of each (lists, one entry a request) and the number of steps."""
+    cfg, B = dec.cfg, len(prompts)
+    text = [list(map(int, p)) + [int(t)] for p, t in zip(prompts, first)]
+    rows, steps = [[] for _ in range(B)], 0
+    ends = [len(t) + count for t in text]
+    held = torch.zeros((B, cfg.max_len), dtype=torch.int32)
+    for b, t in enumerate(text):
+        held[b, :len(t)] = torch.tensor(t)
+    held = held.to(dec.device)
+
+    def i32(a):
+        return torch.from_numpy(np.asarray(a, dtype=np.int32)).to(dec.device)
+
+    while any(len(t) < e for t, e in zip(text, ends)):
+        steps += 1
+        trees = [draft(t) if len(t) < e else ([], []) for t, e in zip(text, ends)]
+        start = [len(t) - 1 for t in text]  # cached tokens
+        trees = [(t[:cfg.max_len - s], p[:cfg.max_len - s]) for (t, p), s in zip(trees, start)]
+        n = [len(t) for t, _ in trees]
+        for b in range(B):
+            dec.reserve(b, start[b] + n[b])
+        dec.publish_pages()
+        tree, depth = fasq.draft_tree([p for _, p in trees], device=dec.device)
+        req, first_row = np.repeat(np.arange(B), n), np.cumsum([0] + n)
+        at = np.array(start)[req] + np.arange(len(req)) - first_row[req]
+        slots = dec.pages[req, at // cfg.page_size] * cfg.page_size + at % cfg.page_size
+        positions, kv_len = i32(np.array(start)[req]) + depth, i32([s + m for s, m in zip(start, n)])
+        spans = None
+        if cfg.window:
+            spans = torch.stack([(positions - cfg.window + 1).clamp_(min=0), kv_len[i32(req).long()]], 1)
+        drafted = i32(np.concatenate([t for t, _ in trees]))
+        batch = Batch(positions, i32(slots), i32(np.asarray(adapters)[req]), i32(first_row), kv_len, tree, spans)
+        out = dec.layers(dec.embed(drafted), batch)
+        rules = {}
+        if cfg.repetition != 1.0:
+            rules = dict(tokens=held, token_count=i32(start), repetition=torch.full((B,), cfg.repetition, device=dec.device),
+                         draft_tokens=drafted, tree=tree, q_start=batch.q_start)
+        chosen = dec.next_tokens(out, i32(req), requests_count=B, **rules).tolist()
+        moved = [[], []]
+        for b, (tokens, parents) in enumerate(trees):
+            if not tokens:
+                continue
+            way, base = [0], int(first_row[b])
+            while True:
+                token = chosen[base + way[-1]]
+                after = [j for j in range(len(tokens)) if parents[j] == way[-1] and tokens[j] == token]
+                if not after:
+                    break
+                way.append(after[0])
+            # the branch that stands moves up in the cache, to where its tokens belong
+            for i, node in enumerate(way):
+                to = start[b] + i
+                moved[0].append(int(slots[base + node]))
+                moved[1].append(int(dec.pages[b, to // cfg.page_size] * cfg.page_size + to % cfg.page_size))
+            rows[b].append(out[base:base + len(tokens)][way])
+            text[b] += [tokens[j] for j in way[1:]] + [token]
+            held[b, :len(text[b])] = i32(text[b][:cfg.max_len])
+        source, target = (torch.tensor(m, device=dec.device) for m in moved)
+        for cache in (dec.k, dec.v):
+            flat = cache.flatten(1, 2)
+            flat[:, target] = flat[:, source]
+    said = [t[len(p):-1] for t, p in zip(text, prompts)]
+    return said, [torch.cat(r) for r in rows], steps
+
+
 def main():
     p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     for name in ("hidden", "heads", "kv_heads", "head_dim", "inter", "layers", "vocab", "adapters", "rank",
@@ -242,7 +330,10 @@ def main():
     p.add_argument("--prompts", default="200,7,133,1", help="prompt lengths, one request each (at most 16)")
     p.add_argument("--chunk", type=int, default=128, help="tokens of a prompt step")
     p.add_argument("--answer", type=int, default=32, help="tokens of every answer")
+    p.add_argument("--draft", action="store_true", help="several tokens a step where the text so far lets them be guessed")
+    p.add_argument("--repetition", type=float, default=Config.repetition, help="penalty for tokens that occurred (with --draft)")
     args = vars(p.parse_args())
+    drafted = args.pop("draft")
     lengths, chunk, count = [int(n) for n in args.pop("prompts").split(",")], args.pop("chunk"), args.pop("answer")
     if not 1 <= len(lengths) <= 16 or min(lengths) < 1 or chunk < 1 or count < 1:
         p.error("1 to 16 prompts, lengths, chunk and answer of at least 1")
@@ -257,13 +348,17 @@ def main():
     first = dec.next_tokens(torch.stack([r[-1] for r in rows]))
     torch.cuda.synchronize()
     t1 = time.perf_counter()
-    tokens, _ = answer(dec, lengths, first, adapters, count)
+    steps = count
+    if drafted:
+        said, _, steps = answer_drafted(dec, prompts, first, adapters, count)
+    else:
+        said = answer(dec, lengths, first, adapters, count)[0].tolist()
     torch.cuda.synchronize()
     t2 = time.perf_counter()
     for b, n in enumerate(lengths):
-        print(f"request {b}: prompt of {n}, adapter {adapters[b]}: {tokens[b].tolist()[:12]} ...")
+        print(f"request {b}: prompt of {n}, adapter {adapters[b]}: {said[b][:12]} ...")
     print(f"{sum(lengths)} prompt tokens in {(t1 - t0) * 1e3:.1f} ms (first calls included), "
-          f"{count} steps of {len(lengths)} tokens in {(t2 - t1) * 1e3:.1f} ms (capture included)")
+          f"{sum(map(len, said))} tokens in {steps} steps in {(t2 - t1) * 1e3:.1f} ms (capture included)")
 
 
 if __name__ == "__main__":
