@@ -694,6 +694,21 @@ def _kv_cache(k_cache, v_cache, device, Hkv=None, D=None):
     return KvCache(k_cache.data_ptr(), v_cache.data_ptr(), pages, page_size, strides[0], strides[1], strides[2])
 
 
+_needs = {}  # workspace bytes by entry point, device and sizes
+
+
+def _workspace_need(name, device, *sizes):
+    """``name(*sizes)`` on the current device (``device``): asked once for sizes that
+    come again with every step (0.6 us of a call)."""
+    key = (name, device, sizes)
+    need = _needs.get(key)
+    if need is None:
+        need = getattr(lib(), name)(*sizes)
+        if need >= 0 and len(_needs) < 4096:
+            _needs[key] = need
+    return need
+
+
 def _workspace(workspace, need, device, like):
     """The workspace to use and its bytes: the caller's, or a new one on the tensor ``like``'s device."""
     if workspace is None:
@@ -881,12 +896,12 @@ def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
         _check_rows(out, "out", torch.float16, q.shape, device)
-    lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if return_lse else None
+    lse = q.new_empty((T, Hq), dtype=torch.float32) if return_lse else None
     qs, os_ = q.stride(), out.stride()
     L = lib()
     scores = None
     if softcap or slopes is not None or spans is not None or tree is not None:
-        scores = AttentionScores(softcap)
+        scores = AttentionScores(softcap or 0.0)
         if slopes is not None:
             _check_tensor(slopes, "slopes", torch.float32, (Hq,), device)
             scores.slopes = slopes.data_ptr()
@@ -897,7 +912,7 @@ def paged_attention(q, k_cache, v_cache, pages, q_start, kv_len, scale: Optional
             scores.tree, scores.tree_stride, scores.tree_words = _tree(tree, T, device)
 
     def call(stream):
-        need = L.fasq_paged_attention_workspace_bytes(T, B, Hq, Hkv, D) if workspace is None else 0
+        need = _workspace_need("fasq_paged_attention_workspace_bytes", device, T, B, Hq, Hkv, D) if workspace is None else 0
         ws, ws_bytes = _workspace(workspace, need, device, q)
         if scores is not None:
             return L.fasq_paged_attention_ex(q.data_ptr(), qs[0], qs[1], T, Hq, cache, Hkv, D, pages.data_ptr(),
@@ -1052,7 +1067,7 @@ def process_logits(logits, requests=None, *, tokens=None, token_count=None, prom
     L = lib()
 
     def call(stream):
-        need = L.fasq_process_logits_workspace_bytes(R, V) if choose and workspace is None else 0
+        need = _workspace_need("fasq_process_logits_workspace_bytes", device, R, V) if choose and workspace is None else 0
         ws, ws_bytes = _workspace(workspace, need, device, logits)
         return L.fasq_process_logits(logits.data_ptr(), wide, logits.stride(0), R, V, rules.buffer_info()[0], out_at, out_wide,
                                      out_stride, _ptr(choice), _ptr(lse), _ptr(ws), ws_bytes, stream)

@@ -128,19 +128,6 @@ __device__ __forceinline__ Request read_request(const AttentionArgs& a, int64_t 
   return {q0, q1 - q0, kv};
 }
 
-// The batch as a wave sees it: lane l keeps requests l, l + 64, ..., the first
-// of them in registers (all there are in most batches).
-struct Batch {
-  Request first;
-  __device__ __forceinline__ explicit Batch(const AttentionArgs& a) {
-    const int lane = threadIdx.x % kWave;
-    first = lane < a.B ? read_request(a, lane) : Request{0, 0, 0};
-  }
-  __device__ __forceinline__ Request of(const AttentionArgs& a, int64_t b) const {
-    return b < kWave ? first : read_request(a, b);
-  }
-};
-
 // Keys [begin, end) that token i of a request sees.
 struct Span {
   int begin, end;
@@ -260,6 +247,41 @@ __device__ __forceinline__ float lse_bias(const AttentionArgs& a, const Request&
   return b.nearest == 0 ? 0.f : b.slope * a.c * (float)b.nearest * 0.69314718055994530942f;
 }
 
+// The batch as a wave sees it: lane l keeps requests l, l + 64, ..., the first
+// of them in registers (all there are in most batches).
+template <class V>
+struct Batch {
+  Request first;
+  int keys;  // that one of its tiles can need
+  __device__ __forceinline__ explicit Batch(const AttentionArgs& a) {
+    const int lane = threadIdx.x % kWave;
+    first = lane < a.B ? read_request(a, lane) : Request{0, 0, 0};
+    keys = first.kv;
+    if constexpr (V::kMore) {
+      // Where a few tokens see runs of keys of their own, the keys that some of them
+      // sees; a single request's by the whole wave.
+      if (a.spans != nullptr) {
+        Request r = first;
+        const bool one = a.B == 1;
+        if (one) r = {__builtin_amdgcn_readfirstlane(first.q0), __builtin_amdgcn_readfirstlane(first.n), __builtin_amdgcn_readfirstlane(first.kv)};
+        Span s = {INT32_MAX, 0};
+        const bool few = r.n <= (one ? 256 : 32);
+        for (int i = one ? lane : 0; few && i < r.n; i += one ? kWave : 1) {
+          const Span t = token_span<V>(a, r, i);
+          if (t.begin < t.end) s = {min(s.begin, t.begin), max(s.end, t.end)};
+        }
+        if (one)
+          s = {wave_join(s.begin, [](int x, int y) { return x < y ? x : y; }), wave_join(s.end, [](int x, int y) { return x > y ? x : y; })};
+        if (few) keys = s.begin < s.end ? s.end - s.begin / 32 * 32 : 0;
+      }
+    }
+  }
+  __device__ __forceinline__ Request of(const AttentionArgs& a, int64_t b) const {
+    return b < kWave ? first : read_request(a, b);
+  }
+  __device__ __forceinline__ int keys_of(const Request& r, int64_t b) const { return V::kMore && b < kWave ? keys : r.kv; }
+};
+
 // The batch as a line of positions.  With `parts` shares, every cache head
 // has the same stretch, in it the requests in order, in them their tiles, and
 // a tile is as long as the keys its request can need (a multiple of STEP, at
@@ -274,20 +296,8 @@ struct Place {
 };
 
 template <class V, int ROWS, int STEP>
-__device__ __forceinline__ int64_t tile_length(const AttentionArgs& a, const Request& r, bool shared) {
+__device__ __forceinline__ int64_t tile_length(const AttentionArgs& a, const Request& r, int keys, bool shared) {
   if (!shared) return 1;
-  int keys = r.kv;
-  if constexpr (V::kMore) {
-    // where a few tokens see runs of keys of their own, the keys that some of them sees
-    if (a.spans != nullptr && r.n <= 8) {
-      Span s = {INT32_MAX, 0};
-      for (int i = 0; i < r.n; ++i) {
-        const Span t = token_span<V>(a, r, i);
-        if (t.begin < t.end) s = {min(s.begin, t.begin), max(s.end, t.end)};
-      }
-      keys = s.begin < s.end ? s.end - s.begin / 32 * 32 : 0;
-    }
-  }
   if (a.window > 0) {
     // of the tile's tokens, from a multiple of 32 on; without causality the
     // request's first token sees the window before it and all that follows
@@ -324,26 +334,30 @@ __device__ __forceinline__ int tiles_of(const AttentionArgs& a, const Request& r
 
 // Positions of one cache head; of every classes-th tile.
 template <class V, int ROWS, int STEP>
-__device__ __forceinline__ int64_t head_length(const AttentionArgs& a, const Batch& batch, bool shared, int classes = 1) {
+__device__ __forceinline__ int64_t head_length(const AttentionArgs& a, const Batch<V>& batch, bool shared, int classes = 1) {
   int64_t sum = 0;
+  if (a.B == 1) {
+    const Request r = {uniform(batch.first.q0), uniform(batch.first.n), uniform(batch.first.kv)};  // of lane 0
+    return tiles_of<ROWS>(a, r, classes) * tile_length<V, ROWS, STEP>(a, r, uniform(batch.keys), shared);
+  }
   for (int64_t b = threadIdx.x % kWave; b < a.B; b += kWave) {
     const Request r = batch.of(a, b);
-    sum += tiles_of<ROWS>(a, r, classes) * tile_length<V, ROWS, STEP>(a, r, shared);
+    sum += tiles_of<ROWS>(a, r, classes) * tile_length<V, ROWS, STEP>(a, r, batch.keys_of(r, b), shared);
   }
-  return a.B == 1 ? lane_value(sum, 0) : uniform(wave_total(sum));
+  return uniform(wave_total(sum));
 }
 
 // The tile at a position within a head's stretch, in every lane of the wave.
 // pos < head_length.
 template <class V, int ROWS, int STEP>
-__device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& batch, int64_t pos, bool shared,
+__device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch<V>& batch, int64_t pos, bool shared,
                                          int classes = 1) {
   Place p = {};
   int64_t base = 0;
   if (a.B == 1) {
     p.b = 0;
     p.r = {uniform(batch.first.q0), uniform(batch.first.n), uniform(batch.first.kv)};  // of lane 0
-    const int64_t one = tile_length<V, ROWS, STEP>(a, p.r, shared);
+    const int64_t one = tile_length<V, ROWS, STEP>(a, p.r, uniform(batch.keys), shared);
     p.tile = (int)(shared ? quotient(pos, one) : pos);
     p.start = p.tile * one;
     p.end = p.start + one;
@@ -355,7 +369,7 @@ __device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& bat
     int64_t one = 0, own = 0;
     if (b < a.B) {
       r = batch.of(a, b);
-      one = tile_length<V, ROWS, STEP>(a, r, shared);
+      one = tile_length<V, ROWS, STEP>(a, r, batch.keys_of(r, b), shared);
       own = tiles_of<ROWS>(a, r, classes) * one;
     }
     int64_t upto = own;  // positions up to and with this lane's request
@@ -389,7 +403,7 @@ __device__ __forceinline__ Place locate(const AttentionArgs& a, const Batch& bat
 // The tile behind `p`, of the next request or the next head where that was the
 // last; there is one.  false: not among the next few requests, use locate().
 template <class V, int ROWS, int STEP>
-__device__ __forceinline__ bool advance(const AttentionArgs& a, const Batch& batch, Place& p, int& head,
+__device__ __forceinline__ bool advance(const AttentionArgs& a, const Batch<V>& batch, Place& p, int& head,
                                         int classes = 1) {
   const int64_t one = p.end - p.start;
   if (++p.tile < tiles_of<ROWS>(a, p.r, classes)) {
@@ -408,7 +422,8 @@ __device__ __forceinline__ bool advance(const AttentionArgs& a, const Batch& bat
     if (p.b < kWave) p.r = {lane_value(batch.first.q0, p.b), lane_value(batch.first.n, p.b), lane_value(batch.first.kv, p.b)};
     else p.r = read_request(a, p.b);
     if (p.r.n > 0) {
-      p.end = p.start + tile_length<V, ROWS, STEP>(a, p.r, true);
+      const int keys = V::kMore && p.b < kWave ? lane_value(batch.keys, p.b) : p.r.kv;
+      p.end = p.start + tile_length<V, ROWS, STEP>(a, p.r, keys, true);
       return true;
     }
   }

@@ -113,7 +113,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
 
   const RowCopy<DP, FULL> copy(given);
   const bool shared = given.part_o != nullptr;
-  const Batch batch(given);
+  const Batch<V> batch(given);
   const int64_t head_len = head_length<V, ROWS, STEP>(given, batch, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   int head;
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 
   const RowCopy<DP, FULL> copy(given);
   const bool shared = given.part_o != nullptr;
-  const Batch batch(given);
+  const Batch<V> batch(given);
   // With two classes every request's even tiles lie in the first half of the line,
   // its odd ones at the same places of the second: workgroups of one compute unit
   // then read the same keys at the same time, once from memory (see plan_attention).
@@ -336,9 +336,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     int64_t length = 0;
     if (given.B == 1) {
       const Request one = {uniform(batch.first.q0), uniform(batch.first.n), uniform(batch.first.kv)};
-      length = tile_length<V, ROWS, STEP>(given, one, true);
+      length = tile_length<V, ROWS, STEP>(given, one, uniform(batch.keys), true);
     } else if (given.window > 0 && given.causal) {  // the longest there can be
-      length = tile_length<V, ROWS, STEP>(given, Request{0, 0, INT32_MAX}, true);
+      length = tile_length<V, ROWS, STEP>(given, Request{0, 0, INT32_MAX}, INT32_MAX, true);
     }
     const bool whole = length > 0 && length * DP <= 384 * 128;
     const int parts = classes == 2 ? given.parts / 2 : given.parts;  // of a class

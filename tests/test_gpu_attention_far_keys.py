@@ -77,3 +77,36 @@ def test_windows_of_more_than_2_to_the_30_keys(n):
     s = k[0, :, 0].double().sum(1)
     want = torch.softmax(s, 0) @ v[0, :, 0].double()
     assert float((out.double() - want).abs().max()) <= 2.0 ** -9 * float(v[0].abs().max())
+
+
+@pytest.mark.parametrize("n", [1, 20, 200])
+@pytest.mark.parametrize("kw", [dict(), dict(softcap=3.0), dict(slopes=True)])
+def test_runs_and_trees_at_the_largest_length(n, kw):
+    """Runs of keys at the end of the longest cache, as a short cache has them; the
+    keys may be split elsewhere, so up to a rounding of the weights and one of the result on each side."""
+    q, k, v, q_start = _inputs(n, n)
+    kw = dict(kw, slopes=torch.tensor([0.5, 0.01], device="cuda:0")) if kw.get("slopes") else dict(kw)
+    far_kv, near_kv = 2 ** 31 - 1024, 1600
+    pages = torch.zeros((1, far_kv // SIZE), dtype=torch.int32, device="cuda:0")
+    i = torch.arange(n, device="cuda:0")
+    if "slopes" not in kw:
+        kw["tree"] = torch.randint(-2 ** 31, 2 ** 31, (n, 7), device="cuda:0").int()
+
+    def run(kv):
+        spans = torch.stack([kv - n + i - 300, kv - n + i + 1], 1).int()
+        return fasq.paged_attention(q, k, v, pages[:, :kv // SIZE], q_start, _len(kv), spans=spans, return_lse=True, **kw)
+
+    far, near = run(far_kv), run(near_kv)
+    assert float((far[0] - near[0]).abs().max()) <= 4 * 2.0 ** -11 * float(v.abs().max())
+    assert float((far[1] - near[1]).abs().max()) <= 2.0 ** -12
+
+
+def test_a_tree_over_the_largest_length():
+    """All keys before the tree are alike, so each node's result is theirs."""
+    q, k, v, q_start = _inputs(3, 5)
+    kv = 2 ** 31 - 1024
+    pages = torch.zeros((1, kv // SIZE), dtype=torch.int32, device="cuda:0")
+    tree = torch.tensor([[1], [3], [4]], dtype=torch.int32, device="cuda:0")
+    out = fasq.paged_attention(q, k, v, pages, q_start, _len(kv), tree=tree)
+    near = fasq.paged_attention(q, k, v, pages[:, :1], q_start, _len(SIZE), causal=False)
+    assert float((out - near).abs().max()) <= (2.0 ** -7 + 2.0 ** -9) * float(v.abs().max())  # as above

@@ -274,3 +274,16 @@ def test_trees_of_several_tiles_over_long_caches(reqs, Hq, Hkv, D):
     b = Scored(reqs, Hq, Hkv, D, 64, seed=9)
     b.both(tree=trees_of(np.random.default_rng(9), reqs))
     b.both(softcap=20.0)
+
+
+@pytest.mark.parametrize("reqs", [[(20, 3000), (32, 2500), (9, 700)], [(200, 6000)], [(33, 4000), (64, 300)], [(1, 9000)], [(24, 30)]])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (5, 1, 64)])
+def test_trees_in_windows(reqs, Hq, Hkv, D):
+    """Each node sees a window before its own depth: short runs of long caches."""
+    b = Scored(reqs, Hq, Hkv, D, 16, seed=21)
+    rng = np.random.default_rng(21)
+    tree, depth = fasq.draft_tree([random_tree(rng, n) for n, _ in reqs], device="cpu")
+    start = np.repeat([kv - n for n, kv in reqs], [n for n, _ in reqs])
+    spans = np.stack([np.maximum(0, start + depth.numpy() - 99), np.repeat([kv for _, kv in reqs], [n for n, _ in reqs])], 1).astype(np.int32)
+    b.both(tree=tree.numpy(), spans=spans)
+    b.both(tree=tree.numpy(), spans=spans, workspace=torch.empty(0, dtype=torch.uint8, device="cuda:0"))
