@@ -85,9 +85,7 @@ struct AttentionArgs {
   int tree_words;
   const float* slopes;  // [Hq]
   float slope_unit;     // a slope times this is one in units of the raw products
-  // With z = scale q.k in powers of two, capped scores are cap * tanh(z / cap)
-  // = cap - 2 cap / (1 + 2^(s cap_in)) of the raw product s.
-  float cap, cap_in;
+  float cap, cap_unit;  // softcap in powers of two; a raw product (with its bias) times this is the tanh's argument
   int classes;  // 1, or 2: see k_attention_tile
 };
 
@@ -592,14 +590,27 @@ __device__ __forceinline__ bool cut_to_finite(uint16_t* values) {
 // it: such rows end not finite and are computed again (SlowRow).
 constexpr float kLift = 7.f;
 
-// Capped scores, in powers of two (see AttentionArgs::cap).  1 / (1 + e) and
-// 2^x are off by an ulp each, which makes 2^-22 of the cap.
-__device__ __forceinline__ float capped(const AttentionArgs& a, float s) {
-  return fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * a.cap_in)), a.cap);
+// Capped scores cap * tanh(x), in powers of two.  Arguments up to kSmall by a
+// polynomial in x^2 that is as near to tanh(x) / x as fp32 is (weighted least squares
+// of the relative error over [0, kSmall]: 7.3e-8); it takes half as long as the others',
+// cap - 2 cap / (1 + 2^(2 x log2(e))), whose exponential and reciprocal are off by an
+// ulp each, which makes 2^-22 of the cap.
+constexpr float kSmall = 0.6f;
+__device__ __forceinline__ float capped_small(const AttentionArgs& a, float s) {
+  const float x = s * a.cap_unit, t = x * x;
+  float p = fmaf(t, 0.0154754265905575f, -0.05210147946762546f);
+  p = fmaf(t, p, 0.1331017364332229f);
+  p = fmaf(t, p, -0.33332309973340374f);
+  p = fmaf(t, p, 0.9999999268688409f);
+  return (a.cap * x) * p;
 }
-// A key that a row does not see, in a variant with capped scores (where -inf is a
-// score like others), and the least score that counts for a maximum.
-constexpr float kUnseen = -3.3e38f, kLeast = -3e38f;
+__device__ __forceinline__ float capped_large(const AttentionArgs& a, float s) {
+  const float e = __builtin_amdgcn_exp2f(s * a.cap_unit * 2.88539008177792681f);
+  return fmaf(-2.f * a.cap, __builtin_amdgcn_rcpf(1.f + e), a.cap);
+}
+__device__ __forceinline__ float capped(const AttentionArgs& a, float s) {
+  return fabsf(s * a.cap_unit) < kSmall ? capped_small(a, s) : capped_large(a, s);
+}
 
 template <class V, int DP, int KB>
 struct WaveTile {
@@ -612,10 +623,20 @@ struct WaveTile {
   TreeRow tree;   // with MORE, in calls with a tree
   bool has_tree;
 
-  // The weight of a capped score: an operation of its own after the other where they are many (block()).
-  __device__ __forceinline__ float capped_weight(const AttentionArgs& a, float s) const {
-    const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * a.cap_in));
-    return __builtin_amdgcn_exp2f(fmaf(-2.f * a.cap, r, a.cap - mc));
+  // Caps a block's scores, of which `top` is the row's largest, and that too.
+  __device__ __forceinline__ void cap_scores(const AttentionArgs& a, float16_t& s, float& top) const {
+    float low = s[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) low = fminf(low, s[e]);
+    if (__all(fmaxf(top, -low) * a.cap_unit < kSmall)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = capped_small(a, s[e]);
+      top = capped_small(a, top);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = capped_large(a, s[e]);
+      top = capped_large(a, top);
+    }
   }
 
   // What variants need of row `row`, which exists.
@@ -655,10 +676,8 @@ struct WaveTile {
     return s;
   }
 
-  // A maximum of scores in powers of two.
-  __device__ __forceinline__ float scaled(const AttentionArgs& a, float top) const {
-    return V::kCap ? capped(a, top) : top * a.c;
-  }
+  // Scores times this are powers of two; capped ones are already.
+  __device__ __forceinline__ static float unit(const AttentionArgs& a) { return V::kCap ? 1.f : a.c; }
 
   // A block's scores with those that the row does not see taken out; returns the largest of this lane's.
   __device__ __forceinline__ float mask(float16_t& s, int key0, int begin, int end) const {
@@ -669,7 +688,7 @@ struct WaveTile {
     }
     bits &= last >= 32 ? ~0u : last <= 0 ? 0u : ~(~0u << last);
     bits &= first <= 0 ? ~0u : first >= 32 ? 0u : ~0u << first;
-    const float unseen = V::kCap ? kUnseen : -INFINITY;
+    const float unseen = -INFINITY;
     float top = unseen;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -679,10 +698,6 @@ struct WaveTile {
       asm("v_bfi_b32 %0, %1, %0, %2" : "+v"(v) : "v"(seen), "s"(unseen));
       s[e] = v;
       top = fmaxf(top, v);
-    }
-    if constexpr (V::kCap) {
-      constexpr uint32_t mine = 0x0F0F0F0Fu;  // the keys of this lane
-      top = (bits & mine) != 0 ? fmaxf(top, kLeast) : -INFINITY;
     }
     return top;
   }
@@ -741,7 +756,7 @@ struct WaveTile {
   // the products that take them; the scheduling barriers keep them there.
   __device__ __forceinline__ void step(const uint16_t* keys, const uint16_t* values, int key0, int begin, int end,
                                        bool masked, const AttentionArgs& a) {
-    const float c = a.c;
+    const float c = unit(a);
     const int lane = threadIdx.x % kWave, l32 = lane % 32, h = lane / 32;
     constexpr int KT = DP / 16, AHEAD = 2;
     const uint32_t k_at = lds_address(keys) + l32 * (DP * 2) + (h ^ chunk_swap<DP>(l32)) * 16;
@@ -795,13 +810,14 @@ struct WaveTile {
       top = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        if (masked) {
-          top = fmaxf(top, mask(s[kb], key0 + kb * 32, begin, end));
-        } else {
+        float most = s[kb][0];
+        if (V::kCap || !masked) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
-          if constexpr (V::kCap) top = fmaxf(top, kLeast);
+          for (int e = 1; e < 16; ++e) most = fmaxf(most, s[kb][e]);
         }
+        if constexpr (V::kCap) cap_scores(a, s[kb], most);
+        if (masked) most = mask(s[kb], key0 + kb * 32, begin, end);
+        top = fmaxf(top, most);
       }
     } else {
       if (masked) {
@@ -830,7 +846,7 @@ struct WaveTile {
     const bool grown = (top - m) * c > 8.f;  // from -inf too; not from -inf to -inf
     if (__any(grown)) {
       // the weights are 2^(s c - mc) with the rounded mc, here too
-      const float next_c = scaled(a, top) - kLift;
+      const float next_c = top * c - kLift;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
       scale_sum(keep);
 #pragma unroll
@@ -846,13 +862,7 @@ struct WaveTile {
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        float w;
-        if constexpr (V::kCap) {
-          w = capped_weight(a, s[kb][e]);
-          if (masked) w = s[kb][e] == kUnseen ? 0.f : w;
-        } else {
-          w = __builtin_amdgcn_exp2f(s[kb][e] * c - mc);
-        }
+        const float w = __builtin_amdgcn_exp2f(s[kb][e] * c - mc);
         sum += w;
         p[2 * kb + e / 8][e % 8] = static_cast<half_t>(w);
       }
@@ -964,9 +974,7 @@ struct WaveTile {
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      float w;
-      if constexpr (V::kCap) w = s[e] == kUnseen ? 0.f : capped_weight(a, s[e]);
-      else w = __builtin_amdgcn_exp2f(s[e] * a.c - mc);
+      const float w = __builtin_amdgcn_exp2f(s[e] * unit(a) - mc);
       sum += w;
       p[e / 8][e % 8] = static_cast<half_t>(w);
     }
@@ -985,8 +993,12 @@ struct WaveTile {
   // values yet.
   __device__ __forceinline__ void settle(float16_t& s, float top, float over, half8_t (&p)[2], int key0, int begin,
                                          int end, bool masked, const AttentionArgs& a) {
-    const float c = a.c;
+    const float c = unit(a);
     if constexpr (V::kCap || V::kMore) {
+      if constexpr (V::kCap) {
+        cap_scores(a, s, top);
+        over = top - m;
+      }
       if (masked) {
         top = row_max(mask(s, key0, begin, end));
         over = (top - m) * c;
@@ -1005,7 +1017,7 @@ struct WaveTile {
     }
     const bool grown = over > 8.f;  // as in step()
     if (__any(grown)) {
-      const float next_c = scaled(a, top) - kLift;
+      const float next_c = top * c - kLift;
       const float keep = !grown ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - next_c);
       scale_sum(keep);
 #pragma unroll
@@ -1030,30 +1042,11 @@ struct WaveTile {
   __device__ __forceinline__ void block(const float16_t& s, float16_t& next, const half8_t (&p)[2], half8_t (&made)[2],
                                         const Lanes& at, uint32_t k_off, uint32_t v_off, bool more,
                                         const AttentionArgs& a, int next_key, float& top, float& over, F at_step) {
-    const float c = a.c;
+    const float c = unit(a);
     constexpr int STEPS = 2 * N;
     float w[16], sum;
     u32x4 packed[2];
-    float ex[16], lift = 0.f, drop = 0.f;
-    if constexpr (V::kCap) {
-      lift = a.cap - mc;
-      drop = -2.f * a.cap;
-    }
     if constexpr (V::kSlopes) next = before(next_key);
-    // with CAP a weight is three operations in turn, each an element behind the one before it
-    auto first_of = [&](int e) {
-      ex[e] = 1.f + __builtin_amdgcn_exp2f(s[e] * a.cap_in);
-      asm volatile("" : "+v"(ex[e]));
-    };
-    auto second_of = [&](int e) {
-      ex[e] = __builtin_amdgcn_rcpf(ex[e]);
-      asm volatile("" : "+v"(ex[e]));
-    };
-    if constexpr (V::kCap) {
-      first_of(0);
-      first_of(1);
-      second_of(0);
-    }
     auto add = [&](int e) {
       sum = e == 0 ? w[0] : sum + w[e];
       asm volatile("" : "+v"(sum));
@@ -1081,14 +1074,7 @@ struct WaveTile {
         // computed here, not where it is used: the compiler would move it
         // there (the empty asm statements); a weight is added up a step later,
         // when the exponential is there
-        if constexpr (V::kCap) {
-          if (e + 2 < 16) first_of(e + 2);
-          w[e] = __builtin_amdgcn_exp2f(fmaf(drop, ex[e], lift));
-          w[e] = s[e] == kUnseen ? 0.f : w[e];
-          if (e + 1 < 16) second_of(e + 1);
-        } else {
-          w[e] = __builtin_amdgcn_exp2f(s[e] * c - mc);
-        }
+        w[e] = __builtin_amdgcn_exp2f(s[e] * c - mc);
         asm volatile("" : "+v"(w[e]));
         if (e >= 1) add(e - 1);
       }
@@ -1100,7 +1086,6 @@ struct WaveTile {
       }
       if (i == SCORED + 4) {
         top = row_max(top);
-        if constexpr (V::kCap) top = fmaxf(top, kLeast);
         over = (top - m) * c;
         asm volatile("" : "+v"(top), "+v"(over));
       }

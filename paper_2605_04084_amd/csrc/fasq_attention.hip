@@ -104,7 +104,7 @@ hipError_t launch_attention(const AttentionProblem& p, const DeviceInfo& dev, hi
   a.slope_unit = (float)(1.4426950408889634074 / a.c);
   a.cap = (float)(more.softcap * 1.4426950408889634074);
   a.classes = pl.classes;
-  a.cap_in = cap ? (float)(2.0 * a.c / more.softcap) : 0.f;
+  a.cap_unit = cap ? (float)(a.c / (more.softcap * 1.4426950408889634074)) : 0.f;
   if (cap) return slopes ? launch_variant<Variant<true, true, true>>(pl, a, stream) : launch_variant<Variant<true, true, false>>(pl, a, stream);
   return slopes ? launch_variant<Variant<true, false, true>>(pl, a, stream) : launch_variant<Variant<true, false, false>>(pl, a, stream);
 }

@@ -483,10 +483,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       }
       top = t.row_max(top);
       top1 = t.row_max(top1);
-      if constexpr (V::kCap) {
-        top = fmaxf(top, kLeast);
-        top1 = fmaxf(top1, kLeast);
-      }
       t.settle(s0, top, (top - t.m) * a.c, p1, lo, mine.begin, mine.end, masked(lo), a);
       t.weights(s0, p0, a);
       t.settle(s1, top1, (top1 - t.m) * a.c, p0, lo + 32, mine.begin, mine.end, masked(lo + 32), a);
