@@ -549,7 +549,7 @@ int64_t fasq_paged_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int H
  * belongs to request s = requests[r].  A field that is NULL is not there.
  *
  *   requests      int32 [R]; NULL: row r is request r (S = R).  A row whose request
- *                 lies outside [0, S) is neither read nor written
+ *                 lies outside [0, S) is not written
  *   S             requests, at most 2^24
  *   tokens        int32 [S rows of max_tokens, token_stride apart]: a request's
  *                 prompt and then its answer so far, token_count[s] of them (int32
