@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
     } else if (given.window > 0 && given.causal) {  // the longest there can be
       length = tile_length<V, ROWS, STEP>(given, Request{0, 0, INT32_MAX}, INT32_MAX, true);
     }
-    const bool whole = length > 0 && length * DP <= 384 * 128;
+    const bool whole = length > 0 && (length - tile_extra<V, ROWS>(given)) * DP <= 384 * 128;
     const int parts = classes == 2 ? given.parts / 2 : given.parts;  // of a class
     share = share_of<STEP>(head_len * given.Hkv, parts, whole ? (int)length : kTileShare);
     if (whole) share = quotient(share - 1, length) * length + length;
