@@ -432,7 +432,7 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
           if (!(met[g] >> e & 1)) continue;
           const uint32_t k = counts[(g * WAVES + wave) * 512 + e * kWave + lane];
           const float y = x[g][e], times = (float)(k & ~kInPrompt);
-          const float z = y * (y > 0.f ? one_over : rho) - (frequency * times + (times > 0.f ? presence : 0.f));
+          const float z = y * (y > 0.f ? one_over : rho) - (times > 0.f ? frequency * times + presence : 0.f);
           x[g][e] = k != 0 ? z : y;
         }
       }

@@ -237,6 +237,17 @@ def test_temperature_of_zero_divides_nothing():
     b.both(("temperature",))
 
 
+def test_infinite_penalties_spare_the_prompt():
+    logits = torch.arange(1, 21, dtype=torch.float32).reshape(1, 20).cuda()
+    got, choice, lse = fasq.process_logits(
+        logits, tokens=to_dev(np.array([[19, 18, 17, 18]], dtype=np.int32)), token_count=to_dev(np.array([4], dtype=np.int32)),
+        prompt_len=to_dev(np.array([2], dtype=np.int32)), repetition=to_dev(np.array([2], dtype=np.float32)),
+        frequency=to_dev(np.array([np.inf], dtype=np.float32)), choose=True)
+    want, best, _ = lo.process_logits(to_np(logits)[0], True, [19, 18, 17, 18], 2, repetition=2.0, frequency=np.inf)
+    assert (to_np(got)[0] == want).all()  # halves and infinities are exact
+    assert int(choice) == best == 16 and np.isfinite(float(lse))
+
+
 def test_trees_at_the_ends():
     """Fewer words than nodes, more nodes than threads, rows of no bit, starts past the rows."""
     b = Rows(1, 300, 70, seed=9)
