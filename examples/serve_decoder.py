@@ -262,6 +262,8 @@ def answer_drafted(dec: Decoder, prompts, first, adapters, count: int, draft=gue
     text = [list(map(int, p)) + [int(t)] for p, t in zip(prompts, first)]
     rows, steps = [[] for _ in range(B)], 0
     ends = [len(t) + count for t in text]
+    if max(ends) - 1 > cfg.max_len:  # the last token is not cached
+        raise ValueError(f"a request holds at most {cfg.max_len} tokens")
     held = torch.zeros((B, cfg.max_len), dtype=torch.int32)
     for b, t in enumerate(text):
         held[b, :len(t)] = torch.tensor(t)
@@ -286,6 +288,8 @@ def answer_drafted(dec: Decoder, prompts, first, adapters, count: int, draft=gue
         positions, kv_len = i32(np.array(start)[req]) + depth, i32([s + m for s, m in zip(start, n)])
         spans = None
         if cfg.window:
+            if int(depth.max()) >= cfg.window:  # a span cannot tell a branch's first nodes from its siblings
+                raise ValueError("guesses deeper than the window")
             spans = torch.stack([(positions - cfg.window + 1).clamp_(min=0), kv_len[i32(req).long()]], 1)
         drafted = i32(np.concatenate([t for t, _ in trees]))
         batch = Batch(positions, i32(slots), i32(np.asarray(adapters)[req]), i32(first_row), kv_len, tree, spans)

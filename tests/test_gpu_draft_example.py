@@ -79,3 +79,17 @@ def test_guesses():
     assert ex.guess([5, 7, 9, 5]) == ([5, 7, 9, 5], [-1, 0, 1, 2])
     assert ex.guess([1, 2]) == ([2], [-1])
     assert ex.guess([3, 1, 3, 2, 3], branches=2, depth=1) == ([3, 2, 1], [-1, 0, 0])
+
+
+def test_answers_that_do_not_fit():
+    cfg = ex.Config(hidden=256, inter=384, vocab=300, max_len=40, window=2, page_size=12)
+    dec = ex.Decoder(cfg, ex.draw_weights(cfg, seed=3), 1)
+    prompts = [np.arange(30)]
+    first = dec.next_tokens(ex.read_prompts(dec, prompts, [-1], 48)[0][-1:]).tolist()
+    alone = lambda text: ([text[-1]], [-1])
+    with pytest.raises(ValueError, match="at most 40"):
+        ex.answer_drafted(dec, prompts, first, [-1], 11, alone)
+    with pytest.raises(ValueError, match="window"):
+        ex.answer_drafted(dec, prompts, first, [-1], 10, lambda text: ([text[-1], 1, 2], [-1, 0, 1]))
+    said, _, steps = ex.answer_drafted(dec, prompts, first, [-1], 10, alone)  # the longest there can be
+    assert steps == 10 and len(said[0]) == 10
