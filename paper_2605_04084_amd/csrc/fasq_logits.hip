@@ -541,14 +541,20 @@ struct LogitsPlan {
 // else two.  One row of 128256, 64 rows, 16 trees of 32 rows, 5 rows with histories of
 // 131072: 7.0 / 25 / 47 / 19 us with one group, 8.7 / 23.9 / 39 / 22 with two; 9 / 23 /
 // 41 / 31 with 256 threads, 11.6 / 26.6 / 49 / 24 with 1024 and two groups (kernel
-// times).  Eight rows of a request share the counts of a slice: with one row a
+// times).  Up to eight rows of a request share the counts of a slice: with one row a
 // workgroup 16 trees take 60 us in all, with eight 42.
 LogitsPlan plan_logits(int64_t R, int64_t V, int64_t rows_of_request, const DeviceInfo& dev) {
   LogitsPlan p;
-  p.rows = (int)(rows_of_request > 8 ? 8 : rows_of_request);
   p.threads = 512;
   p.groups = R * V > (int64_t)dev.num_cus * 4096 ? 2 : 1;
   p.slices = (int)((V + p.threads * p.groups * kEach - 1) / (p.threads * p.groups * kEach));
+  // Rows one after the other share what is counted, but only what the chip does not hold
+  // at once (two workgroups a compute unit).  3 requests of 53 rows of 8550: 20 us, 47
+  // eight by eight; 3 of 36 rows of 146672 25.6 and 31.8; 4 of 16 rows of 128256 19 and
+  // 33; 16 of 16 rows take 50 with three workgroups a unit in place of 40.
+  const int64_t rows = R * p.slices / (2 * dev.num_cus);
+  p.rows = (int)(rows < rows_of_request ? rows : rows_of_request);
+  p.rows = p.rows < 1 ? 1 : p.rows > 8 ? 8 : p.rows;
   return p;
 }
 

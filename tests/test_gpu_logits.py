@@ -330,3 +330,24 @@ def test_tensors_are_checked():
                dict(workspace=torch.empty(16, dtype=torch.uint8, device="cuda:0"), logits=torch.zeros((6, 9000), **f32), allowed=None)):
         with pytest.raises((fasq.FasqError, ValueError)):
             b.run(**kw)
+
+
+@pytest.mark.parametrize("V, n, wide", [(131, 33, False), (131, 12, True), (517, 33, False), (517, 33, True)])
+def test_many_rows_of_a_request(V, n, wide):
+    """More rows than the chip holds at once: several follow each other in a workgroup."""
+    b = Rows(130, n, V, wide=wide, seed=20)
+    b.both()
+    rng = np.random.default_rng(21)
+    b.requests = np.repeat(rng.integers(-1, 131, -(-130 * n // 3)), 3)[:130 * n].astype(np.int32)
+    logits = to_dev(b.logits)
+    names = Rows.ALL[:10]
+    got = b.both(names, logits=logits, out=logits)  # in place
+    none = (b.requests < 0) | (b.requests > 129)
+    assert none.any() and np.array_equal(got[0][none], b.logits[none])
+    # a few of them alone, one to a workgroup
+    few = slice(0, 40)
+    args = {k: to_dev(getattr(b, k)) for k in names if k != "allowed"}
+    alone = fasq.process_logits(to_dev(b.logits[few]), to_dev(b.requests[few]), requests_count=130, choose=True,
+                                allowed=to_dev(b.allowed[few]), **args)
+    assert np.array_equal(to_np(alone[0])[~none[few]], got[0][few][~none[few]])
+    assert np.array_equal(to_np(alone[1])[~none[few]], got[1][few][~none[few]])
