@@ -113,7 +113,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
 
   const RowCopy<DP, FULL> copy(given);
   const bool shared = given.part_o != nullptr;
-  const Batch<V> batch(given);
+  const Batch<V> batch(given, ROWS, nullptr);
   const int64_t head_len = head_length<V, ROWS, STEP>(given, batch, shared);
   int64_t pos, pos_end, share = 0, w = blockIdx.x;
   int head;
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
 
   const RowCopy<DP, FULL> copy(given);
   const bool shared = given.part_o != nullptr;
-  const Batch<V> batch(given);
+  const Batch<V> batch(given, ROWS, flag + 4);
   // With two classes every request's even tiles lie in the first half of the line,
   // its odd ones at the same places of the second: workgroups of one compute unit
   // then read the same keys at the same time, once from memory (see plan_attention).

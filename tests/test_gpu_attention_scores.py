@@ -287,3 +287,27 @@ def test_trees_in_windows(reqs, Hq, Hkv, D):
     spans = np.stack([np.maximum(0, start + depth.numpy() - 99), np.repeat([kv for _, kv in reqs], [n for n, _ in reqs])], 1).astype(np.int32)
     b.both(tree=tree.numpy(), spans=spans)
     b.both(tree=tree.numpy(), spans=spans, workspace=torch.empty(0, dtype=torch.uint8, device="cuda:0"))
+
+
+@pytest.mark.parametrize("n", [63, 65, 300, 1000, 2030, 4096, 4097])
+@pytest.mark.parametrize("Hq,Hkv,D", [(1, 1, 64), (3, 1, 80), (7, 1, 128)])
+def test_one_request_of_many_runs(n, Hq, Hkv, D):
+    """Shares by the longest run of a tile: documents, a long run among short ones at any place, runs of nothing."""
+    rng = np.random.default_rng(n + Hq)
+    b = Scored([(n, n)], Hq, Hkv, D, 20, seed=n)
+    ends = np.unique(np.append(rng.integers(1, n, 7), n))
+    spans = np.zeros((n, 2), dtype=np.int32)
+    begin = 0
+    for end in ends:
+        spans[begin:end, 0] = begin
+        spans[begin:end, 1] = np.maximum(np.arange(begin, end) + 1, min(begin + 9, end))
+        begin = end
+    b.both(spans=spans)
+    short = np.stack([np.maximum(0, np.arange(n) - 5), np.arange(n) + 1], 1).astype(np.int32)
+    for at in (0, n // 2, n - 1):
+        spans = short.copy()
+        spans[at] = 0, n
+        b.both(spans=spans)
+    spans[:] = 7, 7
+    spans[n // 3] = n - 40, n
+    b.both(spans=spans)
