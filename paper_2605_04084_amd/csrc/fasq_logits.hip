@@ -122,6 +122,11 @@ __device__ __forceinline__ float larger(float a, float b, float c) {
 __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// Up to here top * kLog2e is off by at most 2^-4 (half an ulp of 2^20.6), so that weights relative to the
+// rounded product lie within 2^(2^-4) of those relative to `top`.  From 2^31 on it may be off by 2^7
+// and more, which fp32 does not hold as a power of two.
+constexpr float kCloseTop = 1048576.f;
+
 // What a wave's logits come to, in its first lane.  first: the index of x[0][0] in lane
 // 0; lanes lie side by side, groups `apart`.
 template <int GROUPS>
@@ -137,7 +142,8 @@ __device__ __forceinline__ Found find(const float (&x)[GROUPS][kEach], int first
   top = wave_join(top, [](float a, float b) { return larger(a, b); });
   Found f = {0, top, 0.f};
   const float c = top * kLog2e;
-  if (fabsf(top) < 1e38f) {
+  const bool close = fabsf(top) < kCloseTop;
+  if (close) {
     // one operation fewer than (x - top) * kLog2e; what the product rounds is made good below
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
@@ -148,7 +154,7 @@ __device__ __forceinline__ Found find(const float (&x)[GROUPS][kEach], int first
       for (int e = 0; e < kEach; e += 2) w[e] += w[e + 1];
       f.sum += (w[0] + w[2]) + (w[4] + w[6]);
     }
-  } else {  // infinite ones, and masks of the type's lowest value
+  } else {  // infinite ones, and masks of large values
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
@@ -157,8 +163,16 @@ __device__ __forceinline__ Found find(const float (&x)[GROUPS][kEach], int first
                                 : __builtin_amdgcn_exp2f((x[g][e] - top) * kLog2e);
   }
   f.sum = wave_join(f.sum, sum_of);
-  if (fabsf(top) < 1e38f) f.sum *= __builtin_amdgcn_exp2f(-fmaf(top, kLog2e, -c));
-  const bool nan = f.sum != f.sum;  // then some logit is
+  if (close) f.sum *= __builtin_amdgcn_exp2f(-fmaf(top, kLog2e, -c));
+  bool nan = false;  // some logit is: a sum of others is a number
+  if (f.sum != f.sum) {
+    bool own_nan = false;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) own_nan |= x[g][e] != x[g][e];
+    nan = __any(own_nan);
+  }
   uint32_t at = 0;
 #pragma unroll
   for (int g = GROUPS - 1; g >= 0; --g) {
