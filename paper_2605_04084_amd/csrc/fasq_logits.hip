@@ -481,6 +481,13 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
       for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
         for (int e = 0; e < kEach; ++e) x[g][e] = x[g][e] * cool;
+      if (left < SLICE) {  // what lies past the vocabulary stays -inf: an infinite temperature makes NaN of it
+        const int there = again(left);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) x[g][e] = (g * TH + tid) * kEach + e < there ? x[g][e] : -INFINITY;
+      }
     }
     if (a.allowed != nullptr) {
 #pragma unroll
