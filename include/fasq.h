@@ -561,7 +561,8 @@ int64_t fasq_paged_attention_workspace_bytes(int64_t T, int64_t B, int Hq, int H
  *   presence      > 0 times in the answer
  *   bias_ids      int32 [S x max_bias] (at most 2^24) and bias_values fp32: added to these tokens'
  *   bias_values   logits; a token's last entry counts, ids outside [0, V) do not
- *   temperature   fp32 [S]: times 1 / temperature where that is positive
+ *   temperature   fp32 [S]: times 1 / temperature where that is positive (one below 2^-128
+ *                 counts as that; infinity makes every finite logit 0)
  *   allowed       int32 [R rows of ceil(V / 32) words, allowed_stride apart]: a token
  *                 whose bit v % 32 of word v / 32 is clear becomes -inf, whatever it was
  *   draft_tokens  int32 [R], q_start int32 [S + 1], tree as in fasq_attention_scores:

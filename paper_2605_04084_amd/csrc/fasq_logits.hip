@@ -421,7 +421,8 @@ __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) 
         }
       }
       one_over = 1.f / rho;
-      cool = tau > 0.f ? 1.f / tau : 1.f;
+      // fp32 holds no reciprocal of less than 2^-128; an infinite one would make NaN of zeros
+      cool = tau > 0.f ? fminf(1.f / tau, 3.402823466e38f) : 1.f;
     }
 
     int bits[GROUPS];

@@ -49,3 +49,26 @@ def test_infinite_temperatures(V, count, rules):
         else:
             n = int(bits[r].sum())
             assert choice[r] == bits[r].argmax() and abs(lse[r] - np.log(n)) <= 2.0 ** -19 + 2.0 ** -22 * np.log(n)
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -127, 1e-39, 2.0 ** -149])
+def test_temperatures_without_a_reciprocal(tau):
+    """Below 2^-128 fp32 holds no reciprocal: a logit of zero stays zero, and all others are too large
+    for fp16 (the smallest, 2^-24, becomes 2^103 at least)."""
+    rng = np.random.default_rng(3)
+    x = (rng.standard_normal((3, 5000)) * 3).astype(np.float16)
+    x[:, ::7] = 0
+    x[0] = -np.abs(x[0])      # zeros are the largest
+    x[1, 4321] = 2.0 ** -24
+    x[1, :4321] = 0
+    x[1, 4322:] = -1
+    x[2] = np.where(x[2] > 0, -x[2], x[2])
+    x[2, 4000:] = -3
+    x[2, :4000] = np.where(x[2, :4000] == 0, -1, x[2, :4000])
+    got = fasq.process_logits(to_dev(x), temperature=torch.full((3,), tau, dtype=torch.float32, device="cuda:0"), choose=True)
+    out, choice, lse = (to_np(t) for t in got)
+    with np.errstate(over="ignore", invalid="ignore"):
+        assert np.array_equal(out, np.where(x == 0, 0, np.sign(x.astype(np.float32)) * np.inf).astype(np.float16))
+    assert choice[0] == (x[0] == 0).argmax() and choice[1] == 4321
+    assert abs(lse[0] - np.log((x[0] == 0).sum())) <= 2.0 ** -19 + 2.0 ** -22 * 9
+    assert x[2, choice[2]] < 0 and not np.isnan(lse).any()
