@@ -630,7 +630,8 @@ __device__ __forceinline__ bool cut_to_finite(uint16_t* values) {
 // rather than 2^-25, which a sum over 131072 keys beside one far larger shows.
 // With kLift 7 and a maximum up to 2^8 behind they stay below fp16's largest
 // value, but for scores of 2^24 powers of two and more, whose rounding may pass
-// it: such rows end not finite and are computed again (SlowRow).
+// it, or take the weights below what they need: such rows end not finite (total)
+// and are computed again (SlowRow).
 constexpr float kLift = 7.f;
 
 // Capped scores cap * tanh(x), in powers of two.  Arguments up to kSmall by a
@@ -1144,15 +1145,18 @@ struct WaveTile {
   // What partial results' weights are relative to, in powers of two.
   __device__ __forceinline__ float top() const { return m == -INFINITY ? m : mc; }
 
-  // Sum of the row's weights, in both its lanes.
-  __device__ __forceinline__ float total() const {
+  // Sum of the row's weights, in both its lanes; NaN where even the largest has lost 2^2
+  // of its 2^kLift to the rounding of mc, which takes fp16's bits from all of them, or all of them
+  // to zero (scores of 2^26 powers of two and more).
+  __device__ __forceinline__ float total(const AttentionArgs& a) const {
     const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+    const bool lost = m > -INFINITY && fmaf(m, unit(a), -mc) < kLift - 2.f;
+    return lost ? __builtin_nanf("") : __uint_as_float(w[0]) + __uint_as_float(w[1]);
   }
 
-  // Whether this lane's part of the row holds a value that is not finite.
-  __device__ __forceinline__ bool broken() const {
-    float z = (l - l) + (mc - mc);
+  // Whether this lane's part of the row, whose sum is `sum`, holds a value that is not finite.
+  __device__ __forceinline__ bool broken(float sum) const {
+    float z = (sum - sum) + (mc - mc);
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
 #pragma unroll

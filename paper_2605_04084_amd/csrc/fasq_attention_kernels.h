@@ -205,7 +205,7 @@ __global__ __launch_bounds__(NW * kWave, 1) void k_attention_few(AttentionArgs) 
     }
     // ---- join the waves
     __syncthreads();
-    const float l = t.total();
+    const float l = t.total(a);
     if (alive) {
       float* o = jo + (wave * 32 + l32) * OS;
 #pragma unroll
@@ -541,8 +541,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
       }
       wait_loads<0>();  // copies behind the end
     }
-    const float l = t.total();
     const AttentionArgs end = fresh_args();
+    const float l = t.total(end);
     const bool cut = shared && (t0 < pos || seg_end < t1);
     const int64_t slot = cut ? slot_of(w, share, t0) : 0;
     if (shared && seg_end == pos_end && threadIdx.x == 0)
@@ -576,7 +576,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void k_attention_tile(Atten
               final_lse<V>(t.top(), l, sees, end, p.r, head, row0 + l32);
       }
     }
-    uint64_t broken = __ballot(alive && t.broken());
+    uint64_t broken = __ballot(alive && t.broken(l));
     broken = (broken | broken >> 32) & 0xFFFFFFFFu;
     __syncthreads();
     uint64_t again = *flag != 0 && live > 0 ? (uint64_t(1) << live) - 1 : broken;
