@@ -700,15 +700,11 @@ struct WaveTile {
       // at most 2^31 - 1024 + 64: keys behind the last one may be named
       const int back = bias.pos - key0 - h4 - bias.nearest;
       if (__all(bias.pos - key0 - 31 >= 0)) {
-        const float base = bias.slope * (float)back;
+        // each key's distance as a number first, exact below 2^24: from one key to the next by
+        // sums of slopes, the last of a block would keep what rounded the first one's bias
+        const float far = (float)back;
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          // factors that instructions hold themselves: no registers for them
-          s[e] = e == 0 ? base : fmaf(bias.slope, -4.f, fmaf(bias.slope, -4.f, s[e == 0 ? 0 : e - 4]));
-          s[e + 1] = s[e] - bias.slope;
-          s[e + 2] = fmaf(bias.slope, -2.f, s[e]);
-          s[e + 3] = fmaf(bias.slope, -2.f, s[e + 1]);
-        }
+        for (int e = 0; e < 16; ++e) s[e] = bias.slope * (far - (float)((e / 4) * 8 + e % 4));
       } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
