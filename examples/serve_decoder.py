@@ -254,6 +254,19 @@ def guess(text, branches: int = 2, depth: int = 4):
     return tokens, parents
 
 
+def first_tokens(dec: Decoder, prompts, rows):
+    """The likeliest token after each prompt, whose output rows these are, with the penalty for the prompt's own tokens."""
+    rules = {}
+    if dec.cfg.repetition != 1.0:
+        held = np.zeros((len(prompts), max(map(len, prompts))), dtype=np.int32)
+        for b, p in enumerate(prompts):
+            held[b, :len(p)] = p
+        count = np.array([len(p) for p in prompts], dtype=np.int32)
+        rules = dict(tokens=torch.from_numpy(held).to(dec.device), token_count=torch.from_numpy(count).to(dec.device),
+                     repetition=torch.full((len(prompts),), dec.cfg.repetition, device=dec.device))
+    return dec.next_tokens(torch.stack([r[-1] for r in rows]), **rules)
+
+
 def answer_drafted(dec: Decoder, prompts, first, adapters, count: int, draft=guess):
     """At least ``count`` tokens of every request after its prompt, from the
     tokens ``first`` on, several a step where ``draft`` guesses them.  Returns the
@@ -349,7 +362,7 @@ def main():
     torch.cuda.synchronize()
     t0 = time.perf_counter()
     rows = read_prompts(dec, prompts, adapters, chunk)
-    first = dec.next_tokens(torch.stack([r[-1] for r in rows]))
+    first = first_tokens(dec, prompts, rows) if drafted else dec.next_tokens(torch.stack([r[-1] for r in rows]))
     torch.cuda.synchronize()
     t1 = time.perf_counter()
     steps = count
