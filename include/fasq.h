@@ -501,8 +501,9 @@ fasq_status fasq_paged_attention(const void* q, int64_t q_token_stride, int64_t 
  *
  *   softcap  c > 0: a score s becomes c * tanh(s / c).  2^-10 <= c <= 1024, |scale|
  *            <= 2^64; a capped score is off by at most 2^-21 c
- *   slopes   fp32 [Hq], finite: query head h at position p adds -slopes[h] * |p - j|
- *            to its score with key j (before a cap).  2^-24 <= |scale| <= 2^64
+ *   slopes   fp32 [Hq]: query head h at position p adds -slopes[h] * |p - j| to its
+ *            score with key j (before a cap).  2^-24 <= |scale| <= 2^64; slopes[h] / scale
+ *            within fp32, and negative ones times the longest distance too
  *   spans    int32 [T x 2]: token t sees the keys spans[t][0] <= j < spans[t][1]
  *            (cut to what there is) in place of causal and window (window must
  *            be 0): documents packed into one request, prefixes that are read in
@@ -599,7 +600,7 @@ typedef struct {
  *
  *   logits  fp16, or fp32 with logits_fp32; rows `stride` elements apart.  V <= 2^30
  *   out     fp16 or fp32 (out_fp32), rows out_stride apart, or NULL; may be logits
- *           (of the same type and stride)
+ *           (of the same type and stride), and overlaps nothing else
  *   choice  int32 [R] or NULL: the token of the largest value (before it is
  *           rounded to out), the lowest of equal ones; NaN is larger than
  *           all; -1 where every value is -inf

@@ -326,9 +326,9 @@ struct Place {
 // Positions behind a tile's last key, for what a tile of 128 rows costs besides its
 // keys (queries to fetch, rows to leave): without them the share that gets several
 // tiles of few keys is the last to end.  A prompt's 509 tokens, a short prompt and 22
-// single tokens on 77 to 3001 keys (12/4 heads of 80, pages of 20, slopes): 69.5 us without, 55.3 /
-// 55.0 / 58.3 with 192 / 256 / 384; 16 trees of 32 nodes on 300 to 8192 keys (32/8
-// heads of 128): 78.4, and 69.7 / 72.6 / 67.7.  One request's tiles are all of a kind,
+// single tokens on 77 to 3001 keys (12/4 heads of 80, pages of 20, slopes): 71.3 us without, 56.8 /
+// 56.1 / 60.6 with 192 / 256 / 384; 16 trees of 32 nodes on 300 to 8192 keys (32/8
+// heads of 128): 72.5, and 68.9 / 71.3 / 66.1.  One request's tiles are all of a kind,
 // and the plain variant's shares stay as they were.
 constexpr int kTileExtra = 256;
 template <class V, int ROWS>

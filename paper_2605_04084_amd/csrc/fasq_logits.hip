@@ -226,10 +226,10 @@ struct Eight<float> {
 // wave's largest and sum leave for the join.  Eight neighbouring logits a thread are
 // one 16-byte load and one byte of a grammar.
 //
-// 64 rows of 128256 fp16 logits to fp32 with all rules (51 MB): 23.8 us, 2.1 TB/s, bound
-// by the counting before the pass and by vector instructions; 512 rows in 16 trees,
-// nothing written: 39 us, 22 to 25 of it the pass alone; histories of 131072 tokens: 19 us,
-// of which LDS atomics of the slice with most of them are the most.
+// 64 rows of 128256 fp16 logits to fp32 with all rules (51 MB): 24.5 us, 2.1 TB/s, bound
+// by the counting before the pass and by vector instructions; 256 rows in 16 trees,
+// nothing written: 39 us, 22 to 25 of it the pass alone; 5 histories of 20000 to 100000 tokens:
+// 19 us, of which LDS atomics of the slice with most of them are the most.
 template <typename T, int TH, int GROUPS>
 __global__ __launch_bounds__(TH, GROUPS == 2 ? 5 : 7) void k_logits(LogitsArgs) {
 #pragma clang fp contract(off)
@@ -560,8 +560,8 @@ struct LogitsPlan {
 };
 
 // 512 threads with one group of eight logits a thread up to 16 logits a lane of the chip,
-// else two.  One row of 128256, 64 rows, 16 trees of 32 rows, 5 rows with histories of
-// 131072: 7.0 / 25 / 47 / 19 us with one group, 8.7 / 23.9 / 39 / 22 with two; 9 / 23 /
+// else two.  One row of 128256, 64 rows, 16 trees of 16 rows, 5 rows with histories of
+// 20000 to 100000: 7.0 / 25 / 47 / 19 us with one group, 8.7 / 23.9 / 39 / 22 with two; 9 / 23 /
 // 41 / 31 with 256 threads, 11.6 / 26.6 / 49 / 24 with 1024 and two groups (kernel
 // times).  Up to eight rows of a request share the counts of a slice: with one row a
 // workgroup 16 trees take 60 us in all, with eight 42.
