@@ -1004,6 +1004,8 @@ def process_logits(logits, requests=None, *, tokens=None, token_count=None, prom
                 S = t.shape[0]
                 break
         else:
+            if q_start is not None:
+                _require(q_start, "q_start", i32, 1)
             S = (1 << 24) if q_start is None else q_start.shape[0] - 1
     of_request, of_row = (S,), (R,)
 
